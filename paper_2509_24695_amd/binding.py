@@ -3,7 +3,7 @@ the module _sventry (csrc/py_entry.cpp), which takes 1.2 us per call for it wher
 for one interpreter; another one that imports the package makes these calls through ctypes as well.
 
 The functions carry the names and argument order of the C ABI
-(include/sv_linattn.h, include/sv_tconv.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
+(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
 device addresses); nothing here computes, and there is no fallback: if the
 shared library is missing, loading raises.
 """
@@ -27,6 +27,8 @@ EXPORTS = (
     "sv_linattn_workspace_status_offset", "sv_linattn_workspace_status", "sv_linattn_set_wait_limit",
     "sv_block_linattn_step_static", "sv_measure_apply_variant",
     "sv_measure_assume_dies", "sv_mfma_stream", "sv_measure_tconv_variant",
+    "sv_decay_linattn_workspace_bytes", "sv_decay_linattn_backward_workspace_bytes", "sv_decay_linattn",
+    "sv_decay_linattn_token", "sv_decay_linattn_backward",
 )
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -114,6 +116,14 @@ def load_library():
         f.restype = ctypes.c_int
     lib.sv_tconv_block_step.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
     lib.sv_tconv_block_step.restype = ctypes.c_int
+    fl = ctypes.c_float
+    for f in (lib.sv_decay_linattn_workspace_bytes, lib.sv_decay_linattn_backward_workspace_bytes):
+        f.argtypes, f.restype = [i32, i32, i32, i32], sz
+    lib.sv_decay_linattn.argtypes = [vp, vp, vp, dp, vp, vp, fl, vp, vp, vp, dp, vp, sz, vp]
+    lib.sv_decay_linattn_token.argtypes = [vp, vp, vp, dp, vp, vp, i32, fl, vp, vp, vp, dp, vp]
+    lib.sv_decay_linattn_backward.argtypes = [vp, vp, vp, dp, vp, dp, vp, vp, fl, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    for f in (lib.sv_decay_linattn, lib.sv_decay_linattn_token, lib.sv_decay_linattn_backward):
+        f.restype = ctypes.c_int
     lib.sv_measure_apply_variant.argtypes = [i32, vp, dp, i32, i32, vp, vp, ctypes.c_float, vp, vp]
     lib.sv_measure_apply_variant.restype = ctypes.c_int
     lib.sv_measure_assume_dies.argtypes = [i32]
@@ -386,6 +396,37 @@ def sv_tconv_block_step(x, W, cache_in, y, cache_out, B: int, T: int, HW: int, D
     x, y [B][T][HW][D], W [3][D][D], cache_in / cache_out [B][HW][D] or None."""
     _check((_entry or _calls()).sv_tconv_block_step(x, W, cache_in, y, cache_out, B, T, HW, D, dtype, stream),
            "sv_tconv_block_step")
+
+
+def sv_decay_linattn_workspace_bytes(B: int, H: int, n_tokens: int, d: int) -> int:
+    return int(load_library().sv_decay_linattn_workspace_bytes(int(B), int(H), int(n_tokens), int(d)))
+
+
+def sv_decay_linattn_backward_workspace_bytes(B: int, H: int, n_tokens: int, d: int) -> int:
+    return int(load_library().sv_decay_linattn_backward_workspace_bytes(int(B), int(H), int(n_tokens), int(d)))
+
+
+def sv_decay_linattn(Q, K, V, qkv: TensorDesc, log_decay, lengths, scale: float, S_in, S_out, O, o: TensorDesc, workspace,
+                     workspace_bytes: int | None = None, stream=None) -> None:
+    """Causal linear attention with a decay for each head over whole sequences (include/sv_decay.h): log_decay [H] fp32, lengths [B]
+    int32 or None, S_in / S_out [B][H][d][d] fp32 or None."""
+    _check((_entry or _calls()).sv_decay_linattn(Q, K, V, qkv, log_decay, lengths, scale, S_in, S_out, O, o, workspace,
+                                                 workspace_bytes, stream), "sv_decay_linattn")
+
+
+def sv_decay_linattn_token(Q, K, V, qkv: TensorDesc, log_decay, slots, n_slots: int, scale: float, S_in, S_out, O, o: TensorDesc,
+                           stream=None) -> None:
+    """One token of each row of a batch on states of a pool (include/sv_decay.h): slots [B] int32 or None, S_in / S_out
+    [n_slots][H][d][d] fp32, the same tensor or two."""
+    _check((_entry or _calls()).sv_decay_linattn_token(Q, K, V, qkv, log_decay, slots, n_slots, scale, S_in, S_out, O, o, stream),
+           "sv_decay_linattn_token")
+
+
+def sv_decay_linattn_backward(Q, K, V, qkv: TensorDesc, dO, o: TensorDesc, log_decay, lengths, scale: float, S_in, dS_out, dQ, dK, dV,
+                              dS_in, workspace, workspace_bytes: int | None = None, stream=None) -> None:
+    """Gradients of sv_decay_linattn for Q, K, V and S_in (include/sv_decay.h)."""
+    _check((_entry or _calls()).sv_decay_linattn_backward(Q, K, V, qkv, dO, o, log_decay, lengths, scale, S_in, dS_out, dQ, dK, dV,
+                                                          dS_in, workspace, workspace_bytes, stream), "sv_decay_linattn_backward")
 
 
 def sv_measure_apply_variant(variant: int, Q, q: TensorDesc, tok_begin: int, tok_end: int, S, z, eps: float, O,

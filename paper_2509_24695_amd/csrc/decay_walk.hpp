@@ -1,0 +1,659 @@
+// Causal linear attention with a decay for each head, over whole sequences.
+//
+//   S_t = l S_{t-1} + k_t v_t^T          o_t = S_t^T q_t          l = exp(log_decay[h])
+//
+// In chunks of C tokens (rows i, j = 0..C-1; S the state before the chunk):
+//
+//   o_i = l^{i+1} S^T q_i + sum_{j <= i} l^{i-j} (q_i . k_j) v_j
+//   S  <- l^C S + sum_j l^{C-1-j} k_j v_j^T
+//
+// All four products run on the matrix cores; every power of l that occurs has an exponent >= 0, so nothing overflows however strong the
+// decay is.  The backward pass is the same walk three times, on other operands (WalkProblem):
+//
+//   dq   q, k, v = dO, V, K from the transposed state        forwards
+//   dv             K, Q, dO from the gradient of the state   backwards in time
+//   dk             V, dO, Q from its transpose               backwards in time
+//
+// Backwards, G_c = l^C G_{c+1} + sum_i l^{i+1} q_i do_i^T is what the tokens behind a chunk hand to it (G at the end: the gradient of
+// the final state), so with rows counted from the chunk's last token the state's factor is l^r where it is l^{r+1} forwards, and a row's
+// weight in the new state l^{C-r} where it is l^{C-1-r} (`back`).
+//
+// One workgroup walks one segment of one head's sequence, a wave per 32 value features: the wave keeps its 32 columns of S as fp32
+// accumulators over the whole segment, works out all of the chunk's C x C products for itself (C = 64, d = 128: 24 of its 94
+// matrix instructions) and so meets the other waves only where a chunk's tokens are handed over through LDS.  Products are arranged so
+// that a product's accumulators are the next one's operands as they lie: the lane of a 32 x 32 accumulator holds rows 8 (r / 4) + 4 h + r % 4
+// of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to the first
+// operand of a product in the order decay_row, which makes eight accumulators in a row eight consecutive indices.
+//
+// Roundings (bf16 tokens): S enters o as two bf16 pieces (together within 2^-16), the weighted values l^{..} v_j enter S as two pieces, so
+// that the state stays an fp32 one; the weighted scores l^{i-j} (q_i . k_j) are rounded to bf16 once, like the output (both 2^-8 of
+// a term at most).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix instructions).
+#pragma once
+
+#include "common.hpp"
+#include "decay_plan.hpp"
+
+namespace sv {
+
+constexpr int kDecayTableBytes = (96 + 2 * 64) * 4;
+constexpr uint32_t kNoRow = 0x80000000u;      // past every resource: the host keeps 64 rows below 2 GiB
+
+// Row m of a 32-row operand serves index decay_row(m): bits 2 and 3 change places.
+__host__ __device__ constexpr int decay_row(int m) { return (m & 0x13) | ((m & 4) << 1) | ((m & 8) >> 1); }
+
+// One walk over the sequences (device pointers; strides in elements).
+struct WalkProblem {
+    const void *q, *k, *v;
+    void *o;
+    TokStrides sq, sk, sv, so;
+    const float *s_begin;      // [BH][d][d]: state before the walk, NULL: zeros
+    float *s_end;              // [BH][d][d]: receives the state behind it, or NULL
+    float *slots;              // [BH][segments][d][d] partial states: begin of each segment
+    float weight_state;        // factor of what comes out of the state,
+    float weight_chunk;        //   of what comes out of the chunk itself,
+    float weight_update;       //   and of what goes into the state
+    int back;                  // 1: tokens from the last to the first, G's weights
+    int turned;                // 1: s_begin and slots hold the transpose of this walk's state
+};
+
+struct WalkArgs {
+    WalkProblem p[3];
+    const float *log_decay;    // [H]
+    const int32_t *lengths;    // [B] or NULL
+    int B, H, N;
+    int segments, per_segment;
+    int problems;
+    int together;              // neighbouring heads that one die takes in a row
+};
+
+// ---- operands ------------------------------------------------------------------------------------------------------
+
+// Eight consecutive indices of a contraction over 16 (lane half h: 8 h .. 8 h + 7), and the product over them.
+template <typename T> struct Oct;
+template <> struct Oct<uint16_t> {
+    bf16x8 v;
+};
+template <> struct Oct<float> {
+    float v[8];
+};
+__device__ __forceinline__ f32x16 oct_product(const Oct<uint16_t> &a, const Oct<uint16_t> &b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 oct_product(const Oct<float> &a, const Oct<float> &b, f32x16 c)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+    return c;
+}
+
+// Eight fp32 values as an operand: one piece, or (hi + lo) two.
+__device__ __forceinline__ void oct_from(const float (&x)[8], Oct<float> &o)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[e] = x[e];
+}
+__device__ __forceinline__ void oct_from(const float (&x)[8], Oct<uint16_t> &o)
+{
+    const u32x4 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+    o.v = __builtin_bit_cast(bf16x8, w);
+}
+template <typename T> struct Pieces;
+template <> struct Pieces<float> {
+    Oct<float> hi;
+    __device__ __forceinline__ explicit Pieces(const float (&x)[8]) { oct_from(x, hi); }
+    __device__ __forceinline__ f32x16 first(const Oct<float> &b, f32x16 c) const { return oct_product(hi, b, c); }
+    __device__ __forceinline__ f32x16 second(const Oct<float> &, f32x16 c) const { return c; }
+    __device__ __forceinline__ f32x16 first_right(const Oct<float> &a, f32x16 c) const { return oct_product(a, hi, c); }
+    __device__ __forceinline__ f32x16 second_right(const Oct<float> &, f32x16 c) const { return c; }
+};
+template <> struct Pieces<uint16_t> {
+    Oct<uint16_t> hi, lo;
+    __device__ __forceinline__ explicit Pieces(const float (&x)[8])
+    {
+        u32x4 h, l;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const uint32_t w = pack_bf16x2(x[2 * p], x[2 * p + 1]);
+            h[p] = w;
+            l[p] = pack_bf16x2(x[2 * p] - bf16_lo(w), x[2 * p + 1] - bf16_hi(w));
+        }
+        hi.v = __builtin_bit_cast(bf16x8, h);
+        lo.v = __builtin_bit_cast(bf16x8, l);
+    }
+    __device__ __forceinline__ f32x16 first(const Oct<uint16_t> &b, f32x16 c) const { return oct_product(hi, b, c); }
+    __device__ __forceinline__ f32x16 second(const Oct<uint16_t> &b, f32x16 c) const { return oct_product(lo, b, c); }
+    __device__ __forceinline__ f32x16 first_right(const Oct<uint16_t> &a, f32x16 c) const { return oct_product(a, hi, c); }
+    __device__ __forceinline__ f32x16 second_right(const Oct<uint16_t> &a, f32x16 c) const { return oct_product(a, lo, c); }
+};
+
+// Sizes of the walk for element type T and head dimension D (112 is computed as 128: missing features are zeros in LDS).
+template <typename T, int D> struct WalkShape {
+    static constexpr int kDP = (D + 31) / 32 * 32, kPanels = kDP / 32, kWalkThreads = 64 * kPanels;
+    static constexpr int kChunk = sizeof(T) == 2 ? kDecayChunkBf16 : kDecayChunkF32, kTiles = kChunk / 32;
+    static constexpr int kVec = 16 / (int)sizeof(T), kRowVecs = kDP / kVec;
+    // LDS row: 16 bytes past a multiple of 128 (64 at d = 32, bf16), so that eight rows' 16-byte pieces lie in different banks
+    static constexpr int kRowBytes = kDP * (int)sizeof(T) + 16;
+    static constexpr int kTileBytes = kChunk * kRowBytes;
+    static constexpr int kRowsPerStep = kWalkThreads / kRowVecs, kSteps = kChunk / kRowsPerStep;
+    static constexpr int kSubs = D / 16;                     // contractions over features, 16 at a time
+    static constexpr int kTokSubs = kChunk / 16;             // and over the chunk's tokens
+    static_assert(kSteps * kRowsPerStep == kChunk && D % 16 == 0, "whole rows");
+};
+
+// Eight features of a token row in LDS.
+__device__ __forceinline__ void row_operand(const unsigned char *p, Oct<uint16_t> &o)
+{
+    o.v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p));
+}
+__device__ __forceinline__ void row_operand(const unsigned char *p, Oct<float> &o)
+{
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        o.v[e] = a[e];
+        o.v[4 + e] = b[e];
+    }
+}
+
+// One feature of eight consecutive tokens: tokens tok0 + 8 h .. of a tile, features f0 .. f0 + 31 over the lanes' 32 rows, in their
+// order or in that of decay_row (ROWS).
+template <typename W, bool ROWS> __device__ __forceinline__ void token_operand(const unsigned char *tile, int tok0, int f0, int lane, Oct<uint16_t> &o)
+{
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    typedef s16x4 __attribute__((address_space(3))) * lds_s16x4_ptr;
+    // transposing read: within 16 lanes, lane i names token i / 4, features 4 (i % 4) .. + 3 and receives feature i of the four tokens
+    const int i = lane & 15, fb = (lane >> 4) & 1, g = lane >> 5;
+    const int quad = ROWS ? ((i & 1) << 1) | ((i & 2) >> 1) : i & 3;
+    const unsigned char *p = tile + (tok0 + 8 * g + (i >> 2)) * W::kRowBytes + (f0 + 16 * fb + 4 * quad) * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p + 4 * W::kRowBytes));
+    const s16x8 both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    o.v = __builtin_bit_cast(bf16x8, both);
+}
+template <typename W, bool ROWS> __device__ __forceinline__ void token_operand(const unsigned char *tile, int tok0, int f0, int lane, Oct<float> &o)
+{
+    const int m = lane & 31, g = lane >> 5;
+    const unsigned char *p = tile + (tok0 + 8 * g) * W::kRowBytes + (f0 + (ROWS ? decay_row(m) : m)) * 4;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[e] = *reinterpret_cast<const float *>(p + e * W::kRowBytes);
+}
+__device__ __forceinline__ void oct_to(const Oct<uint16_t> &o, float (&x)[8])
+{
+    const u32x4 w = __builtin_bit_cast(u32x4, o.v);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        x[2 * p] = bf16_lo(w[p]);
+        x[2 * p + 1] = bf16_hi(w[p]);
+    }
+}
+__device__ __forceinline__ void oct_to(const Oct<float> &o, float (&x)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = o.v[e];
+}
+
+// ---- powers of the decay ---------------------------------------------------------------------------------------------
+
+// l^e for e >= 0.  A log decay of minus infinity is a decay of zero: l^0 = 1, all other powers 0.
+struct DecayPower {
+    float lg;
+    __device__ __forceinline__ explicit DecayPower(float log_decay) : lg((log_decay < -1e30f ? -1e30f : log_decay) * 1.44269504088896f) {}
+    __device__ __forceinline__ float operator()(int e) const { return exp2f(lg * (float)e); }
+    // for exponents that are the same in all lanes: kept in scalar registers
+    __device__ __forceinline__ float uniform(int e) const { return scalar((*this)(e)); }
+    static __device__ __forceinline__ float scalar(float x)
+    {
+        return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+    }
+    // l^e as the sum of two floats: a segment multiplies its state by the same l^C chunk after chunk, and with a long memory (l^C just
+    // below 1) one float's rounding would add up over hundreds of chunks
+    __device__ __forceinline__ void two(int e, float log_decay, float &hi, float &lo) const
+    {
+        const double x = exp((double)(log_decay < -1e30f ? -1e30f : log_decay) * (double)e);
+        hi = scalar((float)x);
+        lo = scalar((float)(x - (double)hi));
+    }
+};
+
+// ---- a chunk's tokens: global memory -> registers -> LDS ------------------------------------------------------------
+
+// Where the rows of the walk's chunk c lie: a buffer resource over the chunk's rows and this lane's offset into it.  BACK: row r of the
+// chunk is its r-th token from behind.  The lane takes every kRowsPerStep-th row, in the order in which they lie in memory.
+template <typename T, int D, bool BACK> struct ChunkRows {
+    using W = WalkShape<T, D>;
+    const unsigned char *head;      // token 0 of the (batch, head)
+    int64_t row_bytes;
+    uint32_t off0;                  // of the lane's first row; past every row for features that do not exist
+    int row0;
+
+    __device__ __forceinline__ ChunkRows(const void *p, const TokStrides &st, int b, int h)
+        : head(static_cast<const unsigned char *>(p) + (b * st.b + h * st.h) * (int64_t)sizeof(T)), row_bytes(st.n * (int64_t)sizeof(T))
+    {
+        const int c = threadIdx.x % W::kRowVecs;
+        row0 = threadIdx.x / W::kRowVecs;
+        off0 = c * W::kVec < D ? (uint32_t)row0 * (uint32_t)row_bytes + (uint32_t)c * 16u : kNoRow;
+    }
+    // rows that are no tokens (the lead of the first chunk; all of them unless `live`) read as zeros
+    __device__ __forceinline__ void load(int64_t c, bool live, int chunks, int lead, u32x4 (&reg)[W::kSteps]) const
+    {
+        const int64_t base = BACK ? (int64_t)(chunks - 1 - c) * W::kChunk : c * W::kChunk - lead;
+        const rsrc_t r = make_rsrc(head + base * row_bytes, live ? (uint32_t)((W::kChunk - 1) * row_bytes + D * (int)sizeof(T)) : 0u);
+        const int nothing = c == 0 ? lead : 0;                         // rows in front of the first token
+        // the steps' offsets are worked out anew for every chunk: kept over the loop they are twelve registers too many
+        uint32_t off = off0;
+        asm volatile("" : "+v"(off));
+#pragma unroll
+        for (int i = 0; i < W::kSteps; ++i) {
+            constexpr int kStep = W::kRowsPerStep;
+            const bool is = BACK ? row0 < W::kChunk - nothing - i * kStep : row0 >= nothing - i * kStep;
+            reg[i] = load_stream16<false>(r, is ? off + (uint32_t)(i * kStep) * (uint32_t)row_bytes : kNoRow);
+        }
+    }
+    __device__ __forceinline__ void put(unsigned char *tile, const u32x4 (&reg)[W::kSteps]) const
+    {
+        unsigned char *p = tile + (BACK ? W::kRowsPerStep - 1 - row0 : row0) * W::kRowBytes + (threadIdx.x % W::kRowVecs) * 16;
+#pragma unroll
+        for (int i = 0; i < W::kSteps; ++i)
+            *reinterpret_cast<u32x4 *>(p + (BACK ? W::kSteps - 1 - i : i) * W::kRowsPerStep * W::kRowBytes) = reg[i];
+    }
+};
+
+// ---- the state ---------------------------------------------------------------------------------------------------------
+
+// A wave's 32 columns of S: accumulator kt, register r of lane l is key feature 32 kt + 16 (r / 8) + 8 (l / 32) + r % 8, value feature
+// 32 panel + l % 32.
+template <int D> struct StatePanel {
+    static constexpr int kKeyTiles = (D + 31) / 32;
+    f32x16 s[kKeyTiles];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+    }
+    // features that do not exist (112 is computed as 128) read as zeros and are not stored
+    __device__ __forceinline__ void load(const float *src, bool turned, int panel, int lane)
+    {
+        const int h = lane >> 5, vf = 32 * panel + (lane & 31);
+        const rsrc_t r = make_rsrc(src, D * D * 4);
+        if (turned) {
+            const uint32_t at = vf < D ? (uint32_t)(vf * D + 8 * h) * 4u : kNoRow;
+#pragma unroll
+            for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {                            // 16 features of a row and half: two times four for this lane half
+                    const int kf = 32 * kt + 16 * (q >> 1) + 4 * (q & 1);
+                    const f32x4 x = kf < D ? load_cached16(r, at + (uint32_t)kf * 4u) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[kt][4 * q + e] = x[e];
+                }
+        } else {
+            const uint32_t at = vf < D ? (uint32_t)(8 * h * D + vf) * 4u : kNoRow;
+#pragma unroll
+            for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const int kf = 32 * kt + 16 * (q >> 3) + (q & 7);
+                    s[kt][q] = kf < D ? __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at + (uint32_t)(kf * D) * 4u, 0, 0)) : 0.f;
+                }
+        }
+    }
+    __device__ __forceinline__ void store(float *dst, int panel, int lane) const
+    {
+        const int h = lane >> 5, vf = 32 * panel + (lane & 31);
+        const rsrc_t r = make_rsrc(dst, D * D * 4);
+        const uint32_t at = vf < D ? (uint32_t)(8 * h * D + vf) * 4u : kNoRow;
+#pragma unroll
+        for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const int kf = 32 * kt + 16 * (q >> 3) + (q & 7);
+                if (kf < D) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s[kt][q]), r, at + (uint32_t)(kf * D) * 4u, 0, 0);
+            }
+    }
+    __device__ __forceinline__ void scale(float hi, float lo)
+    {
+#pragma unroll
+        for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] = __builtin_fmaf(s[kt][r], hi, s[kt][r] * lo);
+    }
+    __device__ __forceinline__ void eight(int sub, float (&x)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[sub / 2][8 * (sub % 2) + e];
+    }
+};
+
+// A row's weight in the new state, by lane half: l^{C-1-j} = [l^{C-8-16 sub-8 h}] l^{7-e} for j = 16 sub + 8 h + e.
+template <int SUBS> struct UpdateWeights {
+    float base[SUBS], fine[8];
+    __device__ __forceinline__ UpdateWeights(const DecayPower &pw, int chunk, int back, float factor, int lane)
+    {
+        const int h = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) base[s] = factor * pw(chunk - 8 - 16 * s - 8 * h + back);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fine[e] = pw.uniform(7 - e);
+    }
+};
+
+// S += sum over one sub-chunk of 16 tokens, weighted.  `values` is the wave's 32 value features of these tokens.
+template <typename T, int D>
+__device__ __forceinline__ void state_update(StatePanel<D> &S, const unsigned char *tileK, const Oct<T> &values, const UpdateWeights<WalkShape<T, D>::kTokSubs> &w,
+                                             int sub, int lane)
+{
+    using W = WalkShape<T, D>;
+    float x[8];
+    oct_to(values, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = x[e] * w.fine[e] * w.base[sub];
+    const Pieces<T> v(x);
+#pragma unroll
+    for (int kt = 0; kt < StatePanel<D>::kKeyTiles; ++kt) {
+        Oct<T> k;
+        token_operand<W, true>(tileK, 16 * sub, 32 * kt, lane, k);
+        S.s[kt] = v.first_right(k, S.s[kt]);
+        S.s[kt] = v.second_right(k, S.s[kt]);
+    }
+}
+
+// ---- kernels -----------------------------------------------------------------------------------------------------------
+
+// Which segment of which head a workgroup walks.
+struct WalkTask {
+    int problem, segment, bh;
+    bool any;
+    __device__ __forceinline__ WalkTask(int tasks, int BH, int segments, int together)
+    {
+        const int task = decay_task((int)blockIdx.x, together);
+        any = task < tasks;
+        bh = task % BH;
+        segment = task / BH % segments;
+        problem = task / BH / segments;
+    }
+};
+
+__device__ __forceinline__ int walk_length(const WalkArgs &a, int b)
+{
+    if (!a.lengths) return a.N;
+    const int n = a.lengths[b];
+    return n < 0 ? 0 : n > a.N ? a.N : n;
+}
+
+// What each segment but the last adds to the state, starting from zero: into slot segment + 1 of its head.
+template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_sum(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
+{
+    using W = WalkShape<T, D>;
+    unsigned char *tileK = lds, *tileV = lds + W::kTileBytes;
+    const int b = task.bh / a.H, h = task.bh % a.H, lane = threadIdx.x & 63, panel = threadIdx.x >> 6;
+    const DecayWalk walk(walk_length(a, b), W::kChunk);
+    const int c0 = task.segment * a.per_segment, c1 = c0 + a.per_segment;
+    if (c1 >= walk.chunks) return;                                   // the last segment of this sequence, or one behind it
+    const float g = a.log_decay[h];
+    const DecayPower pw(g);
+    const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
+    float all_hi, all_lo;
+    pw.two(W::kChunk, g, all_hi, all_lo);
+    const ChunkRows<T, D, BACK> rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
+    u32x4 nk[W::kSteps], nv[W::kSteps];
+    rk.load(c0, true, walk.chunks, walk.lead, nk);
+    rv.load(c0, true, walk.chunks, walk.lead, nv);
+    StatePanel<D> S;
+    S.clear();
+    for (int c = c0; c < c1; ++c) {
+        lds_barrier();
+        rk.put(tileK, nk);
+        rv.put(tileV, nv);
+        lds_barrier();
+        rk.load(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
+        rv.load(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
+        S.scale(all_hi, all_lo);
+#pragma unroll
+        for (int sub = 0; sub < W::kTokSubs; ++sub) {
+            Oct<T> v;
+            token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
+            state_update<T, D>(S, tileK, v, uw, sub, lane);
+        }
+    }
+    S.store(p.slots + ((int64_t)task.bh * a.segments + task.segment + 1) * D * D, panel, lane);
+}
+template <typename T, int D> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads)) void decay_sums(WalkArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[2 * WalkShape<T, D>::kTileBytes];
+    const int BH = a.B * a.H;
+    const WalkTask task(a.problems * BH * (a.segments - 1), BH, a.segments - 1, a.together);
+    if (!task.any) return;
+    const WalkProblem &p = a.p[task.problem];
+    if (p.back) segment_sum<T, D, true>(a, p, task, lds);
+    else segment_sum<T, D, false>(a, p, task, lds);
+}
+
+// Slot s of each head: from what segment s - 1 adds to the state before segment s, over all segments.  A thread per four elements.
+template <typename T, int D> __global__ __launch_bounds__(256) void decay_scan(WalkArgs a)
+{
+    using W = WalkShape<T, D>;
+    constexpr int kQuads = D * D / 4, kAhead = 8;
+    const int BH = a.B * a.H, blocks = (kQuads + 255) / 256;
+    const int i = (int)(blockIdx.x % blocks) * 256 + (int)threadIdx.x, bh = (int)(blockIdx.x / blocks) % BH;
+    if (i >= kQuads) return;
+    const WalkProblem &p = a.p[blockIdx.x / blocks / BH];
+    const int b = bh / a.H, h = bh % a.H;
+    const DecayWalk walk(walk_length(a, b), W::kChunk);
+    const int last = (walk.chunks - 1) / a.per_segment;             // last segment with chunks
+    if (walk.chunks == 0) return;
+    const DecayPower pw(a.log_decay[h]);
+    f32x4 *slot = reinterpret_cast<f32x4 *>(p.slots) + (int64_t)bh * a.segments * kQuads + i;
+    f32x4 S = {0.f, 0.f, 0.f, 0.f};
+    if (p.s_begin) {
+        S = reinterpret_cast<const f32x4 *>(p.s_begin)[(int64_t)bh * kQuads + i];
+        slot[0] = S;
+    }
+    const float whole = pw(a.per_segment * W::kChunk), first = pw(a.per_segment * W::kChunk - walk.lead);
+    for (int s0 = 1; s0 <= last; s0 += kAhead) {
+        f32x4 u[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (s0 + j <= last) u[j] = slot[(int64_t)(s0 + j) * kQuads];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (s0 + j <= last) {
+                const float f = s0 + j == 1 ? first : whole;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S[e] = __builtin_fmaf(S[e], f, u[j][e]);
+                slot[(int64_t)(s0 + j) * kQuads] = S;
+            }
+    }
+}
+
+// Stores 16 features of a row tile: accumulators r0 .. r0 + 7 of lane l are value features 32 panel + 2 r0 + 8 (.. / 4) + 4 h + .. of token l % 32.
+__device__ __forceinline__ void store_features(rsrc_t r, uint32_t off, const f32x16 &acc, int half)
+{
+    uint32_t a0 = pack_bf16x2(acc[8 * half], acc[8 * half + 1]), a1 = pack_bf16x2(acc[8 * half + 2], acc[8 * half + 3]);
+    uint32_t b0 = pack_bf16x2(acc[8 * half + 4], acc[8 * half + 5]), b1 = pack_bf16x2(acc[8 * half + 6], acc[8 * half + 7]);
+    // lane half 0 gives its features 8..11 for the other half's 4..7: each lane then holds eight in a row
+    const auto x = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), y = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+    const u32x4 w = {x[0], y[0], x[1], y[1]};
+    store_stream16<false>(r, off, w);
+}
+
+template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
+{
+    using W = WalkShape<T, D>;
+    unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes;
+    float *table = reinterpret_cast<float *>(lds + 3 * W::kTileBytes), *from_state = table + 96;
+    const int b = task.bh / a.H, h = task.bh % a.H, lane = threadIdx.x & 63, panel = threadIdx.x >> 6;
+    const int half = lane >> 5, col = lane & 31;
+    const DecayWalk walk(walk_length(a, b), W::kChunk);
+    const int c0 = task.segment * a.per_segment;
+    int c1 = c0 + a.per_segment;
+    const bool last = c1 >= walk.chunks;
+    if (c1 > walk.chunks) c1 = walk.chunks;
+    if (c0 >= c1 && task.segment > 0) return;
+    const float *begin = a.segments > 1 && walk.chunks > 0 && (task.segment > 0 || p.s_begin) ? p.slots + ((int64_t)task.bh * a.segments + task.segment) * D * D
+                         : p.s_begin                                                          ? p.s_begin + (int64_t)task.bh * D * D
+                                                                                              : nullptr;
+    StatePanel<D> S;
+    if (begin) S.load(begin, p.turned, panel, lane);
+    else S.clear();
+    const bool keep = last && p.s_end;                               // this workgroup's state is the sequence's last
+
+    const float g = a.log_decay[h];
+    const DecayPower pw(g);
+    const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
+    // the first chunk of a sequence holds `lead` tokens fewer
+    float all_hi, all_lo, first_hi, first_lo;
+    pw.two(W::kChunk, g, all_hi, all_lo);
+    pw.two(W::kChunk - walk.lead, g, first_hi, first_lo);
+    // a row's weight on what comes out of the state, whole chunks and the first one
+    for (int i = threadIdx.x; i < W::kChunk; i += W::kWalkThreads) {
+        const int e = i + 1 - (int)BACK;
+        from_state[i] = p.weight_state * pw(e);
+        from_state[64 + i] = p.weight_state * pw(e < walk.lead ? 0 : e - walk.lead);
+    }
+    // weights of the scores by distance: table[63 - distance], zeros where the row lies behind.  Row 32 it + col and row 32 jt + 16 s + 8 half
+    // + e are 32 (it - jt) + col - 16 s - 8 half - e apart.  In LDS: sixteen registers that every chunk needs for a moment only.
+    for (int i = threadIdx.x; i < 96; i += W::kWalkThreads) table[i] = i < 64 ? p.weight_chunk * pw(63 - i) : 0.f;
+    const float *distance = table + 31 - col + 8 * half;
+
+    const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
+    unsigned char *out = static_cast<unsigned char *>(p.o) + (b * p.so.b + h * p.so.h) * (int64_t)sizeof(T);
+    const int64_t out_row = p.so.n * (int64_t)sizeof(T);
+    u32x4 nq[W::kSteps], nk[W::kSteps], nv[W::kSteps];
+    rq.load(c0, c0 < c1, walk.chunks, walk.lead, nq);
+    rk.load(c0, c0 < c1, walk.chunks, walk.lead, nk);
+    rv.load(c0, c0 < c1, walk.chunks, walk.lead, nv);
+
+    for (int c = c0; c < c1; ++c) {
+        lds_barrier();
+        rq.put(tileQ, nq);
+        rk.put(tileK, nk);
+        rv.put(tileV, nv);
+        lds_barrier();
+        const bool more = c + 1 < c1;
+        // scores, weighted, as operands: of rows 0..31 with themselves, of rows 32..63 with rows 0..31 and with themselves
+        Oct<T> own[W::kTiles][2], across[2];
+        {
+            f32x16 P00, P01, P11;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) P00[r] = P01[r] = P11[r] = 0.f;
+#pragma unroll
+            for (int sub = 0; sub < W::kSubs; ++sub) {
+                const int at = (16 * sub + 8 * half) * (int)sizeof(T);
+                Oct<T> q[W::kTiles], k[W::kTiles];
+#pragma unroll
+                for (int t = 0; t < W::kTiles; ++t) {
+                    row_operand(tileQ + (32 * t + col) * W::kRowBytes + at, q[t]);
+                    row_operand(tileK + (32 * t + decay_row(col)) * W::kRowBytes + at, k[t]);
+                }
+                P00 = oct_product(k[0], q[0], P00);
+                if constexpr (W::kTiles == 2) {
+                    P01 = oct_product(k[0], q[1], P01);
+                    P11 = oct_product(k[1], q[1], P11);
+                }
+                if (sub % 2 == 1 || sub == W::kSubs - 1) __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float x[8], near[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) near[e] = distance[32 + 16 * s + e];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = P00[8 * s + e] * near[e];
+                oct_from(x, own[0][s]);
+                if constexpr (W::kTiles == 2) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = P11[8 * s + e] * near[e];
+                    oct_from(x, own[1][s]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = P01[8 * s + e] * distance[16 * s + e];
+                    oct_from(x, across[s]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // the next chunk's tokens are requested where registers come free
+        rk.load(c + 1, more, walk.chunks, walk.lead, nk);
+        rv.load(c + 1, more, walk.chunks, walk.lead, nv);
+        // acc[it]: output of row tile it, value features x tokens, from the state
+        f32x16 acc[W::kTiles];
+#pragma unroll
+        for (int it = 0; it < W::kTiles; ++it)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[it][r] = 0.f;
+#pragma unroll
+        for (int sub = 0; sub < W::kSubs; ++sub) {
+            Oct<T> q[W::kTiles];
+#pragma unroll
+            for (int t = 0; t < W::kTiles; ++t) row_operand(tileQ + (32 * t + col) * W::kRowBytes + (16 * sub + 8 * half) * (int)sizeof(T), q[t]);
+            float x[8];
+            S.eight(sub, x);
+            const Pieces<T> s(x);
+#pragma unroll
+            for (int t = 0; t < W::kTiles; ++t) acc[t] = s.first(q[t], acc[t]);
+#pragma unroll
+            for (int t = 0; t < W::kTiles; ++t) acc[t] = s.second(q[t], acc[t]);
+            if (sub % 2 == 1 || sub == W::kSubs - 1) __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int it = 0; it < W::kTiles; ++it) {
+            const float weight = from_state[(c == 0 ? 64 : 0) + 32 * it + col];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[it][r] *= weight;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // from the chunk itself, and the chunk into the state
+        S.scale(c == 0 ? first_hi : all_hi, c == 0 ? first_lo : all_lo);
+#pragma unroll
+        for (int sub = 0; sub < W::kTokSubs; ++sub) {
+            Oct<T> v;
+            if (sub == W::kTokSubs - 1) rq.load(c + 1, more, walk.chunks, walk.lead, nq);
+            token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
+            if (sub < 2) acc[0] = oct_product(v, own[0][sub], acc[0]);
+            if constexpr (W::kTiles == 2) acc[1] = oct_product(v, sub < 2 ? across[sub] : own[1][sub - 2], acc[1]);
+            state_update<T, D>(S, tileK, v, uw, sub, lane);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // the chunk's output rows, where they are tokens
+        const int64_t base = BACK ? (int64_t)(walk.chunks - 1 - c) * W::kChunk : (int64_t)c * W::kChunk - walk.lead;
+        const rsrc_t ro = make_rsrc(out + base * out_row, (uint32_t)((W::kChunk - 1) * out_row + D * (int)sizeof(T)));
+        const int nothing = c == 0 ? walk.lead : 0;
+#pragma unroll
+        for (int it = 0; it < W::kTiles; ++it) {
+            const int row = 32 * it + col;
+            const uint32_t off = row >= nothing ? (uint32_t)(BACK ? W::kChunk - 1 - row : row) * (uint32_t)out_row : kNoRow;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int f = 32 * panel + 16 * x + 8 * half;
+                    store_features(ro, f < D ? off + (uint32_t)f * 2u : kNoRow, acc[it], x);
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int f = 32 * panel + 8 * x + 4 * half;
+                    const f32x4 w = {acc[it][4 * x], acc[it][4 * x + 1], acc[it][4 * x + 2], acc[it][4 * x + 3]};
+                    store_stream16<false>(ro, f < D ? off + (uint32_t)f * 4u : kNoRow, __builtin_bit_cast(u32x4, w));
+                }
+            }
+        }
+    }
+    if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, lane);
+}
+template <typename T, int D> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[3 * WalkShape<T, D>::kTileBytes + kDecayTableBytes];
+    const int BH = a.B * a.H;
+    const WalkTask task(a.problems * BH * a.segments, BH, a.segments, a.together);
+    if (!task.any) return;
+    const WalkProblem &p = a.p[task.problem];
+    if (p.back) walk_segment<T, D, true>(a, p, task, lds);
+    else walk_segment<T, D, false>(a, p, task, lds);
+}
+
+}  // namespace sv

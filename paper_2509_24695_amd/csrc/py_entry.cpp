@@ -10,6 +10,7 @@
 #include <tuple>
 #include <utility>
 
+#include "../../include/sv_decay.h"
 #include "../../include/sv_linattn.h"
 #include "../../include/sv_tconv.h"
 
@@ -133,7 +134,7 @@ struct Flag {                          // int(x)
     }
     int32_t c() { return v; }
 };
-struct Eps {                           // float(x)
+struct Eps {                           // float(x): eps, scales
     float v;
     bool get(PyObject *const *args, int i)
     {
@@ -231,6 +232,9 @@ ENTRY(sv_linattn_apply_rope3d, P, Desc, Rope, Int, Int, P, P, Eps, P, Stream)
 ENTRY(sv_block_linattn_step_rope3d, P, P, P, Desc, Rope, P, P, Eps, P, P, Bytes, Stream)
 ENTRY(sv_block_linattn_lookahead_rope3d, P, P, P, Desc, Rope, P, P, Eps, P, P, Bytes, Stream)
 ENTRY(sv_tconv_block_step, P, P, P, P, P, Int, Int, Int, Int, Int, Stream)
+ENTRY(sv_decay_linattn, P, P, P, Desc, P, P, Eps, P, P, P, Desc, P, Bytes, Stream)
+ENTRY(sv_decay_linattn_token, P, P, P, Desc, P, P, Int, Eps, P, P, P, Desc, Stream)
+ENTRY(sv_decay_linattn_backward, P, P, P, Desc, P, Desc, P, P, Eps, P, P, P, P, P, P, P, Bytes, Stream)
 
 // attach(handle): the entry points of the loaded library with this dlopen handle.
 PyObject *attach(PyObject *, PyObject *handle)
@@ -250,7 +254,8 @@ PyObject *attach(PyObject *, PyObject *handle)
     X(sv_linattn_state) X(sv_linattn_apply) X(sv_block_linattn_step) X(sv_block_linattn_lookahead)                     \
     X(sv_block_linattn_step_static) X(sv_linattn_state_rope) X(sv_linattn_apply_rope) X(sv_block_linattn_step_rope)    \
     X(sv_block_linattn_lookahead_rope) X(sv_linattn_state_rope3d) X(sv_linattn_apply_rope3d)                           \
-    X(sv_block_linattn_step_rope3d) X(sv_block_linattn_lookahead_rope3d) X(sv_tconv_block_step)
+    X(sv_block_linattn_step_rope3d) X(sv_block_linattn_lookahead_rope3d) X(sv_tconv_block_step)        \
+    X(sv_decay_linattn) X(sv_decay_linattn_token) X(sv_decay_linattn_backward)
     EACH(ATTACH)
     Py_RETURN_NONE;
 }

@@ -18,6 +18,7 @@
 #include "coop128.hpp"
 #include "coop_state.hpp"
 #include "common.hpp"
+#include "desc_checks.hpp"
 #include "f32_mfma.hpp"
 #include "generic_kernels.hpp"
 #include "layout_rules.hpp"
@@ -57,14 +58,6 @@ constexpr uint32_t kSpinLimit = 1u << 24;      // polls of ~100 ns: far beyond a
 std::atomic<uint32_t> g_spin_limit{kSpinLimit};  // sv_linattn_set_wait_limit
 uint32_t spin_limit() { return g_spin_limit.load(std::memory_order_relaxed); }
 std::atomic<int> g_assumed_dies{kDies};          // sv_measure_assume_dies
-
-struct Shape {
-    int B, H, N, d, BH;
-    TokStrides st;
-    bool bf16;
-    int elem_bytes;
-    bool host_epochs_only = false;   // the workspace is the library's own static array (see next_epoch)
-};
 
 struct Device {
     int num_cu = 0;
@@ -279,19 +272,6 @@ __global__ void workspace_header_init(unsigned long long *flags, size_t n_flags,
     }
 }
 
-bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 112 || d == 128; }
-
-// Calls f(std::integral_constant<int, D>) for the supported head dimension d.
-template <typename F> void with_head_dim(int d, F &&f)
-{
-    switch (d) {
-    case 32: f(std::integral_constant<int, 32>{}); break;
-    case 64: f(std::integral_constant<int, 64>{}); break;
-    case 112: f(std::integral_constant<int, 112>{}); break;
-    default: f(std::integral_constant<int, 128>{}); break;
-    }
-}
-
 // Per-device facts, queried once (no device memory is touched).
 const Device &device_info()
 {
@@ -354,40 +334,6 @@ unsigned long long next_epoch(bool host_epochs_only = false)
     // odd, never zero, never repeated (2^62 calls apart); the top bit is the kernels' kHostEpochsOnly
     const unsigned long long e = ((ctr.fetch_add(1, std::memory_order_relaxed) << 1) | 1ull) & ~kHostEpochsOnly;
     return host_epochs_only ? e | kHostEpochsOnly : e;
-}
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-sv_status check_desc(const sv_tensor_desc *t, Shape *s)
-{
-    if (!t) return SV_ERR_NULL;
-    if (t->dtype != SV_BF16 && t->dtype != SV_F32) return SV_ERR_UNSUPPORTED;
-    if (!head_dim_ok(t->d)) return SV_ERR_UNSUPPORTED;
-    if (t->B <= 0 || t->H <= 0 || t->N <= 0) return SV_ERR_SHAPE;
-    if ((int64_t)t->B * t->H > 65535) return SV_ERR_SHAPE;           // grid.y limit
-    if (t->stride_n < t->d || t->stride_b < 0 || t->stride_h < 0) return SV_ERR_SHAPE;
-    if (t->B > 1 && t->stride_b == 0) return SV_ERR_SHAPE;
-    if (t->H > 1 && t->stride_h == 0) return SV_ERR_SHAPE;
-    s->B = t->B; s->H = t->H; s->N = t->N; s->d = t->d; s->BH = t->B * t->H;
-    s->st = TokStrides{t->stride_b, t->stride_h, t->stride_n};
-    s->bf16 = t->dtype == SV_BF16;
-    s->elem_bytes = s->bf16 ? 2 : 4;
-    const int64_t per16 = 16 / s->elem_bytes;
-    if (t->stride_n % per16 || t->stride_b % per16 || t->stride_h % per16) return SV_ERR_ALIGN;
-    // No two (b, h, n) rows may share memory (O rows would overwrite each other): taken in order of
-    // ascending stride, every axis with more than one index must step over all that the axes below it span.
-    struct Axis { int64_t stride, extent; } ax[3] = {{t->stride_b, t->B}, {t->stride_h, t->H}, {t->stride_n, t->N}};
-    for (int i = 0; i < 3; ++i)
-        for (int j = i + 1; j < 3; ++j)
-            if (ax[j].stride < ax[i].stride) { const Axis x = ax[i]; ax[i] = ax[j]; ax[j] = x; }
-    int64_t span = t->d;                             // elements covered by the axes handled so far
-    for (const Axis &a : ax) {
-        if (a.extent <= 1) continue;
-        if (a.stride < span) return SV_ERR_SHAPE;
-        if (a.stride > INT64_MAX / a.extent) return SV_ERR_SHAPE;
-        span = a.stride * a.extent;
-    }
-    return SV_OK;
 }
 
 // Do 32-bit offsets reach a head's tokens and the rotation table's rows?
