@@ -1,7 +1,7 @@
 """MI355X (gfx950) ReLU linear attention for long video token sequences.
 
 Thin Python binding over libsvlinattn.so (hand-written HIP kernels behind a C
-ABI, declared in include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h and include/sv_measure.h).  PyTorch is used by callers for device
+ABI, declared in the headers of include/).  PyTorch is used by callers for device
 memory and streams only; every step of the computation runs in the library.
 """
 from .binding import (  # noqa: F401
@@ -14,5 +14,5 @@ from .binding import (  # noqa: F401
     sv_linattn_workspace_status, sv_linattn_workspace_status_offset, sv_linattn_set_wait_limit, sv_block_linattn_step_static, sv_measure_apply_variant, sv_measure_assume_dies,
     sv_mfma_stream, sv_measure_tconv_variant,
     sv_decay_linattn_workspace_bytes, sv_decay_linattn_backward_workspace_bytes, sv_decay_linattn, sv_decay_linattn_token,
-    sv_decay_linattn_backward,
+    sv_decay_linattn_backward, sv_rope3d_rotate, sv_layernorm, sv_layernorm_backward_workspace_bytes, sv_layernorm_backward,
 )

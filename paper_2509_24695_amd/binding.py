@@ -3,7 +3,7 @@ the module _sventry (csrc/py_entry.cpp), which takes 1.2 us per call for it wher
 for one interpreter; another one that imports the package makes these calls through ctypes as well.
 
 The functions carry the names and argument order of the C ABI
-(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
+(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_rope.h, include/sv_norm.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
 device addresses); nothing here computes, and there is no fallback: if the
 shared library is missing, loading raises.
 """
@@ -28,7 +28,8 @@ EXPORTS = (
     "sv_block_linattn_step_static", "sv_measure_apply_variant",
     "sv_measure_assume_dies", "sv_mfma_stream", "sv_measure_tconv_variant",
     "sv_decay_linattn_workspace_bytes", "sv_decay_linattn_backward_workspace_bytes", "sv_decay_linattn",
-    "sv_decay_linattn_token", "sv_decay_linattn_backward",
+    "sv_decay_linattn_token", "sv_decay_linattn_backward", "sv_rope3d_rotate", "sv_layernorm",
+    "sv_layernorm_backward_workspace_bytes", "sv_layernorm_backward",
 )
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -122,7 +123,13 @@ def load_library():
     lib.sv_decay_linattn.argtypes = [vp, vp, vp, dp, vp, vp, fl, vp, vp, vp, dp, vp, sz, vp]
     lib.sv_decay_linattn_token.argtypes = [vp, vp, vp, dp, vp, vp, i32, fl, vp, vp, vp, dp, vp]
     lib.sv_decay_linattn_backward.argtypes = [vp, vp, vp, dp, vp, dp, vp, vp, fl, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    for f in (lib.sv_decay_linattn, lib.sv_decay_linattn_token, lib.sv_decay_linattn_backward):
+    lib.sv_rope3d_rotate.argtypes = [vp, vp, dp, rp, vp, ctypes.c_int, vp, vp, dp, vp]
+    lib.sv_layernorm.argtypes = [vp, dp, vp, vp, i32, fl, vp, dp, vp, vp, vp]
+    lib.sv_layernorm_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.sv_layernorm_backward_workspace_bytes.restype = sz
+    lib.sv_layernorm_backward.argtypes = [vp, dp, vp, dp, vp, i32, vp, vp, vp, dp, vp, vp, vp, sz, vp]
+    for f in (lib.sv_decay_linattn, lib.sv_decay_linattn_token, lib.sv_decay_linattn_backward, lib.sv_rope3d_rotate, lib.sv_layernorm,
+              lib.sv_layernorm_backward):
         f.restype = ctypes.c_int
     lib.sv_measure_apply_variant.argtypes = [i32, vp, dp, i32, i32, vp, vp, ctypes.c_float, vp, vp]
     lib.sv_measure_apply_variant.restype = ctypes.c_int
@@ -427,6 +434,31 @@ def sv_decay_linattn_backward(Q, K, V, qkv: TensorDesc, dO, o: TensorDesc, log_d
     """Gradients of sv_decay_linattn for Q, K, V and S_in (include/sv_decay.h)."""
     _check((_entry or _calls()).sv_decay_linattn_backward(Q, K, V, qkv, dO, o, log_decay, lengths, scale, S_in, dS_out, dQ, dK, dV,
                                                           dS_in, workspace, workspace_bytes, stream), "sv_decay_linattn_backward")
+
+
+def sv_rope3d_rotate(Q, K, x: TensorDesc, rope: Rope3D, positions, inverse, YQ, YK, y: TensorDesc, stream=None) -> None:
+    """Rotation of Q and, if not None, K by three-axis positions (include/sv_rope.h): positions [B][N][3] int32, or None for the tables'
+    grid; inverse turns back (the backward pass)."""
+    _check((_entry or _calls()).sv_rope3d_rotate(Q, K, x, rope, positions, inverse, YQ, YK, y, stream), "sv_rope3d_rotate")
+
+
+def sv_layernorm(X, x: TensorDesc, weight, bias, weight_heads: int, eps: float, Y, y: TensorDesc, mean, rstd, stream=None) -> None:
+    """Layer norm of the rows of a token tensor (include/sv_norm.h): weight, bias [weight_heads][d] fp32 or None, mean, rstd [B][H][N]
+    fp32 or None."""
+    _check((_entry or _calls()).sv_layernorm(X, x, weight, bias, weight_heads, eps, Y, y, mean, rstd, stream), "sv_layernorm")
+
+
+def sv_layernorm_backward_workspace_bytes(B: int, H: int, n_tokens: int, d: int) -> int:
+    return int(load_library().sv_layernorm_backward_workspace_bytes(int(B), int(H), int(n_tokens), int(d)))
+
+
+def sv_layernorm_backward(X, x: TensorDesc, dY, dy: TensorDesc, weight, weight_heads: int, mean, rstd, dX, dx: TensorDesc, dweight, dbias,
+                          workspace, workspace_bytes: int | None = None, stream=None) -> None:
+    """Gradients of sv_layernorm for X, weight and bias (include/sv_norm.h)."""
+    if workspace is None and workspace_bytes is None:
+        workspace_bytes = 0
+    _check((_entry or _calls()).sv_layernorm_backward(X, x, dY, dy, weight, weight_heads, mean, rstd, dX, dx, dweight, dbias, workspace,
+                                                      workspace_bytes, stream), "sv_layernorm_backward")
 
 
 def sv_measure_apply_variant(variant: int, Q, q: TensorDesc, tok_begin: int, tok_end: int, S, z, eps: float, O,

@@ -12,6 +12,8 @@
 
 #include "../../include/sv_decay.h"
 #include "../../include/sv_linattn.h"
+#include "../../include/sv_norm.h"
+#include "../../include/sv_rope.h"
 #include "../../include/sv_tconv.h"
 
 namespace {
@@ -235,6 +237,9 @@ ENTRY(sv_tconv_block_step, P, P, P, P, P, Int, Int, Int, Int, Int, Stream)
 ENTRY(sv_decay_linattn, P, P, P, Desc, P, P, Eps, P, P, P, Desc, P, Bytes, Stream)
 ENTRY(sv_decay_linattn_token, P, P, P, Desc, P, P, Int, Eps, P, P, P, Desc, Stream)
 ENTRY(sv_decay_linattn_backward, P, P, P, Desc, P, Desc, P, P, Eps, P, P, P, P, P, P, P, Bytes, Stream)
+ENTRY(sv_rope3d_rotate, P, P, Desc, Rope, P, Flag, P, P, Desc, Stream)
+ENTRY(sv_layernorm, P, Desc, P, P, Int, Eps, P, Desc, P, P, Stream)
+ENTRY(sv_layernorm_backward, P, Desc, P, Desc, P, Int, P, P, P, Desc, P, P, P, Bytes, Stream)
 
 // attach(handle): the entry points of the loaded library with this dlopen handle.
 PyObject *attach(PyObject *, PyObject *handle)
@@ -255,7 +260,8 @@ PyObject *attach(PyObject *, PyObject *handle)
     X(sv_block_linattn_step_static) X(sv_linattn_state_rope) X(sv_linattn_apply_rope) X(sv_block_linattn_step_rope)    \
     X(sv_block_linattn_lookahead_rope) X(sv_linattn_state_rope3d) X(sv_linattn_apply_rope3d)                           \
     X(sv_block_linattn_step_rope3d) X(sv_block_linattn_lookahead_rope3d) X(sv_tconv_block_step)        \
-    X(sv_decay_linattn) X(sv_decay_linattn_token) X(sv_decay_linattn_backward)
+    X(sv_decay_linattn) X(sv_decay_linattn_token) X(sv_decay_linattn_backward) X(sv_rope3d_rotate) X(sv_layernorm)     \
+    X(sv_layernorm_backward)
     EACH(ATTACH)
     Py_RETURN_NONE;
 }

@@ -1,0 +1,159 @@
+// C ABI of layer norm (include/sv_norm.h): argument checks and launches.
+#include "../../include/sv_norm.h"
+
+#include <math.h>
+
+#include "desc_checks.hpp"
+#include "norm.hpp"
+
+namespace {
+
+using namespace sv;
+
+constexpr int64_t kMostHeads = 1 << 24;
+
+sv_status check_rows(const sv_tensor_desc *t, Shape *s)
+{
+    const sv_status rc = check_desc(t, s, true, kMostHeads);
+    if (rc != SV_OK) return rc;
+    const int per = 16 / s->elem_bytes;
+    if (s->d <= 0 || s->d % per || s->d > kNormMostWidth) return SV_ERR_UNSUPPORTED;
+    return (int64_t)s->BH * s->N >= (int64_t)1 << 31 ? SV_ERR_SHAPE : SV_OK;
+}
+
+bool same_shape(const Shape &x, const Shape &y) { return x.B == y.B && x.H == y.H && x.N == y.N && x.d == y.d && x.bf16 == y.bf16; }
+bool same_rows(const Shape &x, const Shape &y) { return x.st.b == y.st.b && x.st.h == y.st.h && x.st.n == y.st.n; }
+
+// The rows of x's shape as groups (heads with parameters of their own, or one) of rows, walked in the order in which x lies in memory.
+void set_rows(NormArgs &g, const Shape &x, const Shape &b, const Shape &c, int groups)
+{
+    NormAxis ax[3] = {{x.N, x.st.n, b.st.n, c.st.n, 1}, {x.H, x.st.h, b.st.h, c.st.h, x.N}, {x.B, x.st.b, b.st.b, c.st.b, (int64_t)x.H * x.N}};
+    if (groups > 1) {
+        g.group_a = ax[1].a; g.group_b = ax[1].b; g.group_c = ax[1].c; g.group_stat = ax[1].stat;
+        ax[1].extent = 1;
+    }
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (ax[j].extent > 1 && (ax[i].extent == 1 || ax[j].a < ax[i].a)) { const NormAxis t = ax[i]; ax[i] = ax[j]; ax[j] = t; }
+    for (int i = 0; i < 3; ++i) g.axis[i] = ax[i];
+    g.groups = groups;
+    g.rows = (int64_t)x.BH * x.N / groups;
+    g.d = x.d;
+}
+
+sv_status launched() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
+
+// Calls f(lanes, vecs) with the constants of a form.
+template <typename F> void with_form(const NormForm &form, F &&f)
+{
+    auto vecs = [&](auto v) { f(std::integral_constant<int, 64>{}, v); };
+    switch (form.lanes) {
+    case 4: f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{}); break;
+    case 8: f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{}); break;
+    case 16: f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}); break;
+    case 32: f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{}); break;
+    case 64:
+        switch (form.vecs) {
+        case 1: vecs(std::integral_constant<int, 1>{}); break;
+        case 2: vecs(std::integral_constant<int, 2>{}); break;
+        case 3: vecs(std::integral_constant<int, 3>{}); break;
+        case 4: vecs(std::integral_constant<int, 4>{}); break;
+        case 5: vecs(std::integral_constant<int, 5>{}); break;
+        default: vecs(std::integral_constant<int, 6>{}); break;
+        }
+        break;
+    case 256: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{}); break;
+    case 512: f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{}); break;
+    default: f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{}); break;
+    }
+}
+
+size_t partial_bytes(int64_t groups, int workgroups, int d) { return (size_t)groups * workgroups * 2 * d * sizeof(float); }
+
+}  // namespace
+
+extern "C" sv_status sv_layernorm(const void *X, const sv_tensor_desc *x, const float *weight, const float *bias, int32_t weight_heads, float eps,
+                                  void *Y, const sv_tensor_desc *y, float *mean, float *rstd, void *stream)
+{
+    if (!X || !Y || (mean == nullptr) != (rstd == nullptr)) return SV_ERR_NULL;
+    Shape in, out;
+    sv_status rc = check_rows(x, &in);
+    if (rc != SV_OK) return rc;
+    rc = check_rows(y, &out);
+    if (rc != SV_OK) return rc;
+    if (!same_shape(in, out) || (weight_heads != 1 && weight_heads != in.H)) return SV_ERR_SHAPE;
+    if (!aligned16(X) || !aligned16(Y) || !aligned16(weight) || !aligned16(bias) || !aligned16(mean) || !aligned16(rstd)) return SV_ERR_ALIGN;
+    if (!isfinite(eps) || eps < 0.f) return SV_ERR_RANGE;
+    if ((Y == X && !same_rows(in, out)) || (mean && mean == rstd)) return SV_ERR_SHAPE;
+    NormArgs a{};
+    a.x = X; a.y = Y; a.weight = weight; a.bias = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
+    set_rows(a, in, out, out, weight_heads);
+    const NormForm form = norm_form(in.d * in.elem_bytes / 16);
+    a.workgroups = norm_workgroups(form, a.rows, a.groups, kNormForwardWgs);
+    const unsigned grid = (unsigned)((int64_t)a.groups * a.workgroups);
+    const auto hs = static_cast<hipStream_t>(stream);
+    with_form(form, [&](auto lanes, auto vecs) {
+        if constexpr (lanes() * vecs() <= kNormMostWidth / 8)         // bf16 rows have no more pieces
+            if (in.bf16) norm_rows<uint16_t, lanes(), vecs()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
+        if (!in.bf16) norm_rows<float, lanes(), vecs()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
+    });
+    return launched();
+}
+
+extern "C" size_t sv_layernorm_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d)
+{
+    if (B <= 0 || H <= 0 || n_tokens <= 0 || d <= 0 || d % 4 || d > kNormMostWidth || (int64_t)B * H > kMostHeads) return 0;
+    // at most this many partial sums, whatever the type and the number of parameter rows
+    const int64_t most = H > kNormBackwardWgs ? H : kNormBackwardWgs;
+    return partial_bytes(1, (int)most, d);
+}
+
+extern "C" sv_status sv_layernorm_backward(const void *X, const sv_tensor_desc *x, const void *dY, const sv_tensor_desc *dy, const float *weight,
+                                           int32_t weight_heads, const float *mean, const float *rstd, void *dX, const sv_tensor_desc *dx,
+                                           float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const bool params = dweight || dbias;
+    if (!X || !dY || !dX || !mean || !rstd || (params && !workspace)) return SV_ERR_NULL;
+    Shape in, grad, out;
+    sv_status rc = check_rows(x, &in);
+    if (rc != SV_OK) return rc;
+    rc = check_rows(dy, &grad);
+    if (rc != SV_OK) return rc;
+    rc = check_rows(dx, &out);
+    if (rc != SV_OK) return rc;
+    if (!same_shape(in, grad) || !same_shape(in, out) || (weight_heads != 1 && weight_heads != in.H)) return SV_ERR_SHAPE;
+    for (const void *p : {X, dY, static_cast<const void *>(dX), static_cast<const void *>(weight), static_cast<const void *>(mean), static_cast<const void *>(rstd),
+                          static_cast<const void *>(dweight), static_cast<const void *>(dbias), static_cast<const void *>(workspace)})
+        if (!aligned16(p)) return SV_ERR_ALIGN;
+    if (dX == X || (dX == dY && !same_rows(grad, out)) || (dweight && dweight == dbias) || (params && (dweight == weight || dbias == weight) && weight)) return SV_ERR_SHAPE;
+    NormArgs a{};
+    a.x = X; a.dy = dY; a.y = dX; a.weight = weight;
+    a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
+    a.dw = dweight; a.db = dbias;
+    set_rows(a, in, grad, out, weight_heads);
+    const NormForm form = norm_form(in.d * in.elem_bytes / 16);
+    a.workgroups = norm_workgroups(form, a.rows, a.groups, kNormBackwardWgs);
+    if (params && workspace_bytes < partial_bytes(a.groups, a.workgroups, in.d)) return SV_ERR_WORKSPACE;
+    a.partial = static_cast<float *>(workspace);
+    const unsigned grid = (unsigned)((int64_t)a.groups * a.workgroups);
+    const auto hs = static_cast<hipStream_t>(stream);
+    with_form(form, [&](auto lanes, auto vecs) {
+        auto go = [&](auto t, auto p) {
+            norm_rows_backward<decltype(t), lanes(), vecs(), p()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
+        };
+        auto pick = [&](auto t) {
+            if (params) go(t, std::true_type{});
+            else go(t, std::false_type{});
+        };
+        if constexpr (lanes() * vecs() <= kNormMostWidth / 8)
+            if (in.bf16) pick(uint16_t{});
+        if (!in.bf16) pick(float{});
+    });
+    if (launched() != SV_OK) return SV_ERR_LAUNCH;
+    if (params) {
+        const int64_t tiles = (in.d / 4 * 2 + 15) / 16;
+        norm_fold<<<(unsigned)(a.groups * tiles), 256, 0, hs>>>(a);
+        return launched();
+    }
+    return SV_OK;
+}

@@ -4,6 +4,7 @@
 
 #include <climits>
 #include <cstdio>
+#include <initializer_list>
 #include <vector>
 
 using namespace sv;
