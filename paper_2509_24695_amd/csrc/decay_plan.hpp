@@ -16,11 +16,16 @@ struct DecayPlan {
     int chunks, segments, per_segment;
 };
 
-inline DecayPlan decay_plan(int64_t BH, int n_tokens, int chunk)
+// As many workgroups as run at once, in all `walks` of a launch together: the walk is bound by what a wave waits for (its own products, LDS,
+// the other waves), so a second round or fewer waves cost more than the partial states of shorter segments (32 heads, 4 680 tokens, us with
+// half as many / these / one and a half times: d = 64 41.3 / 37.9 / 45.1, d = 128 74.8 / 71.1 / 81.8; d = 32, 128 heads of 4 096: 56.4 / 45.2 /
+// 49.8; backward, all three walks with the forward call's number each: d = 64 72.7 against 64).  No segment is a single chunk.
+inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walks)
 {
     DecayPlan p;
     p.chunks = (int)(((int64_t)n_tokens + chunk - 1) / chunk);
-    const int64_t wanted = 512 / BH < 1 ? 1 : 512 / BH;
+    const int64_t workgroups = (d <= 64 ? 1024 : 512) / walks;
+    const int64_t wanted = workgroups / BH < 1 ? 1 : workgroups / BH;
     int64_t segments = wanted > kMaxDecaySegments ? kMaxDecaySegments : wanted;
     if (segments > (p.chunks + 1) / 2) segments = (p.chunks + 1) / 2;
     if (segments < 1) segments = 1;

@@ -138,6 +138,9 @@ template <typename T, int D> struct WalkShape {
     static constexpr int kRowsPerStep = kWalkThreads / kRowVecs, kSteps = kChunk / kRowsPerStep;
     static constexpr int kSubs = D / 16;                     // contractions over features, 16 at a time
     static constexpr int kTokSubs = kChunk / 16;             // and over the chunk's tokens
+    static constexpr int kScoreTiles = kTiles == 2 ? 3 : 1;
+    static constexpr bool kShared = sizeof(T) == 2 && kPanels == 4;
+    static constexpr int kOwnTiles = kShared ? 1 : kScoreTiles, kScoreBytes = kShared ? kScoreTiles * 2 * 64 * 8 * (int)sizeof(T) : 0;
     static_assert(kSteps * kRowsPerStep == kChunk && D % 16 == 0, "whole rows");
 };
 
@@ -194,6 +197,19 @@ __device__ __forceinline__ void oct_to(const Oct<float> &o, float (&x)[8])
     for (int e = 0; e < 8; ++e) x[e] = o.v[e];
 }
 
+// The operand is worked out here: nothing that reads memory later is moved in front of it.  (A scheduling barrier does not do: the compiler
+// puts arithmetic next to its use before it schedules, and scores then live on in fp32 through the next product.)
+__device__ __forceinline__ void settle(Oct<uint16_t> &o)
+{
+    u32x4 w = __builtin_bit_cast(u32x4, o.v);
+    asm volatile("" : "+v"(w)::"memory");
+    o.v = __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ void settle(Oct<float> &o)
+{
+    asm volatile("" : "+v"(o.v[0]), "+v"(o.v[1]), "+v"(o.v[2]), "+v"(o.v[3]), "+v"(o.v[4]), "+v"(o.v[5]), "+v"(o.v[6]), "+v"(o.v[7])::"memory");
+}
+
 // ---- powers of the decay ---------------------------------------------------------------------------------------------
 
 // l^e for e >= 0.  A log decay of minus infinity is a decay of zero: l^0 = 1, all other powers 0.
@@ -207,14 +223,20 @@ struct DecayPower {
     {
         return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
     }
-    // l^e as the sum of two floats: a segment multiplies its state by the same l^C chunk after chunk, and with a long memory (l^C just
-    // below 1) one float's rounding would add up over hundreds of chunks
-    __device__ __forceinline__ void two(int e, float log_decay, float &hi, float &lo) const
+};
+
+// l^C, by which a segment multiplies its state chunk after chunk.  With a long memory, l^C just below 1, the rounding of one float would add
+// up over hundreds of chunks: every eighth factor makes up for the other seven's.
+struct ChunkDecay {
+    float usual, eighth;
+    __device__ __forceinline__ ChunkDecay(int chunk, float log_decay)
     {
-        const double x = exp((double)(log_decay < -1e30f ? -1e30f : log_decay) * (double)e);
-        hi = scalar((float)x);
-        lo = scalar((float)(x - (double)hi));
+        const double x = exp((double)(log_decay < -1e30f ? -1e30f : log_decay) * (double)chunk);
+        const float f = (float)x;
+        usual = DecayPower::scalar(f);
+        eighth = DecayPower::scalar((float)(x + 7.0 * (x - (double)f)));
     }
+    __device__ __forceinline__ float operator()(int nth) const { return (nth & 7) == 7 ? eighth : usual; }
 };
 
 // ---- a chunk's tokens: global memory -> registers -> LDS ------------------------------------------------------------
@@ -236,7 +258,7 @@ template <typename T, int D, bool BACK> struct ChunkRows {
         off0 = c * W::kVec < D ? (uint32_t)row0 * (uint32_t)row_bytes + (uint32_t)c * 16u : kNoRow;
     }
     // rows that are no tokens (the lead of the first chunk; all of them unless `live`) read as zeros
-    __device__ __forceinline__ void load(int64_t c, bool live, int chunks, int lead, u32x4 (&reg)[W::kSteps]) const
+    template <bool NT = false> __device__ __forceinline__ void load(int64_t c, bool live, int chunks, int lead, u32x4 (&reg)[W::kSteps]) const
     {
         const int64_t base = BACK ? (int64_t)(chunks - 1 - c) * W::kChunk : c * W::kChunk - lead;
         const rsrc_t r = make_rsrc(head + base * row_bytes, live ? (uint32_t)((W::kChunk - 1) * row_bytes + D * (int)sizeof(T)) : 0u);
@@ -248,7 +270,7 @@ template <typename T, int D, bool BACK> struct ChunkRows {
         for (int i = 0; i < W::kSteps; ++i) {
             constexpr int kStep = W::kRowsPerStep;
             const bool is = BACK ? row0 < W::kChunk - nothing - i * kStep : row0 >= nothing - i * kStep;
-            reg[i] = load_stream16<false>(r, is ? off + (uint32_t)(i * kStep) * (uint32_t)row_bytes : kNoRow);
+            reg[i] = load_stream16<NT>(r, is ? off + (uint32_t)(i * kStep) * (uint32_t)row_bytes : kNoRow);
         }
     }
     __device__ __forceinline__ void put(unsigned char *tile, const u32x4 (&reg)[W::kSteps]) const
@@ -257,6 +279,23 @@ template <typename T, int D, bool BACK> struct ChunkRows {
 #pragma unroll
         for (int i = 0; i < W::kSteps; ++i)
             *reinterpret_cast<u32x4 *>(p + (BACK ? W::kSteps - 1 - i : i) * W::kRowsPerStep * W::kRowBytes) = reg[i];
+    }
+    // the other way: chunk c's rows from LDS, where they are tokens (none unless `live`)
+    __device__ __forceinline__ void store(int64_t c, bool live, int chunks, int lead, const unsigned char *tile) const
+    {
+        const int64_t base = BACK ? (int64_t)(chunks - 1 - c) * W::kChunk : c * W::kChunk - lead;
+        const rsrc_t r = make_rsrc(head + base * row_bytes, live ? (uint32_t)((W::kChunk - 1) * row_bytes + D * (int)sizeof(T)) : 0u);
+        const int nothing = c == 0 ? lead : 0;
+        const unsigned char *p = tile + (BACK ? W::kRowsPerStep - 1 - row0 : row0) * W::kRowBytes + (threadIdx.x % W::kRowVecs) * 16;
+        uint32_t off = off0;
+        asm volatile("" : "+v"(off));
+#pragma unroll
+        for (int i = 0; i < W::kSteps; ++i) {
+            constexpr int kStep = W::kRowsPerStep;
+            const bool is = BACK ? row0 < W::kChunk - nothing - i * kStep : row0 >= nothing - i * kStep;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(p + (BACK ? W::kSteps - 1 - i : i) * kStep * W::kRowBytes);
+            store_stream16<true>(r, is ? off + (uint32_t)(i * kStep) * (uint32_t)row_bytes : kNoRow, v);
+        }
     }
 };
 
@@ -315,12 +354,12 @@ template <int D> struct StatePanel {
                 if (kf < D) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s[kt][q]), r, at + (uint32_t)(kf * D) * 4u, 0, 0);
             }
     }
-    __device__ __forceinline__ void scale(float hi, float lo)
+    __device__ __forceinline__ void scale(float f)
     {
 #pragma unroll
         for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] = __builtin_fmaf(s[kt][r], hi, s[kt][r] * lo);
+            for (int r = 0; r < 16; ++r) s[kt][r] *= f;
     }
     __device__ __forceinline__ void eight(int sub, float (&x)[8]) const
     {
@@ -329,16 +368,18 @@ template <int D> struct StatePanel {
     }
 };
 
-// A row's weight in the new state, by lane half: l^{C-1-j} = [l^{C-8-16 sub-8 h}] l^{7-e} for j = 16 sub + 8 h + e.
+// A row's weight in the new state, by lane half: l^{C-1-j} for j = 16 sub + 8 h + e.
 template <int SUBS> struct UpdateWeights {
-    float base[SUBS], fine[8];
+    float w[SUBS][8];
     __device__ __forceinline__ UpdateWeights(const DecayPower &pw, int chunk, int back, float factor, int lane)
     {
         const int h = lane >> 5;
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s) base[s] = factor * pw(chunk - 8 - 16 * s - 8 * h + back);
+        for (int s = 0; s < SUBS; ++s) {
+            const float base = factor * pw(chunk - 8 - 16 * s - 8 * h + back);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) fine[e] = pw.uniform(7 - e);
+            for (int e = 0; e < 8; ++e) w[s][e] = base * pw.uniform(7 - e);
+        }
     }
 };
 
@@ -351,7 +392,7 @@ __device__ __forceinline__ void state_update(StatePanel<D> &S, const unsigned ch
     float x[8];
     oct_to(values, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] * w.fine[e] * w.base[sub];
+    for (int e = 0; e < 8; ++e) x[e] *= w.w[sub][e];
     const Pieces<T> v(x);
 #pragma unroll
     for (int kt = 0; kt < StatePanel<D>::kKeyTiles; ++kt) {
@@ -397,12 +438,11 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
     const float g = a.log_decay[h];
     const DecayPower pw(g);
     const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
-    float all_hi, all_lo;
-    pw.two(W::kChunk, g, all_hi, all_lo);
+    const ChunkDecay decay(W::kChunk, g);
     const ChunkRows<T, D, BACK> rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
     u32x4 nk[W::kSteps], nv[W::kSteps];
-    rk.load(c0, true, walk.chunks, walk.lead, nk);
-    rv.load(c0, true, walk.chunks, walk.lead, nv);
+    rk.template load<false>(c0, true, walk.chunks, walk.lead, nk);
+    rv.template load<false>(c0, true, walk.chunks, walk.lead, nv);
     StatePanel<D> S;
     S.clear();
     for (int c = c0; c < c1; ++c) {
@@ -410,9 +450,9 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
         rk.put(tileK, nk);
         rv.put(tileV, nv);
         lds_barrier();
-        rk.load(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
-        rv.load(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
-        S.scale(all_hi, all_lo);
+        rk.template load<false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
+        rv.template load<false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
+        S.scale(decay(c));
 #pragma unroll
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
             Oct<T> v;
@@ -422,7 +462,7 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
     }
     S.store(p.slots + ((int64_t)task.bh * a.segments + task.segment + 1) * D * D, panel, lane);
 }
-template <typename T, int D> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads)) void decay_sums(WalkArgs a)
+template <typename T, int D> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_sums(WalkArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * WalkShape<T, D>::kTileBytes];
     const int BH = a.B * a.H;
@@ -470,24 +510,32 @@ template <typename T, int D> __global__ __launch_bounds__(256) void decay_scan(W
     }
 }
 
-// Stores 16 features of a row tile: accumulators r0 .. r0 + 7 of lane l are value features 32 panel + 2 r0 + 8 (.. / 4) + 4 h + .. of token l % 32.
-__device__ __forceinline__ void store_features(rsrc_t r, uint32_t off, const f32x16 &acc, int half)
+// Sixteen value features of a row tile into the tokens' rows in LDS: accumulators 8 x .. 8 x + 7 of lane l are features 16 x + 8 (.. / 4) + 4 h
+// + .. of the panel, token l % 32.
+template <typename W> __device__ __forceinline__ void put_features(unsigned char *row, const f32x16 &acc, int half, uint16_t)
 {
-    uint32_t a0 = pack_bf16x2(acc[8 * half], acc[8 * half + 1]), a1 = pack_bf16x2(acc[8 * half + 2], acc[8 * half + 3]);
-    uint32_t b0 = pack_bf16x2(acc[8 * half + 4], acc[8 * half + 5]), b1 = pack_bf16x2(acc[8 * half + 6], acc[8 * half + 7]);
-    // lane half 0 gives its features 8..11 for the other half's 4..7: each lane then holds eight in a row
-    const auto x = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), y = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-    const u32x4 w = {x[0], y[0], x[1], y[1]};
-    store_stream16<false>(r, off, w);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const uint32_t a0 = pack_bf16x2(acc[8 * x], acc[8 * x + 1]), a1 = pack_bf16x2(acc[8 * x + 2], acc[8 * x + 3]);
+        const uint32_t b0 = pack_bf16x2(acc[8 * x + 4], acc[8 * x + 5]), b1 = pack_bf16x2(acc[8 * x + 6], acc[8 * x + 7]);
+        // lane half 0 gives its features 8..11 for the other half's 4..7: each lane then holds eight in a row
+        const auto p = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), q = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+        *reinterpret_cast<u32x4 *>(row + (16 * x + 8 * half) * 2) = u32x4{p[0], q[0], p[1], q[1]};
+    }
+}
+template <typename W> __device__ __forceinline__ void put_features(unsigned char *row, const f32x16 &acc, int half, float)
+{
+#pragma unroll
+    for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(row + (8 * x + 4 * half) * 4) = f32x4{acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]};
 }
 
-template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
+template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
 {
     using W = WalkShape<T, D>;
-    unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes;
-    float *table = reinterpret_cast<float *>(lds + 3 * W::kTileBytes), *from_state = table + 96;
-    const int b = task.bh / a.H, h = task.bh % a.H, lane = threadIdx.x & 63, panel = threadIdx.x >> 6;
-    const int half = lane >> 5, col = lane & 31;
+    unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes, *tileO = lds + 3 * W::kTileBytes;
+    Oct<T> *scores = reinterpret_cast<Oct<T> *>(lds + 4 * W::kTileBytes);
+    float *table = reinterpret_cast<float *>(lds + 4 * W::kTileBytes + W::kScoreBytes), *from_state = table + 96;
+    const int b = task.bh / a.H, h = task.bh % a.H, own_lane = threadIdx.x & 63, panel = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const DecayWalk walk(walk_length(a, b), W::kChunk);
     const int c0 = task.segment * a.per_segment;
     int c1 = c0 + a.per_segment;
@@ -498,17 +546,15 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_seg
                          : p.s_begin                                                          ? p.s_begin + (int64_t)task.bh * D * D
                                                                                               : nullptr;
     StatePanel<D> S;
-    if (begin) S.load(begin, p.turned, panel, lane);
+    if (begin) S.load(begin, p.turned, panel, own_lane);
     else S.clear();
     const bool keep = last && p.s_end;                               // this workgroup's state is the sequence's last
 
     const float g = a.log_decay[h];
     const DecayPower pw(g);
-    const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
-    // the first chunk of a sequence holds `lead` tokens fewer
-    float all_hi, all_lo, first_hi, first_lo;
-    pw.two(W::kChunk, g, all_hi, all_lo);
-    pw.two(W::kChunk - walk.lead, g, first_hi, first_lo);
+    const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, own_lane);
+    const ChunkDecay decay(W::kChunk, g);
+    const float first_decay = pw.uniform(W::kChunk - walk.lead);     // the first chunk of a sequence holds `lead` tokens fewer
     // a row's weight on what comes out of the state, whole chunks and the first one
     for (int i = threadIdx.x; i < W::kChunk; i += W::kWalkThreads) {
         const int e = i + 1 - (int)BACK;
@@ -518,29 +564,48 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_seg
     // weights of the scores by distance: table[63 - distance], zeros where the row lies behind.  Row 32 it + col and row 32 jt + 16 s + 8 half
     // + e are 32 (it - jt) + col - 16 s - 8 half - e apart.  In LDS: sixteen registers that every chunk needs for a moment only.
     for (int i = threadIdx.x; i < 96; i += W::kWalkThreads) table[i] = i < 64 ? p.weight_chunk * pw(63 - i) : 0.f;
-    const float *distance = table + 31 - col + 8 * half;
 
-    const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
-    unsigned char *out = static_cast<unsigned char *>(p.o) + (b * p.so.b + h * p.so.h) * (int64_t)sizeof(T);
-    const int64_t out_row = p.so.n * (int64_t)sizeof(T);
+    const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h), ro(p.o, p.so, b, h);
     u32x4 nq[W::kSteps], nk[W::kSteps], nv[W::kSteps];
-    rq.load(c0, c0 < c1, walk.chunks, walk.lead, nq);
-    rk.load(c0, c0 < c1, walk.chunks, walk.lead, nk);
-    rv.load(c0, c0 < c1, walk.chunks, walk.lead, nv);
+    rq.template load<NT>(c0, c0 < c1, walk.chunks, walk.lead, nq);
+    rk.template load<NT>(c0, c0 < c1, walk.chunks, walk.lead, nk);
+    rv.template load<NT>(c0, c0 < c1, walk.chunks, walk.lead, nv);
 
     for (int c = c0; c < c1; ++c) {
         lds_barrier();
+        ro.store(c - 1, c > c0, walk.chunks, walk.lead, tileO);
         rq.put(tileQ, nq);
         rk.put(tileK, nk);
         rv.put(tileV, nv);
         lds_barrier();
-        const bool more = c + 1 < c1;
-        // scores, weighted, as operands: of rows 0..31 with themselves, of rows 32..63 with rows 0..31 and with themselves
-        Oct<T> own[W::kTiles][2], across[2];
-        {
-            f32x16 P00, P01, P11;
+        rq.template load<NT>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nq);
+        rk.template load<NT>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
+        rv.template load<NT>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
+        // addresses are worked out anew for every chunk: kept over the loop they take the registers that the products need
+        int lane = own_lane;
+        asm volatile("" : "+v"(lane));
+        const int half = lane >> 5, col = lane & 31;
+        const float *distance = table + 31 - col + 8 * half;
+        // Scores P[jt, it] (rows jt, in decay_row's order, x rows it), weighted, as operands, and acc[it]: the output of rows it (value features x
+        // tokens) from the state.  SHARED: each tile of the scores is one wave's work (another one's with every chunk) for all waves, through LDS,
+        // in one run over the features with the products of the state; otherwise every wave has its own, worked out before.
+        f32x16 acc[W::kTiles];
+        Oct<T> own[W::kOwnTiles][2];
+        auto weigh = [&](const f32x16 &p, const float *near, Oct<T> (&o)[2]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) P00[r] = P01[r] = P11[r] = 0.f;
+            for (int s = 0; s < 2; ++s) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = p[8 * s + e] * near[16 * s + e];
+                oct_from(x, o[s]);
+            }
+        };
+        if constexpr (!W::kShared) {
+            f32x16 P[W::kScoreTiles];
+#pragma unroll
+            for (int t = 0; t < W::kScoreTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) P[t][r] = 0.f;
 #pragma unroll
             for (int sub = 0; sub < W::kSubs; ++sub) {
                 const int at = (16 * sub + 8 * half) * (int)sizeof(T);
@@ -550,47 +615,41 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_seg
                     row_operand(tileQ + (32 * t + col) * W::kRowBytes + at, q[t]);
                     row_operand(tileK + (32 * t + decay_row(col)) * W::kRowBytes + at, k[t]);
                 }
-                P00 = oct_product(k[0], q[0], P00);
+                P[0] = oct_product(k[0], q[0], P[0]);
                 if constexpr (W::kTiles == 2) {
-                    P01 = oct_product(k[0], q[1], P01);
-                    P11 = oct_product(k[1], q[1], P11);
+                    P[1] = oct_product(k[0], q[1], P[1]);
+                    P[2] = oct_product(k[1], q[1], P[2]);
                 }
-                if (sub % 2 == 1 || sub == W::kSubs - 1) __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float x[8], near[8];
+            for (int t = 0; t < W::kScoreTiles; ++t) weigh(P[t], distance + (t == 1 ? 0 : 32), own[t]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) near[e] = distance[32 + 16 * s + e];
+            for (int t = 0; t < W::kScoreTiles; ++t)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = P00[8 * s + e] * near[e];
-                oct_from(x, own[0][s]);
-                if constexpr (W::kTiles == 2) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = P11[8 * s + e] * near[e];
-                    oct_from(x, own[1][s]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = P01[8 * s + e] * distance[16 * s + e];
-                    oct_from(x, across[s]);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
+                for (int s = 0; s < 2; ++s) settle(own[t][s]);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        // the next chunk's tokens are requested where registers come free
-        rk.load(c + 1, more, walk.chunks, walk.lead, nk);
-        rv.load(c + 1, more, walk.chunks, walk.lead, nv);
-        // acc[it]: output of row tile it, value features x tokens, from the state
-        f32x16 acc[W::kTiles];
+        // the tile that is this wave's (SHARED): none from kScoreTiles on, which is worked out all the same to keep the run free of branches
+        f32x16 P;
+        const int mine = (panel + c) % W::kPanels;
+        const int my_j = W::kTiles == 2 && mine >= 2, my_i = W::kTiles == 2 && mine >= 1;
 #pragma unroll
-        for (int it = 0; it < W::kTiles; ++it)
+        for (int r = 0; r < 16; ++r) {
+            P[r] = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[it][r] = 0.f;
+            for (int it = 0; it < W::kTiles; ++it) acc[it][r] = 0.f;
+        }
 #pragma unroll
         for (int sub = 0; sub < W::kSubs; ++sub) {
+            const int at = (16 * sub + 8 * half) * (int)sizeof(T);
             Oct<T> q[W::kTiles];
 #pragma unroll
-            for (int t = 0; t < W::kTiles; ++t) row_operand(tileQ + (32 * t + col) * W::kRowBytes + (16 * sub + 8 * half) * (int)sizeof(T), q[t]);
+            for (int t = 0; t < W::kTiles; ++t) row_operand(tileQ + (32 * t + col) * W::kRowBytes + at, q[t]);
+            if constexpr (W::kShared) {
+                Oct<T> k, mq;
+                row_operand(tileK + (32 * my_j + decay_row(col)) * W::kRowBytes + at, k);
+                row_operand(tileQ + (32 * my_i + col) * W::kRowBytes + at, mq);
+                P = oct_product(k, mq, P);
+            }
             float x[8];
             S.eight(sub, x);
             const Pieces<T> s(x);
@@ -598,7 +657,14 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_seg
             for (int t = 0; t < W::kTiles; ++t) acc[t] = s.first(q[t], acc[t]);
 #pragma unroll
             for (int t = 0; t < W::kTiles; ++t) acc[t] = s.second(q[t], acc[t]);
-            if (sub % 2 == 1 || sub == W::kSubs - 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (W::kShared) {
+            if (mine < W::kScoreTiles) {
+                weigh(P, distance + (mine == 1 ? 0 : 32), own[0]);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) scores[(2 * mine + s) * 64 + lane] = own[0][s];
+            }
+            lds_barrier();
         }
 #pragma unroll
         for (int it = 0; it < W::kTiles; ++it) {
@@ -606,54 +672,34 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_seg
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[it][r] *= weight;
         }
-        __builtin_amdgcn_sched_barrier(0);
         // from the chunk itself, and the chunk into the state
-        S.scale(c == 0 ? first_hi : all_hi, c == 0 ? first_lo : all_lo);
+        S.scale(c == 0 ? first_decay : decay(c));
 #pragma unroll
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
             Oct<T> v;
-            if (sub == W::kTokSubs - 1) rq.load(c + 1, more, walk.chunks, walk.lead, nq);
             token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
-            if (sub < 2) acc[0] = oct_product(v, own[0][sub], acc[0]);
-            if constexpr (W::kTiles == 2) acc[1] = oct_product(v, sub < 2 ? across[sub] : own[1][sub - 2], acc[1]);
+            auto weights = [&](int t, int s) __attribute__((always_inline)) { return W::kShared ? scores[(2 * t + s) * 64 + lane] : own[W::kShared ? 0 : t][s]; };
+            if (sub < 2) acc[0] = oct_product(v, weights(0, sub), acc[0]);
+            if constexpr (W::kTiles == 2) acc[1] = oct_product(v, weights(1 + sub / 2, sub % 2), acc[1]);
             state_update<T, D>(S, tileK, v, uw, sub, lane);
-            __builtin_amdgcn_sched_barrier(0);
         }
-        // the chunk's output rows, where they are tokens
-        const int64_t base = BACK ? (int64_t)(walk.chunks - 1 - c) * W::kChunk : (int64_t)c * W::kChunk - walk.lead;
-        const rsrc_t ro = make_rsrc(out + base * out_row, (uint32_t)((W::kChunk - 1) * out_row + D * (int)sizeof(T)));
-        const int nothing = c == 0 ? walk.lead : 0;
+        // the output's rows, for whole-row stores once all panels are in
 #pragma unroll
-        for (int it = 0; it < W::kTiles; ++it) {
-            const int row = 32 * it + col;
-            const uint32_t off = row >= nothing ? (uint32_t)(BACK ? W::kChunk - 1 - row : row) * (uint32_t)out_row : kNoRow;
-            if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int f = 32 * panel + 16 * x + 8 * half;
-                    store_features(ro, f < D ? off + (uint32_t)f * 2u : kNoRow, acc[it], x);
-                }
-            } else {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int f = 32 * panel + 8 * x + 4 * half;
-                    const f32x4 w = {acc[it][4 * x], acc[it][4 * x + 1], acc[it][4 * x + 2], acc[it][4 * x + 3]};
-                    store_stream16<false>(ro, f < D ? off + (uint32_t)f * 4u : kNoRow, __builtin_bit_cast(u32x4, w));
-                }
-            }
-        }
+        for (int it = 0; it < W::kTiles; ++it) put_features<W>(tileO + (32 * it + col) * W::kRowBytes + 32 * panel * (int)sizeof(T), acc[it], half, T{});
     }
-    if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, lane);
+    lds_barrier();
+    if (c0 < c1) ro.store(c1 - 1, true, walk.chunks, walk.lead, tileO);
+    if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, own_lane);
 }
-template <typename T, int D> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
+template <typename T, int D, bool NT> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
 {
-    __shared__ __align__(16) unsigned char lds[3 * WalkShape<T, D>::kTileBytes + kDecayTableBytes];
+    __shared__ __align__(16) unsigned char lds[4 * WalkShape<T, D>::kTileBytes + WalkShape<T, D>::kScoreBytes + kDecayTableBytes];
     const int BH = a.B * a.H;
     const WalkTask task(a.problems * BH * a.segments, BH, a.segments, a.together);
     if (!task.any) return;
     const WalkProblem &p = a.p[task.problem];
-    if (p.back) walk_segment<T, D, true>(a, p, task, lds);
-    else walk_segment<T, D, false>(a, p, task, lds);
+    if (p.back) walk_segment<T, D, true, NT>(a, p, task, lds);
+    else walk_segment<T, D, false, NT>(a, p, task, lds);
 }
 
 }  // namespace sv

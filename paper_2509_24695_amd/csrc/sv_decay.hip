@@ -6,12 +6,15 @@
 #include "decay_token.hpp"
 #include "decay_walk.hpp"
 #include "desc_checks.hpp"
+#include "layout_rules.hpp"
 
 namespace {
 
 using namespace sv;
 
 constexpr int64_t kMostHeads = 1 << 24;
+constexpr int64_t kLastCacheBytes = (int64_t)256 << 20;      // the memory side's cache
+constexpr int kBackwardWalks = 3;              // dq, dv and dk, in one launch
 
 bool overlaps(const void *a, const void *b, size_t bytes)
 {
@@ -39,11 +42,11 @@ sv_status check_pair(const sv_tensor_desc *qkv, const sv_tensor_desc *o, Shape *
     return SV_OK;
 }
 
-DecayPlan plan_of(int64_t BH, int n_tokens, bool bf16) { return decay_plan(BH, n_tokens, bf16 ? kDecayChunkBf16 : kDecayChunkF32); }
+DecayPlan plan_of(int64_t BH, int n_tokens, int d, bool bf16, int walks) { return decay_plan(BH, n_tokens, d, bf16 ? kDecayChunkBf16 : kDecayChunkF32, walks); }
 
-size_t slots_bytes(int64_t BH, int n_tokens, int d)
+size_t slots_bytes(int64_t BH, int n_tokens, int d, int walks)
 {
-    const int a = plan_of(BH, n_tokens, true).segments, b = plan_of(BH, n_tokens, false).segments;
+    const int a = plan_of(BH, n_tokens, d, true, walks).segments, b = plan_of(BH, n_tokens, d, false, walks).segments;
     return (size_t)BH * (a > b ? a : b) * d * d * sizeof(float);
 }
 
@@ -65,7 +68,11 @@ template <typename T, int D> sv_status run_walk(WalkArgs sums, const WalkArgs &w
         decay_scan<T, D><<<(unsigned)(sums.problems * BH * ((D * D / 4 + 255) / 256)), 256, 0, stream>>>(sums);
         if (launched() != SV_OK) return SV_ERR_LAUNCH;
     }
-    decay_walk<T, D><<<decay_grid(walks.problems * BH * walks.segments, walks.together), W::kWalkThreads, 0, stream>>>(walks);
+    const unsigned grid = decay_grid(walks.problems * BH * walks.segments, walks.together);
+    if (walks.problems == 1 && (int64_t)2 * BH * walks.N * D * (int)sizeof(T) > kLastCacheBytes)
+        decay_walk<T, D, true><<<grid, W::kWalkThreads, 0, stream>>>(walks);
+    else
+        decay_walk<T, D, false><<<grid, W::kWalkThreads, 0, stream>>>(walks);
     return launched();
 }
 
@@ -88,7 +95,7 @@ WalkArgs walk_args(const Shape &s, const float *log_decay, const int32_t *length
     a.segments = plan.segments;
     a.per_segment = plan.per_segment;
     a.problems = problems;
-    a.together = 1;
+    a.together = TokenLayout{s.BH, s.H, s.d, s.elem_bytes, s.st.h, s.st.n}.shares_lines() ? 4 : 1;
     return a;
 }
 
@@ -96,12 +103,12 @@ WalkArgs walk_args(const Shape &s, const float *log_decay, const int32_t *length
 
 extern "C" size_t sv_decay_linattn_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d)
 {
-    return sizes_ok(B, H, n_tokens, d) ? slots_bytes((int64_t)B * H, n_tokens, d) : 0;
+    return sizes_ok(B, H, n_tokens, d) ? slots_bytes((int64_t)B * H, n_tokens, d, 1) : 0;
 }
 
 extern "C" size_t sv_decay_linattn_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d)
 {
-    return sizes_ok(B, H, n_tokens, d) ? 2 * slots_bytes((int64_t)B * H, n_tokens, d) : 0;
+    return sizes_ok(B, H, n_tokens, d) ? 2 * slots_bytes((int64_t)B * H, n_tokens, d, kBackwardWalks) : 0;
 }
 
 extern "C" sv_status sv_decay_linattn(const void *Q, const void *K, const void *V, const sv_tensor_desc *qkv, const float *log_decay,
@@ -116,8 +123,8 @@ extern "C" sv_status sv_decay_linattn(const void *Q, const void *K, const void *
     if (!isfinite(scale)) return SV_ERR_RANGE;
     const size_t states = (size_t)x.BH * x.d * x.d * sizeof(float);
     if (O == Q || O == K || O == V || (S_in != S_out && overlaps(S_in, S_out, states))) return SV_ERR_SHAPE;
-    if (workspace_bytes < slots_bytes(x.BH, x.N, x.d)) return SV_ERR_WORKSPACE;
-    WalkArgs a = walk_args(x, log_decay, lengths, plan_of(x.BH, x.N, x.bf16), 1);
+    if (workspace_bytes < slots_bytes(x.BH, x.N, x.d, 1)) return SV_ERR_WORKSPACE;
+    WalkArgs a = walk_args(x, log_decay, lengths, plan_of(x.BH, x.N, x.d, x.bf16, 1), 1);
     a.p[0] = WalkProblem{Q, K, V, O, x.st, x.st, x.st, y.st, S_in, S_out, static_cast<float *>(workspace), scale, scale, 1.f, 0, 0};
     return run_walk(x.bf16, x.d, a, a, stream);
 }
@@ -137,11 +144,11 @@ extern "C" sv_status sv_decay_linattn_backward(const void *Q, const void *K, con
     for (const void *out : {dQ, dK, dV})
         if (out == Q || out == K || out == V || out == dO) return SV_ERR_SHAPE;
     if (dQ == dK || dQ == dV || dK == dV || overlaps(dS_in, dS_out, states) || overlaps(dS_in, S_in, states)) return SV_ERR_SHAPE;
-    const size_t half = slots_bytes(x.BH, x.N, x.d);
+    const size_t half = slots_bytes(x.BH, x.N, x.d, kBackwardWalks);
     if (workspace_bytes < 2 * half) return SV_ERR_WORKSPACE;
     float *states_fwd = static_cast<float *>(workspace), *states_back = states_fwd + half / sizeof(float);
-    const DecayPlan plan = plan_of(x.BH, x.N, x.bf16);
-    WalkArgs sums = walk_args(x, log_decay, lengths, plan, 2), walks = walk_args(x, log_decay, lengths, plan, 3);
+    const DecayPlan plan = plan_of(x.BH, x.N, x.d, x.bf16, kBackwardWalks);
+    WalkArgs sums = walk_args(x, log_decay, lengths, plan, 2), walks = walk_args(x, log_decay, lengths, plan, kBackwardWalks);
     sums.p[0] = WalkProblem{nullptr, K, V, nullptr, x.st, x.st, x.st, y.st, S_in, nullptr, states_fwd, 0.f, 0.f, 1.f, 0, 0};
     sums.p[1] = WalkProblem{nullptr, Q, dO, nullptr, x.st, x.st, y.st, y.st, dS_out, nullptr, states_back, 0.f, 0.f, scale, 1, 0};
     walks.p[0] = WalkProblem{dO, V, K, dQ, y.st, x.st, x.st, x.st, S_in, nullptr, states_fwd, scale, scale, 1.f, 0, 1};

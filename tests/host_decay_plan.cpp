@@ -22,7 +22,7 @@ int main()
     for (int chunk : {32, 64})
         for (int n : lengths)
             for (long long BH : heads) {
-                const DecayPlan p = decay_plan(BH, n, chunk);
+                const DecayPlan p = decay_plan(BH, n, 64, chunk, 1);
                 if (p.chunks != (int)(((long long)n + chunk - 1) / chunk)) return fail("chunks", n, BH);
                 if (p.segments < 1 || p.segments > kMaxDecaySegments || p.per_segment < 1) return fail("segments", n, BH);
                 if ((long long)p.segments * p.per_segment < p.chunks) return fail("chunks left over", n, BH);

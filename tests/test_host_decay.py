@@ -91,7 +91,7 @@ def test_aliases():
 def test_workspace_and_pool():
     for (B, H, N, d) in ((1, 2, 128, 64), (3, 20, 4000, 112), (1, 1, 1, 32), (2, 300, 100000, 128)):
         n, m = sv.sv_decay_linattn_workspace_bytes(B, H, N, d), sv.sv_decay_linattn_backward_workspace_bytes(B, H, N, d)
-        assert n >= B * H * d * d * 4 and m == 2 * n and n % 16 == 0
+        assert n >= B * H * d * d * 4 and m >= 2 * B * H * d * d * 4 and n % 16 == 0 and m % 16 == 0
         dsc = _desc(B=B, H=H, N=N, d=d, stride_b=H * N * d, stride_h=N * d, stride_n=d)
         assert _prompt(qkv=dsc, o=dsc, wb=n - 1, s_in=None, s_out=None) == 6
         assert _backward(qkv=dsc, o=dsc, wb=m - 1, s_in=None, ds_out=None, ds_in=None) == 6
