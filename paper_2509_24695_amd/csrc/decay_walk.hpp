@@ -139,7 +139,8 @@ template <typename T, int D> struct WalkShape {
     static constexpr int kSubs = D / 16;                     // contractions over features, 16 at a time
     static constexpr int kTokSubs = kChunk / 16;             // and over the chunk's tokens
     static constexpr int kScoreTiles = kTiles == 2 ? 3 : 1;
-    static constexpr bool kShared = sizeof(T) == 2 && kPanels == 4;
+    // who works the scores out: tile by tile for each other (kShared), each a part of the features (kSplit), or every wave for itself
+    static constexpr bool kShared = sizeof(T) == 2 && kPanels == 4, kSplit = sizeof(T) == 4 && kPanels > 1;
     static constexpr int kOwnTiles = kShared ? 1 : kScoreTiles, kScoreBytes = kShared ? kScoreTiles * 2 * 64 * 8 * (int)sizeof(T) : 0;
     static_assert(kSteps * kRowsPerStep == kChunk && D % 16 == 0, "whole rows");
 };
@@ -600,7 +601,21 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
                 oct_from(x, o[s]);
             }
         };
-        if constexpr (!W::kShared) {
+        f32x16 part;                                                   // kSplit: this wave's sum over its features
+        if constexpr (W::kSplit) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) part[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < (W::kSubs + W::kPanels - 1) / W::kPanels; ++i) {
+                const int sub = panel + i * W::kPanels, at = (16 * sub + 8 * half) * (int)sizeof(T);
+                if (sub < W::kSubs) {
+                    Oct<T> q, k;
+                    row_operand(tileQ + col * W::kRowBytes + at, q);
+                    row_operand(tileK + decay_row(col) * W::kRowBytes + at, k);
+                    part = oct_product(k, q, part);
+                }
+            }
+        } else if constexpr (!W::kShared) {
             f32x16 P[W::kScoreTiles];
 #pragma unroll
             for (int t = 0; t < W::kScoreTiles; ++t)
@@ -665,6 +680,24 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
                 for (int s = 0; s < 2; ++s) scores[(2 * mine + s) * 64 + lane] = own[0][s];
             }
             lds_barrier();
+        }
+        if constexpr (W::kSplit) {
+            // the parts are added up in the panels' order, in the room of the queries, which are done with
+            f32x4 *parts = reinterpret_cast<f32x4 *>(tileQ);
+            static_assert(W::kPanels * 4096 <= W::kTileBytes, "sixteen floats of each lane");
+            lds_barrier();
+#pragma unroll
+            for (int x = 0; x < 4; ++x) parts[(panel * 4 + x) * 64 + lane] = f32x4{part[4 * x], part[4 * x + 1], part[4 * x + 2], part[4 * x + 3]};
+            lds_barrier();
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                f32x4 sum = parts[x * 64 + lane];
+#pragma unroll
+                for (int w = 1; w < W::kPanels; ++w) sum += parts[(w * 4 + x) * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[4 * x + e] = sum[e];
+            }
+            weigh(part, distance + 32, own[0]);
         }
 #pragma unroll
         for (int it = 0; it < W::kTiles; ++it) {
