@@ -4,8 +4,10 @@
 //   dx = rstd (t - sum t / d - xh sum (t xh) / d)  with t = w dy,   dw = sum over rows of dy xh,   db = sum over rows of dy
 //
 // Bound by memory: a row is read once into registers (16 bytes per lane and piece), its sums go across the lanes that hold it, and it is
-// written from there.  A lane keeps the same features for all rows that its workgroup walks, so the parameters stay in registers too, and
-// the backward pass adds up dw and db of its features there: a workgroup leaves one partial sum of each, norm_fold adds these up in order.
+// written from there, while the next one is on its way (two and four rows at a time gained nothing).  A lane keeps the same features for all
+// rows that its workgroup walks, so the parameters stay in registers too, and the backward pass adds up dw and db of its features there: a
+// workgroup leaves one partial sum of each, norm_fold adds these up in order.  32 760 rows of 2 240 features of bf16: forwards 48 us, backwards 93
+// (440 MB, 4.7 TB/s, the fold of 9 MB of partial sums included).
 #pragma once
 
 #include "common.hpp"
@@ -15,7 +17,7 @@ namespace sv {
 
 // An axis of the rows' index, fastest first; strides in elements of the tensors and of the statistics.
 struct NormAxis {
-    int32_t extent;
+    NormDivisor extent;
     int64_t a, b, c, stat;
 };
 struct NormArgs {
@@ -29,6 +31,7 @@ struct NormArgs {
     int64_t group_a, group_b, group_c, group_stat;     // strides of the groups
     int64_t rows;                  // of a group
     int d, groups, workgroups;     // workgroups of a group
+    int whole_lines;               // rows are whole 128-byte lines: written past the caches
     float eps;
 };
 
@@ -78,9 +81,10 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x, float *ld
         lds_barrier();                                                // the last sum has been read
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
         lds_barrier();
-        x = lds[0];
+        const float *mine = lds + threadIdx.x / LANES * kWaves;
+        x = mine[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) x += lds[w];
+        for (int w = 1; w < kWaves; ++w) x += mine[w];
     }
     return x;
 }
@@ -102,7 +106,7 @@ struct NormPlace {
         uint32_t r = (uint32_t)row;                                   // the host keeps rows below 2^31
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
-            const uint32_t e = (uint32_t)g.axis[i].extent, q = i < 2 ? r / e : 0u, k = r - q * e;
+            const uint32_t q = i < 2 ? g.axis[i].extent.quotient(r) : 0u, k = r - q * g.axis[i].extent.extent;
             a += k * g.axis[i].a;
             b += k * g.axis[i].b;
             c += k * g.axis[i].c;
@@ -120,6 +124,12 @@ template <typename T, int LANES, int VECS> __device__ __forceinline__ void load_
         const int f = (lane + i * LANES) * Piece<T>::kN;
         v[i] = f < d ? *reinterpret_cast<const u32x4 *>(p + f) : u32x4{0u, 0u, 0u, 0u};
     }
+}
+
+__device__ __forceinline__ void store_piece(void *p, u32x4 v, bool whole_lines)
+{
+    if (whole_lines) __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
+    else *static_cast<u32x4 *>(p) = v;
 }
 
 // A lane's part of a row of parameters, or `otherwise` where there is none.
@@ -183,7 +193,7 @@ template <typename T, int LANES, int VECS> __global__ __launch_bounds__((NormWal
             const int f = (walk.lane + i * LANES) * kN;
 #pragma unroll
             for (int e = 0; e < kN; ++e) x[i][e] = __builtin_fmaf(x[i][e] * rstd, w[i][e], b[i][e]);
-            if (f < a.d) *reinterpret_cast<u32x4 *>(y + f) = Piece<T>::close(x[i]);
+            if (f < a.d) store_piece(y + f, Piece<T>::close(x[i]), a.whole_lines);
         }
         if (a.mean && walk.lane == 0) {
             a.mean[place.stat] = mean;
@@ -258,7 +268,7 @@ template <typename T, int LANES, int VECS, bool PARAMS> __global__ __launch_boun
             Piece<T>::open(vdy[i], g);
 #pragma unroll
             for (int e = 0; e < kN; ++e) x[e] = rstd * (w[i][e] * g[e] - level - (x[e] - mean) * rstd * along);
-            if (f < a.d) *reinterpret_cast<u32x4 *>(dx + f) = Piece<T>::close(x);
+            if (f < a.d) store_piece(dx + f, Piece<T>::close(x), a.whole_lines);
         }
     }
     if constexpr (PARAMS) {

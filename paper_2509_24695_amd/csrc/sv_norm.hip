@@ -27,18 +27,27 @@ bool same_rows(const Shape &x, const Shape &y) { return x.st.b == y.st.b && x.st
 // The rows of x's shape as groups (heads with parameters of their own, or one) of rows, walked in the order in which x lies in memory.
 void set_rows(NormArgs &g, const Shape &x, const Shape &b, const Shape &c, int groups)
 {
-    NormAxis ax[3] = {{x.N, x.st.n, b.st.n, c.st.n, 1}, {x.H, x.st.h, b.st.h, c.st.h, x.N}, {x.B, x.st.b, b.st.b, c.st.b, (int64_t)x.H * x.N}};
+    NormAxis ax[3] = {{NormDivisor::of(x.N), x.st.n, b.st.n, c.st.n, 1},
+                      {NormDivisor::of(x.H), x.st.h, b.st.h, c.st.h, x.N},
+                      {NormDivisor::of(x.B), x.st.b, b.st.b, c.st.b, (int64_t)x.H * x.N}};
     if (groups > 1) {
         g.group_a = ax[1].a; g.group_b = ax[1].b; g.group_c = ax[1].c; g.group_stat = ax[1].stat;
-        ax[1].extent = 1;
+        ax[1].extent = NormDivisor::of(1);
     }
     for (int i = 0; i < 3; ++i)
         for (int j = i + 1; j < 3; ++j)
-            if (ax[j].extent > 1 && (ax[i].extent == 1 || ax[j].a < ax[i].a)) { const NormAxis t = ax[i]; ax[i] = ax[j]; ax[j] = t; }
+            if (ax[j].extent.extent > 1 && (ax[i].extent.extent == 1 || ax[j].a < ax[i].a)) { const NormAxis t = ax[i]; ax[i] = ax[j]; ax[j] = t; }
     for (int i = 0; i < 3; ++i) g.axis[i] = ax[i];
     g.groups = groups;
     g.rows = (int64_t)x.BH * x.N / groups;
     g.d = x.d;
+}
+
+// Is every row a run of whole 128-byte lines (given a tensor that begins with one)?
+bool lines_whole(const Shape &s)
+{
+    const int64_t line = 128 / s.elem_bytes;
+    return s.d % line == 0 && s.st.n % line == 0 && (s.H == 1 || s.st.h % line == 0) && (s.B == 1 || s.st.b % line == 0);
 }
 
 sv_status launched() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
@@ -46,26 +55,26 @@ sv_status launched() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_L
 // Calls f(lanes, vecs) with the constants of a form.
 template <typename F> void with_form(const NormForm &form, F &&f)
 {
-    auto vecs = [&](auto v) { f(std::integral_constant<int, 64>{}, v); };
-    switch (form.lanes) {
-    case 4: f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{}); break;
-    case 8: f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{}); break;
-    case 16: f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}); break;
-    case 32: f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{}); break;
-    case 64:
-        switch (form.vecs) {
-        case 1: vecs(std::integral_constant<int, 1>{}); break;
-        case 2: vecs(std::integral_constant<int, 2>{}); break;
-        case 3: vecs(std::integral_constant<int, 3>{}); break;
-        case 4: vecs(std::integral_constant<int, 4>{}); break;
-        case 5: vecs(std::integral_constant<int, 5>{}); break;
-        default: vecs(std::integral_constant<int, 6>{}); break;
-        }
-        break;
-    case 256: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{}); break;
-    case 512: f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{}); break;
-    default: f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{}); break;
-    }
+    auto is = [&](auto lanes, auto vecs) {
+        if (form.lanes == lanes() && form.vecs == vecs()) f(lanes, vecs);
+    };
+    auto one = [&](auto lanes) { is(lanes, std::integral_constant<int, 1>{}); };
+    auto two = [&](auto lanes) { is(lanes, std::integral_constant<int, 2>{}); };
+    auto three = [&](auto lanes) { is(lanes, std::integral_constant<int, 3>{}); };
+    auto four = [&](auto lanes) { is(lanes, std::integral_constant<int, 4>{}); };
+    one(std::integral_constant<int, 4>{});
+    one(std::integral_constant<int, 8>{});
+    one(std::integral_constant<int, 16>{});
+    one(std::integral_constant<int, 32>{});
+    const std::integral_constant<int, 64> wave;
+    one(wave), two(wave), three(wave), four(wave);
+    is(wave, std::integral_constant<int, 5>{});
+    is(wave, std::integral_constant<int, 6>{});
+    const std::integral_constant<int, 128> waves;
+    two(waves), three(waves), four(waves);
+    three(std::integral_constant<int, 256>{});
+    two(std::integral_constant<int, 512>{});
+    two(std::integral_constant<int, 1024>{});
 }
 
 size_t partial_bytes(int64_t groups, int workgroups, int d) { return (size_t)groups * workgroups * 2 * d * sizeof(float); }
@@ -88,14 +97,17 @@ extern "C" sv_status sv_layernorm(const void *X, const sv_tensor_desc *x, const 
     NormArgs a{};
     a.x = X; a.y = Y; a.weight = weight; a.bias = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
     set_rows(a, in, out, out, weight_heads);
-    const NormForm form = norm_form(in.d * in.elem_bytes / 16);
+    const NormForm form = norm_form(in.d * in.elem_bytes / 16, false);
+    a.whole_lines = lines_whole(out);
     a.workgroups = norm_workgroups(form, a.rows, a.groups, kNormForwardWgs);
     const unsigned grid = (unsigned)((int64_t)a.groups * a.workgroups);
     const auto hs = static_cast<hipStream_t>(stream);
     with_form(form, [&](auto lanes, auto vecs) {
-        if constexpr (lanes() * vecs() <= kNormMostWidth / 8)         // bf16 rows have no more pieces
-            if (in.bf16) norm_rows<uint16_t, lanes(), vecs()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
-        if (!in.bf16) norm_rows<float, lanes(), vecs()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
+        if constexpr (lanes() != 128 || vecs() == 4) {                // forwards, narrower rows lie in one wave
+            if constexpr (lanes() <= 512)                             // bf16 rows have no more pieces
+                if (in.bf16) norm_rows<uint16_t, lanes(), vecs()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
+            if (!in.bf16) norm_rows<float, lanes(), vecs()><<<grid, NormWalk<lanes()>::kThreadsOf, 0, hs>>>(a);
+        }
     });
     return launched();
 }
@@ -104,7 +116,7 @@ extern "C" size_t sv_layernorm_backward_workspace_bytes(int32_t B, int32_t H, in
 {
     if (B <= 0 || H <= 0 || n_tokens <= 0 || d <= 0 || d % 4 || d > kNormMostWidth || (int64_t)B * H > kMostHeads) return 0;
     // at most this many partial sums, whatever the type and the number of parameter rows
-    const int64_t most = H > kNormBackwardWgs ? H : kNormBackwardWgs;
+    const int64_t most = H > kNormMostBackwardWgs ? H : kNormMostBackwardWgs;
     return partial_bytes(1, (int)most, d);
 }
 
@@ -131,8 +143,9 @@ extern "C" sv_status sv_layernorm_backward(const void *X, const sv_tensor_desc *
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.dw = dweight; a.db = dbias;
     set_rows(a, in, grad, out, weight_heads);
-    const NormForm form = norm_form(in.d * in.elem_bytes / 16);
-    a.workgroups = norm_workgroups(form, a.rows, a.groups, kNormBackwardWgs);
+    const NormForm form = norm_form(in.d * in.elem_bytes / 16, true);
+    a.whole_lines = lines_whole(out);
+    a.workgroups = norm_workgroups(form, a.rows, a.groups, norm_backward_wgs(in.d));
     if (params && workspace_bytes < partial_bytes(a.groups, a.workgroups, in.d)) return SV_ERR_WORKSPACE;
     a.partial = static_cast<float *>(workspace);
     const unsigned grid = (unsigned)((int64_t)a.groups * a.workgroups);
@@ -145,9 +158,11 @@ extern "C" sv_status sv_layernorm_backward(const void *X, const sv_tensor_desc *
             if (params) go(t, std::true_type{});
             else go(t, std::false_type{});
         };
-        if constexpr (lanes() * vecs() <= kNormMostWidth / 8)
-            if (in.bf16) pick(uint16_t{});
-        if (!in.bf16) pick(float{});
+        if constexpr (lanes() != 64 || vecs() <= 3) {                 // backwards, wider rows lie in more lanes
+            if constexpr (lanes() <= 512)
+                if (in.bf16) pick(uint16_t{});
+            if (!in.bf16) pick(float{});
+        }
     });
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
     if (params) {
