@@ -2,7 +2,8 @@
 //
 // A copy with four multiplications per pair: bound by memory.  A thread owns 16 bytes of one token's rows (four pairs of bf16, two of fp32),
 // works the token's place out and fetches its angles once, and then runs over the heads, first of q, then of k, whose rows all take the
-// same angles.
+// same angles.  32 760 tokens of 20 heads of 112, views of one projection's output: 587 MB in 130 us, 4.5 TB/s; 3 519 tokens of 3 x 16 heads of 128 in
+// fp32 50 us, 6.6 TB/s (61 without the hint at the stores, which heads that share lines do without: 133 with it).
 #pragma once
 
 #include "common.hpp"
@@ -19,6 +20,7 @@ struct RotateArgs {
     const int32_t *positions;      // [B][N][3] or NULL
     float sign;                    // of the sines
     int head_group;                // heads that a workgroup runs over
+    int own_lines;                 // heads of y share no cache lines: written past the caches
 };
 
 template <typename T, int D> struct RotateShape {
@@ -41,6 +43,12 @@ __device__ __forceinline__ u32x4 rotate16(u32x4 v, const f32x2 (&cs)[2], float)
         v[2 * p + 1] = __float_as_uint(a * cs[p].y + b * cs[p].x);
     }
     return v;
+}
+
+__device__ __forceinline__ void store_rotated(void *p, u32x4 v, bool own_lines)
+{
+    if (own_lines) __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
+    else *static_cast<u32x4 *>(p) = v;
 }
 
 template <typename T, int D> __global__ __launch_bounds__(kThreads) void rotate_rows(RotateArgs a)
@@ -81,9 +89,9 @@ template <typename T, int D> __global__ __launch_bounds__(kThreads) void rotate_
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) v[i] = *reinterpret_cast<const u32x4 *>(x + (h + i) * a.sx.h);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) *reinterpret_cast<u32x4 *>(y + (h + i) * a.sy.h) = rotate16(v[i], cs, T{});
+            for (int i = 0; i < kAhead; ++i) store_rotated(y + (h + i) * a.sy.h, rotate16(v[i], cs, T{}), a.own_lines);
         }
-        for (; h < h1; ++h) *reinterpret_cast<u32x4 *>(y + h * a.sy.h) = rotate16(*reinterpret_cast<const u32x4 *>(x + h * a.sx.h), cs, T{});
+        for (; h < h1; ++h) store_rotated(y + h * a.sy.h, rotate16(*reinterpret_cast<const u32x4 *>(x + h * a.sx.h), cs, T{}), a.own_lines);
     }
 }
 

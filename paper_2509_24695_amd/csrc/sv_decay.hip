@@ -178,7 +178,7 @@ extern "C" sv_status sv_decay_linattn_token(const void *Q, const void *K, const 
             constexpr int kSplit = split();
             decay_token<T, D(), kSplit><<<(unsigned)((int64_t)x.BH * kSplit), TokenShape<D(), kSplit>::kTokThreads, 0, hs>>>(a);
         };
-        const bool few = x.BH < 256;
+        const bool few = x.BH <= kFewTokenHeads;
         auto pick = [&](auto t) {
             if (few) go(t, std::integral_constant<int, 4>{});
             else go(t, std::integral_constant<int, 1>{});

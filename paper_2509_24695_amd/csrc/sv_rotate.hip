@@ -2,6 +2,7 @@
 #include "../../include/sv_rope.h"
 
 #include "desc_checks.hpp"
+#include "layout_rules.hpp"
 #include "rotate.hpp"
 
 namespace {
@@ -46,6 +47,7 @@ extern "C" sv_status sv_rope3d_rotate(const void *Q, const void *K, const sv_ten
     a.cs_t = rope->cs_t; a.cs_h = rope->cs_h; a.cs_w = rope->cs_w;
     a.positions = positions;
     a.sign = inverse ? -1.f : 1.f;
+    a.own_lines = !TokenLayout{out.BH, out.H, out.d, out.elem_bytes, out.st.h, out.st.n}.shares_lines();
     with_head_dim(in.d, [&](auto D) {
         auto go = [&](auto t) {
             using W = RotateShape<decltype(t), D()>;
