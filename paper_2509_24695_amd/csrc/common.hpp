@@ -84,6 +84,19 @@ template <bool NT = true> __device__ __forceinline__ u32x4 load_stream16(rsrc_t 
 template <bool NT = true> __device__ __forceinline__ void store_stream16(rsrc_t r, uint32_t off, u32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, NT ? 2 : 0);
 }
+// 16 bytes to global memory, past the caches or not.  The empty statements keep the two stores apart: the compiler makes one of them otherwise,
+// without the hint.
+template <typename V> __device__ __forceinline__ void store16(void *p, V v, bool past_caches)
+{
+    static_assert(sizeof(V) == 16, "a piece");
+    if (past_caches) {
+        asm volatile("");
+        __builtin_nontemporal_store(v, static_cast<V *>(p));
+        asm volatile("");
+    } else {
+        *static_cast<V *>(p) = v;
+    }
+}
 // Cached 16-byte load (rotation table: shared by all heads, worth keeping in L2).
 __device__ __forceinline__ f32x4 load_cached16(rsrc_t r, uint32_t off) {
     return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));

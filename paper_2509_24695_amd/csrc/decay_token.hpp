@@ -77,9 +77,7 @@ template <typename T, int D, int SPLIT> __global__ __launch_bounds__(256) void d
                 s[i][e] = __builtin_fmaf(kk, vv[e], l * s[i][e]);
                 sum[e] = __builtin_fmaf(qq, s[i][e], sum[e]);
             }
-            f32x4 *to = reinterpret_cast<f32x4 *>(a.s_out + at + row * D + c);
-            if (elsewhere) __builtin_nontemporal_store(s[i], to);
-            else *to = s[i];
+            store16(a.s_out + at + row * D + c, s[i], elsewhere);
         }
     }
     sums[row0][group] = sum;

@@ -126,12 +126,6 @@ template <typename T, int LANES, int VECS> __device__ __forceinline__ void load_
     }
 }
 
-__device__ __forceinline__ void store_piece(void *p, u32x4 v, bool whole_lines)
-{
-    if (whole_lines) __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
-    else *static_cast<u32x4 *>(p) = v;
-}
-
 // A lane's part of a row of parameters, or `otherwise` where there is none.
 template <typename T, int LANES, int VECS>
 __device__ __forceinline__ void load_parameters(const float *p, int group, int lane, int d, float otherwise, float (&w)[VECS][Piece<T>::kN])
@@ -193,7 +187,7 @@ template <typename T, int LANES, int VECS> __global__ __launch_bounds__((NormWal
             const int f = (walk.lane + i * LANES) * kN;
 #pragma unroll
             for (int e = 0; e < kN; ++e) x[i][e] = __builtin_fmaf(x[i][e] * rstd, w[i][e], b[i][e]);
-            if (f < a.d) store_piece(y + f, Piece<T>::close(x[i]), a.whole_lines);
+            if (f < a.d) store16(y + f, Piece<T>::close(x[i]), a.whole_lines);
         }
         if (a.mean && walk.lane == 0) {
             a.mean[place.stat] = mean;
@@ -268,7 +262,7 @@ template <typename T, int LANES, int VECS, bool PARAMS> __global__ __launch_boun
             Piece<T>::open(vdy[i], g);
 #pragma unroll
             for (int e = 0; e < kN; ++e) x[e] = rstd * (w[i][e] * g[e] - level - (x[e] - mean) * rstd * along);
-            if (f < a.d) store_piece(dx + f, Piece<T>::close(x), a.whole_lines);
+            if (f < a.d) store16(dx + f, Piece<T>::close(x), a.whole_lines);
         }
     }
     if constexpr (PARAMS) {

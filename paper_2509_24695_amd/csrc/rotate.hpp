@@ -2,8 +2,9 @@
 //
 // A copy with four multiplications per pair: bound by memory.  A thread owns 16 bytes of one token's rows (four pairs of bf16, two of fp32),
 // works the token's place out and fetches its angles once, and then runs over the heads, first of q, then of k, whose rows all take the
-// same angles.  32 760 tokens of 20 heads of 112, views of one projection's output: 587 MB in 130 us, 4.5 TB/s; 3 519 tokens of 3 x 16 heads of 128 in
-// fp32 50 us, 6.6 TB/s (61 without the hint at the stores, which heads that share lines do without: 133 with it).
+// same angles.  Sixteen heads at a time (32 760 tokens of 20 heads of 112, views of one projection's output, 587 MB: 122 us, 4.8 TB/s; four at a
+// time 132).  Heads that share no cache lines are written past the caches (3 519 tokens of 3 x 16 heads of 128 in fp32 50 us, 6.6 TB/s, without the
+// hint 61); heads that do, do without (133 with it).
 #pragma once
 
 #include "common.hpp"
@@ -45,16 +46,10 @@ __device__ __forceinline__ u32x4 rotate16(u32x4 v, const f32x2 (&cs)[2], float)
     return v;
 }
 
-__device__ __forceinline__ void store_rotated(void *p, u32x4 v, bool own_lines)
-{
-    if (own_lines) __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
-    else *static_cast<u32x4 *>(p) = v;
-}
-
 template <typename T, int D> __global__ __launch_bounds__(kThreads) void rotate_rows(RotateArgs a)
 {
     using W = RotateShape<T, D>;
-    constexpr int kPairs = W::kVec / 2, kAhead = 4;
+    constexpr int kPairs = W::kVec / 2, kAhead = 16;              // heads whose rows are on their way together
     const int groups = (a.H + a.head_group - 1) / a.head_group, tiles = (a.N + W::kTokens - 1) / W::kTokens;
     const int h0 = (int)(blockIdx.x % groups) * a.head_group, h1 = h0 + a.head_group < a.H ? h0 + a.head_group : a.H;
     const int b = (int)(blockIdx.x / groups / tiles);
@@ -83,15 +78,15 @@ template <typename T, int D> __global__ __launch_bounds__(kThreads) void rotate_
     for (int which = 0; which < a.tensors; ++which) {
         const T *x = static_cast<const T *>(a.x[which]) + b * a.sx.b + n * a.sx.n + col * W::kVec;
         T *y = static_cast<T *>(a.y[which]) + b * a.sy.b + n * a.sy.n + col * W::kVec;
-        int h = h0;
-        for (; h + kAhead <= h1; h += kAhead) {
+        for (int h = h0; h < h1; h += kAhead) {
             u32x4 v[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) v[i] = *reinterpret_cast<const u32x4 *>(x + (h + i) * a.sx.h);
+            for (int i = 0; i < kAhead; ++i)
+                if (h + i < h1) v[i] = *reinterpret_cast<const u32x4 *>(x + (h + i) * a.sx.h);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) store_rotated(y + (h + i) * a.sy.h, rotate16(v[i], cs, T{}), a.own_lines);
+            for (int i = 0; i < kAhead; ++i)
+                if (h + i < h1) store16(y + (h + i) * a.sy.h, rotate16(v[i], cs, T{}), a.own_lines);
         }
-        for (; h < h1; ++h) store_rotated(y + h * a.sy.h, rotate16(*reinterpret_cast<const u32x4 *>(x + h * a.sx.h), cs, T{}), a.own_lines);
     }
 }
 
