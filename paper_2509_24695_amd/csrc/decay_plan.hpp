@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "tile_walk.hpp"
 
 namespace sv {
@@ -16,22 +18,59 @@ struct DecayPlan {
     int chunks, segments, per_segment;
 };
 
-// As many workgroups as run at once, in all `walks` of a launch together: the walk is bound by what a wave waits for (its own products, LDS,
-// the other waves), so a second round or fewer waves cost more than the partial states of shorter segments (32 heads, 4 680 tokens, us with
-// half as many / these / one and a half times: d = 64 41.3 / 37.9 / 45.1, d = 128 74.8 / 71.1 / 81.8; d = 32, 128 heads of 4 096: 56.4 / 45.2 /
-// 49.8; backward, all three walks with the forward call's number each: d = 64 72.7 against 64).  No segment is a single chunk.
+// What a plan takes, in ns.  A chunk is a step that waits mostly for itself (products, LDS, the other waves), so a second workgroup on a compute
+// unit costs `beside` of the first one's time, up to `resident` of them; what is beyond them waits its turn.  More than one segment costs two more
+// launches (6 us), a third of a walk step for each chunk that is not in the last segment (decay_sums; three walks share two such problems), and
+// the state's d x d numbers written, scanned and read again (8 bytes each at 4 TB/s: 2 ns per 1 000).
+struct DecayCost {
+    int step, resident;
+    double beside;
+};
+inline DecayCost decay_cost(int d, bool bf16)
+{
+    if (d <= 32) return {bf16 ? 2200 : 2300, 4, 0.15};
+    if (d <= 64) return {bf16 ? 2450 : 3900, 4, 0.35};
+    return {bf16 ? 3450 : 6450, 2, 0.73};
+}
+
+constexpr int kDecayUnits = 256;            // compute units
+constexpr double kDecayLaunches = 6000, kDecaySumsStep = 0.33, kDecayStateNs = 0.002;
+
+inline double decay_time(const DecayCost &cost, int64_t BH, int segments, int per_segment, int d, int walks)
+{
+    const auto steps = [&](int64_t workgroups) {
+        const int64_t on_a_unit = (workgroups + kDecayUnits - 1) / kDecayUnits;
+        const auto load = [&](int64_t n) { return n ? 1 + cost.beside * (double)(n - 1) : 0; };
+        return (double)per_segment * cost.step * ((double)(on_a_unit / cost.resident) * load(cost.resident) + load(on_a_unit % cost.resident));
+    };
+    const double walk = steps(BH * walks * segments);
+    if (segments == 1) return walk;
+    const int64_t states = BH * (walks > 1 ? 2 : 1);
+    return kDecayLaunches + walk + kDecaySumsStep * steps(states * (segments - 1)) + kDecayStateNs * (double)states * segments * d * d;
+}
+
+// The cut that takes least by decay_time.  Its figures were fitted to the times of 178 calls (both directions and types, d of 32 to 128, 2 to 224
+// heads, 100 to 75 600 tokens) each cut into one to 128 segments: over them it takes 1.7 % longer than the best cut of each, at most 14 %, where
+// "as many workgroups as run at once, segments of two chunks or more" takes 12 %, at most 92 %.  us, in one segment / as many as run at once /
+// this: bf16, d = 128, 224 heads of 2 400 tokens 156 / 184 / 156, 64 heads of 150 16.6 / 27.1 / 16.6, 4 heads of 600 38.6 / 24 / 19.0.
 inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walks)
 {
-    DecayPlan p;
-    p.chunks = (int)(((int64_t)n_tokens + chunk - 1) / chunk);
-    const int64_t workgroups = (d <= 64 ? 1024 : 512) / walks;
-    const int64_t wanted = workgroups / BH < 1 ? 1 : workgroups / BH;
-    int64_t segments = wanted > kMaxDecaySegments ? kMaxDecaySegments : wanted;
-    if (segments > (p.chunks + 1) / 2) segments = (p.chunks + 1) / 2;
-    if (segments < 1) segments = 1;
-    p.per_segment = (int)((p.chunks + segments - 1) / segments);
-    p.segments = (p.chunks + p.per_segment - 1) / p.per_segment;
-    return p;
+    const int chunks = (int)(((int64_t)n_tokens + chunk - 1) / chunk);
+    const DecayCost cost = decay_cost(d, chunk == kDecayChunkBf16);
+    DecayPlan best{chunks, 1, chunks};
+    double least = decay_time(cost, BH, 1, chunks, d, walks);
+    for (int segments : {2, 3, 4, 5, 6, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64, 80, 96, 112, kMaxDecaySegments}) {
+        const int per_segment = (chunks + segments - 1) / segments;
+        if (per_segment == best.per_segment) continue;
+        const int used = (chunks + per_segment - 1) / per_segment;
+        const double time = decay_time(cost, BH, used, per_segment, d, walks);
+        if (time < least) {
+            least = time;
+            best = {chunks, used, per_segment};
+        }
+        if (per_segment == 1) break;
+    }
+    return best;
 }
 
 // The chunks of one sequence of `length` tokens: whole ones at its end, so that every chunk's last row is a token and only the first

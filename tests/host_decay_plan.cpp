@@ -20,15 +20,18 @@ int main()
     const int lengths[] = {1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 1000, 4680, 32760, 75600, 1 << 20, INT_MAX};
     const long long heads[] = {1, 2, 3, 20, 40, 64, 255, 256, 257, 511, 512, 513, 4096, 1 << 24};
     for (int chunk : {32, 64})
-        for (int n : lengths)
-            for (long long BH : heads) {
-                const DecayPlan p = decay_plan(BH, n, 64, chunk, 1);
-                if (p.chunks != (int)(((long long)n + chunk - 1) / chunk)) return fail("chunks", n, BH);
-                if (p.segments < 1 || p.segments > kMaxDecaySegments || p.per_segment < 1) return fail("segments", n, BH);
-                if ((long long)p.segments * p.per_segment < p.chunks) return fail("chunks left over", n, BH);
-                if ((long long)(p.segments - 1) * p.per_segment >= p.chunks) return fail("empty segment", n, BH);
-                if (p.segments > 1 && (long long)p.per_segment * chunk > (1ll << 30) + chunk) return fail("tokens of a segment", n, BH);
-            }
+        for (int d : {32, 64, 112, 128})
+            for (int walks : {1, 3})
+                for (int n : lengths)
+                    for (long long BH : heads) {
+                        const DecayPlan p = decay_plan(BH, n, d, chunk, walks);
+                        if (p.chunks != (int)(((long long)n + chunk - 1) / chunk)) return fail("chunks", n, BH);
+                        if (p.segments < 1 || p.segments > kMaxDecaySegments || p.per_segment < 1) return fail("segments", n, BH);
+                        if ((long long)p.segments * p.per_segment < p.chunks) return fail("chunks left over", n, BH);
+                        if ((long long)(p.segments - 1) * p.per_segment >= p.chunks) return fail("empty segment", n, BH);
+                        if (p.segments > 1 && (long long)p.per_segment * chunk > (1ll << 30) + chunk) return fail("tokens of a segment", n, BH);
+                        if (p.segments > 1 && BH * walks * p.segments > 1 << 20) return fail("workgroups", n, BH);
+                    }
     for (int chunk : {32, 64})
         for (int n : lengths) {
             const DecayWalk w(n, chunk);
