@@ -41,7 +41,8 @@ extern "C" {
 #endif
 
 /* Bytes of device workspace of sv_decay_linattn and of sv_decay_linattn_backward for these sizes (either dtype); contents need
- * no preparation.  Pure host functions; 0 for unsupported arguments. */
+ * no preparation.  What a call needs does for every call with no more batches, heads and tokens and the same d.  Pure host functions; 0 for
+ * unsupported arguments. */
 size_t sv_decay_linattn_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d);
 size_t sv_decay_linattn_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d);
 

@@ -49,8 +49,18 @@ inline double decay_time(const DecayCost &cost, int64_t BH, int segments, int pe
     return kDecayLaunches + walk + kDecaySumsStep * steps(states * (segments - 1)) + kDecayStateNs * (double)states * segments * d * d;
 }
 
+// States that the segments of all heads together begin from: no more than this, where there are fewer heads (eight workgroups of a walk on a compute
+// unit, four at d > 64; twice the figure, or none, gains nothing, half of it costs up to 33 %).  A call with fewer batches, heads or tokens
+// needs no more than one with more.
+inline int64_t decay_slots(int64_t BH, int n_tokens, int d, int walks)
+{
+    const int64_t most = (d <= 64 ? 2048 : 1024) / walks, chunks = ((int64_t)n_tokens + kDecayChunkF32 - 1) / kDecayChunkF32;
+    const int64_t slots = BH * (chunks < kMaxDecaySegments ? chunks : kMaxDecaySegments);
+    return BH >= most ? BH : slots < most ? slots : most;
+}
+
 // The cut that takes least by decay_time.  Its figures were fitted to the times of 178 calls (both directions and types, d of 32 to 128, 2 to 224
-// heads, 100 to 75 600 tokens) each cut into one to 128 segments: over them it takes 1.7 % longer than the best cut of each, at most 14 %, where
+// heads, 100 to 75 600 tokens) each cut into one to 128 segments: over them it takes 1.6 % longer than the best cut of each, at most 13 %, where
 // "as many workgroups as run at once, segments of two chunks or more" takes 12 %, at most 92 %.  us, in one segment / as many as run at once /
 // this: bf16, d = 128, 224 heads of 2 400 tokens 156 / 184 / 156, 64 heads of 150 16.6 / 27.1 / 16.6, 4 heads of 600 38.6 / 24 / 19.0.
 inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walks)
@@ -59,10 +69,12 @@ inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walk
     const DecayCost cost = decay_cost(d, chunk == kDecayChunkBf16);
     DecayPlan best{chunks, 1, chunks};
     double least = decay_time(cost, BH, 1, chunks, d, walks);
+    const int64_t slots = decay_slots(BH, n_tokens, d, walks);
     for (int segments : {2, 3, 4, 5, 6, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64, 80, 96, 112, kMaxDecaySegments}) {
         const int per_segment = (chunks + segments - 1) / segments;
         if (per_segment == best.per_segment) continue;
         const int used = (chunks + per_segment - 1) / per_segment;
+        if (BH * used > slots) break;
         const double time = decay_time(cost, BH, used, per_segment, d, walks);
         if (time < least) {
             least = time;

@@ -46,8 +46,7 @@ DecayPlan plan_of(int64_t BH, int n_tokens, int d, bool bf16, int walks) { retur
 
 size_t slots_bytes(int64_t BH, int n_tokens, int d, int walks)
 {
-    const int a = plan_of(BH, n_tokens, d, true, walks).segments, b = plan_of(BH, n_tokens, d, false, walks).segments;
-    return (size_t)BH * (a > b ? a : b) * d * d * sizeof(float);
+    return (size_t)decay_slots(BH, n_tokens, d, walks) * d * d * sizeof(float);
 }
 
 bool sizes_ok(int32_t B, int32_t H, int32_t N, int32_t d)

@@ -30,7 +30,9 @@ int main()
                         if ((long long)p.segments * p.per_segment < p.chunks) return fail("chunks left over", n, BH);
                         if ((long long)(p.segments - 1) * p.per_segment >= p.chunks) return fail("empty segment", n, BH);
                         if (p.segments > 1 && (long long)p.per_segment * chunk > (1ll << 30) + chunk) return fail("tokens of a segment", n, BH);
-                        if (p.segments > 1 && BH * walks * p.segments > 1 << 20) return fail("workgroups", n, BH);
+                        const long long slots = decay_slots(BH, n, d, walks);
+                        if (BH * p.segments > slots || slots > (BH > 2048 ? BH : 2048)) return fail("slots", n, BH);
+                        if (decay_slots(BH + 1, n, d, walks) < slots || (n < INT_MAX && decay_slots(BH, n + 1, d, walks) < slots)) return fail("slots of a larger call", n, BH);
                     }
     for (int chunk : {32, 64})
         for (int n : lengths) {

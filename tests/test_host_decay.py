@@ -95,6 +95,12 @@ def test_workspace_and_pool():
         dsc = _desc(B=B, H=H, N=N, d=d, stride_b=H * N * d, stride_h=N * d, stride_n=d)
         assert _prompt(qkv=dsc, o=dsc, wb=n - 1, s_in=None, s_out=None) == 6
         assert _backward(qkv=dsc, o=dsc, wb=m - 1, s_in=None, ds_out=None, ds_in=None) == 6
+    for f in (sv.sv_decay_linattn_workspace_bytes, sv.sv_decay_linattn_backward_workspace_bytes):
+        for d in (64, 128):                                                    # what a large call needs does for every smaller one
+            sizes = [f(1, 20, n, d) for n in range(1, 6000, 61)] + [f(1, 20, 1 << 22, d)]
+            assert sizes == sorted(sizes)
+            sizes = [f(b, 3, 1000, d) for b in range(1, 400, 7)] + [f(b, 8, 1000, d) for b in (150, 151)]
+            assert sizes == sorted(sizes)
     for bad in ((0, 2, 128, 64), (1, 0, 128, 64), (1, 2, 0, 64), (1, 2, 128, 48), (1 << 12, 1 << 13, 128, 64)):
         assert sv.sv_decay_linattn_workspace_bytes(*bad) == 0 and sv.sv_decay_linattn_backward_workspace_bytes(*bad) == 0
     assert _token(qkv=_one(N=2, stride_n=128), o=_one(N=2, stride_n=128)) == 2
