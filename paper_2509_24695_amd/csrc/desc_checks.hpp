@@ -31,6 +31,10 @@ template <typename F> void with_head_dim(int d, F &&f)
     }
 }
 
+// A launch's lanes are counted in 32 bits.
+inline bool grid_ok(int64_t workgroups, int threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // `any_width`: rows of any width (the caller checks it), not a head dimension of the attention kernels.  `most_heads`: bound of B*H, by

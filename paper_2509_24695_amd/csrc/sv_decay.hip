@@ -61,6 +61,8 @@ template <typename T, int D> sv_status run_walk(WalkArgs sums, const WalkArgs &w
 {
     using W = WalkShape<T, D>;
     const int64_t BH = (int64_t)walks.B * walks.H;
+    // (the sums are fewer; a scan has D * D / 4 lanes a head and problem, and is there only where heads are few)
+    if (!grid_ok(walks.problems * BH * walks.segments + 64, W::kWalkThreads)) return SV_ERR_SHAPE;
     if (walks.segments > 1) {
         decay_sums<T, D><<<decay_grid(sums.problems * BH * (walks.segments - 1), walks.together), W::kWalkThreads, 0, stream>>>(sums);
         if (launched() != SV_OK) return SV_ERR_LAUNCH;
@@ -118,7 +120,7 @@ extern "C" sv_status sv_decay_linattn(const void *Q, const void *K, const void *
     Shape x, y;
     const sv_status rc = check_pair(qkv, o, &x, &y);
     if (rc != SV_OK) return rc;
-    if (!all_aligned({Q, K, V, O, S_in, S_out, workspace})) return SV_ERR_ALIGN;
+    if (!all_aligned({Q, K, V, O, S_in, S_out, workspace}) || !aligned4(log_decay) || !aligned4(lengths)) return SV_ERR_ALIGN;
     if (!isfinite(scale)) return SV_ERR_RANGE;
     const size_t states = (size_t)x.BH * x.d * x.d * sizeof(float);
     if (O == Q || O == K || O == V || (S_in != S_out && overlaps(S_in, S_out, states))) return SV_ERR_SHAPE;
@@ -137,7 +139,7 @@ extern "C" sv_status sv_decay_linattn_backward(const void *Q, const void *K, con
     Shape x, y;
     const sv_status rc = check_pair(qkv, o, &x, &y);
     if (rc != SV_OK) return rc;
-    if (!all_aligned({Q, K, V, dO, S_in, dS_out, dQ, dK, dV, dS_in, workspace})) return SV_ERR_ALIGN;
+    if (!all_aligned({Q, K, V, dO, S_in, dS_out, dQ, dK, dV, dS_in, workspace}) || !aligned4(log_decay) || !aligned4(lengths)) return SV_ERR_ALIGN;
     if (!isfinite(scale)) return SV_ERR_RANGE;
     const size_t states = (size_t)x.BH * x.d * x.d * sizeof(float);
     for (const void *out : {dQ, dK, dV})
@@ -165,10 +167,11 @@ extern "C" sv_status sv_decay_linattn_token(const void *Q, const void *K, const 
     const sv_status rc = check_pair(qkv, o, &x, &y);
     if (rc != SV_OK) return rc;
     if (x.N != 1 || n_slots <= 0 || (!slots && n_slots < x.B)) return SV_ERR_SHAPE;
-    if (!all_aligned({Q, K, V, O, S_in, S_out})) return SV_ERR_ALIGN;
+    if (!all_aligned({Q, K, V, O, S_in, S_out}) || !aligned4(log_decay) || !aligned4(slots)) return SV_ERR_ALIGN;
     if (!isfinite(scale)) return SV_ERR_RANGE;
     const size_t states = (size_t)n_slots * x.H * x.d * x.d * sizeof(float);
     if (O == Q || O == K || O == V || (S_in != S_out && overlaps(S_in, S_out, states))) return SV_ERR_SHAPE;
+    if (!grid_ok(x.BH, 256)) return SV_ERR_SHAPE;
     TokenArgs a{Q, K, V, O, x.st.b, x.st.h, y.st.b, y.st.h, log_decay, slots, n_slots, x.B, x.H, scale, S_in, S_out};
     const auto hs = static_cast<hipStream_t>(stream);
     with_head_dim(x.d, [&](auto D) {

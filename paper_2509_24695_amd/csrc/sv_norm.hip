@@ -100,6 +100,7 @@ extern "C" sv_status sv_layernorm(const void *X, const sv_tensor_desc *x, const 
     const NormForm form = norm_form(in.d * in.elem_bytes / 16, false);
     a.whole_lines = lines_whole(out);
     a.workgroups = norm_workgroups(form, a.rows, a.groups, kNormForwardWgs);
+    if (!grid_ok((int64_t)a.groups * a.workgroups, norm_threads(form))) return SV_ERR_SHAPE;
     const unsigned grid = (unsigned)((int64_t)a.groups * a.workgroups);
     const auto hs = static_cast<hipStream_t>(stream);
     with_form(form, [&](auto lanes, auto vecs) {
@@ -148,6 +149,8 @@ extern "C" sv_status sv_layernorm_backward(const void *X, const sv_tensor_desc *
     a.workgroups = norm_workgroups(form, a.rows, a.groups, norm_backward_wgs(in.d));
     if (params && workspace_bytes < partial_bytes(a.groups, a.workgroups, in.d)) return SV_ERR_WORKSPACE;
     a.partial = static_cast<float *>(workspace);
+    const int64_t tiles = (in.d / 4 * 2 + 15) / 16;
+    if (!grid_ok((int64_t)a.groups * a.workgroups, norm_threads(form)) || (params && !grid_ok(a.groups * tiles, 256))) return SV_ERR_SHAPE;
     const unsigned grid = (unsigned)((int64_t)a.groups * a.workgroups);
     const auto hs = static_cast<hipStream_t>(stream);
     with_form(form, [&](auto lanes, auto vecs) {
@@ -166,7 +169,6 @@ extern "C" sv_status sv_layernorm_backward(const void *X, const sv_tensor_desc *
     });
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
     if (params) {
-        const int64_t tiles = (in.d / 4 * 2 + 15) / 16;
         norm_fold<<<(unsigned)(a.groups * tiles), 256, 0, hs>>>(a);
         return launched();
     }

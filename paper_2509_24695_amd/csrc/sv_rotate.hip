@@ -33,7 +33,7 @@ extern "C" sv_status sv_rope3d_rotate(const void *Q, const void *K, const sv_ten
     if (!positions && ((int64_t)rope->frames * rope->rows > in.N || (int64_t)rope->frames * rope->rows * rope->cols != in.N)) return SV_ERR_SHAPE;
     if ((rope->n_t && !rope->cs_t) || (rope->n_h && !rope->cs_h) || (rope->n_w && !rope->cs_w)) return SV_ERR_NULL;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(YQ) || !aligned16(YK)) return SV_ERR_ALIGN;
-    if (!aligned8(rope->cs_t) || !aligned8(rope->cs_h) || !aligned8(rope->cs_w) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return SV_ERR_ALIGN;
+    if (!aligned8(rope->cs_t) || !aligned8(rope->cs_h) || !aligned8(rope->cs_w) || !aligned4(positions)) return SV_ERR_ALIGN;
     if (((YQ == Q || (K && YK == K)) && !same_rows(in, out)) || YQ == K || YK == Q || YQ == YK) return SV_ERR_SHAPE;
 
     RotateArgs a{};
@@ -58,7 +58,7 @@ extern "C" sv_status sv_rope3d_rotate(const void *Q, const void *K, const sv_ten
             while (group > 1 && tiles * in.B * ((in.H + group - 1) / group) < 2048) group = (group + 1) / 2;
             a.head_group = group;
             const int64_t wgs = tiles * in.B * ((in.H + group - 1) / group);
-            if (wgs >= (int64_t)1 << 31) rc = SV_ERR_SHAPE;
+            if (!grid_ok(wgs, kThreads)) rc = SV_ERR_SHAPE;
             else rotate_rows<decltype(t), D()><<<(unsigned)wgs, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
         };
         if (in.bf16) go(uint16_t{});

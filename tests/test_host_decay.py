@@ -66,6 +66,20 @@ def test_descriptors(call, base):
         assert call(scale=scale) == 5
 
 
+@pytest.mark.parametrize("call,name", [(_prompt, "g"), (_prompt, "lengths"), (_backward, "g"), (_backward, "lengths"), (_token, "g"), (_token, "slots")])
+def test_alignment_of_numbers(call, name):
+    assert call(**{name: A[15] + 2}) == 4
+
+
+def test_lanes_of_a_launch():
+    """A launch has fewer than 2^32 lanes; larger calls are refused."""
+    many = dict(B=1 << 12, H=1 << 12, N=1, d=128, stride_b=(1 << 12) * 128, stride_h=128, stride_n=128)
+    assert _token(qkv=_desc(**many), o=_desc(**many)) == 2
+    assert _prompt(qkv=_desc(**many), o=_desc(**many), s_in=None, s_out=None) == 2
+    many.update(B=1 << 11)
+    assert _backward(qkv=_desc(**many), o=_desc(**many), s_in=None, ds_out=None, ds_in=None) == 2
+
+
 def test_far_rows():
     """64 rows span less than 2 GiB, or the call is refused: in-chunk offsets are 32-bit."""
     far = (1 << 31) // (64 * 2)

@@ -54,6 +54,18 @@ def test_rotate_refusals():
     assert _rotate(YQ=A[1]) == 2 and _rotate(YK=A[0]) == 2 and _rotate(YQ=A[3]) == 2
 
 
+def test_lanes_of_a_launch():
+    """A launch has fewer than 2^32 lanes; larger calls are refused."""
+    n = 1 << 28                                                       # 16 tokens a workgroup of 256
+    long = _desc(H=1, N=n, d=128, stride_n=128, stride_h=n * 128, stride_b=n * 128)
+    assert _rotate(x=long, y=long, rope=_rope(frames=1 << 8, rows=1 << 10, cols=1 << 10, n_t=24, n_h=20, n_w=20)) == 2
+    heads = _desc(H=1 << 24, N=1, d=8, stride_n=8, stride_h=8, stride_b=8 << 24)
+    assert _norm(x=heads, y=heads, heads=1 << 24) == 2
+    assert _norm_backward(x=heads, dy=heads, dx=heads, heads=1 << 24) == 2
+    wide = _desc(H=1 << 16, N=1, d=8192, stride_n=8192, stride_h=8192, stride_b=8192 << 16)     # 256 workgroups a head add the partial sums up
+    assert _norm_backward(x=wide, dy=wide, dx=wide, heads=1 << 16) == 2
+
+
 def _norm(x=None, y=None, heads=1, eps=1e-5, **at):
     p = dict(X=A[0], w=A[1], b=A[2], Y=A[3], mean=A[4], rstd=A[5])
     p.update(at)
