@@ -19,15 +19,29 @@
 // weight in the new state l^{C-r} where it is l^{C-1-r} (`back`).
 //
 // One workgroup walks one segment of one head's sequence, a wave per 32 value features: the wave keeps its 32 columns of S as fp32
-// accumulators over the whole segment, works out all of the chunk's C x C products for itself (C = 64, d = 128: 24 of its 94
-// matrix instructions) and so meets the other waves only where a chunk's tokens are handed over through LDS.  Products are arranged so
-// that a product's accumulators are the next one's operands as they lie: the lane of a 32 x 32 accumulator holds rows 8 (r / 4) + 4 h + r % 4
-// of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to the first
-// operand of a product in the order decay_row, which makes eight accumulators in a row eight consecutive indices.
+// accumulators over the whole segment.  The chunk's C x C products are the same for all of the workgroup's waves: at bf16 and four waves each
+// wave works one of the three 32 x 32 tiles out for all (32 760 tokens of 20 heads of 112 228 us, every wave for itself, 24 of its 94 matrix
+// instructions, 243; 7 x 8 heads of up to 1 501 tokens of 128 46 and 51), at fp32 each adds up a part of the features (4 680 tokens of 32 heads
+// of 64 73.6 us, every wave for itself 76.5; 8 000 tokens of 20 heads of 112 176 and 195), at bf16 with fewer waves every wave has its own
+// (4 680 tokens of 32 heads of 64, backward: 60 us, shared 72).
+//
+// Products are arranged so that a product's accumulators are the next one's operands as they lie: the lane of a 32 x 32 accumulator holds rows
+// 8 (r / 4) + 4 h + r % 4 of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to
+// the first operand of a product in the order decay_row, which makes eight accumulators in a row eight consecutive indices.
 //
 // Roundings (bf16 tokens): S enters o as two bf16 pieces (together within 2^-16), the weighted values l^{..} v_j enter S as two pieces, so
-// that the state stays an fp32 one; the weighted scores l^{i-j} (q_i . k_j) are rounded to bf16 once, like the output (both 2^-8 of
+// that the state stays an fp32 one (2.4e-6 off after 32 760 tokens; with one piece the call is 3 to 8 % faster and the output 2.4e-3 off
+// instead of 1.8e-3); the weighted scores l^{i-j} (q_i . k_j) are rounded to bf16 once, like the output (both 2^-8 of
 // a term at most).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix instructions).
+//
+// A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and
+// v twice: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.7 that do) 700 us = 215 + 8 + 470, 5.3 TB/s, which is more
+// than a copy of that size reaches (4.9): bound by memory.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
+// take 228 us = 68 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
+// memory accesses 114.  Calls that give each compute unit one or two workgroups are bound by a chunk's own run through LDS and the
+// matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
+// Measured and left: two chunks' rows on their way in decay_sums (the same, +-2 %) or in the walk (one workgroup less on a compute unit: 289 us
+// instead of 252); heads in groups whose k and v fit the memory side's cache, one group after the other (702 us instead of 718).
 #pragma once
 
 #include "common.hpp"
@@ -474,7 +488,8 @@ template <typename T, int D> __global__ __launch_bounds__((WalkShape<T, D>::kWal
     else segment_sum<T, D, false>(a, p, task, lds);
 }
 
-// Slot s of each head: from what segment s - 1 adds to the state before segment s, over all segments.  A thread per four elements.
+// Slot s of each head: from what segment s - 1 adds to the state before segment s, over all segments.  A thread per four elements, eight segments
+// on their way (10 us for 24 MB of states; sixteen, or threads of two elements, the same).
 template <typename T, int D> __global__ __launch_bounds__(256) void decay_scan(WalkArgs a)
 {
     using W = WalkShape<T, D>;
