@@ -25,8 +25,9 @@
  *  - lengths is int32 [B] or NULL: sequence b has the tokens [0, lengths[b]) of its row (values are held to [0, N]); NULL: N each.
  *    Rows behind a sequence's last token are neither read nor written, whatever they hold.  A sequence of length zero has
  *    S_out = S_in.
- *  - SV_BF16: bf16 products with fp32 accumulation; what enters the state and what comes out of it goes through pairs of bf16 values
- *    (2^-16 of a term: an fp32 state to about 3e-6), weighted scores and outputs are rounded to bf16 once.  SV_F32: fp32 products.
+ *  - SV_BF16: bf16 products with fp32 accumulation; S_out and dS_in are fp32 states (what enters them goes through three bf16 values, 2^-24 of
+ *    a term), what comes out of a state on its way to O, dQ, dK and dV goes through pairs of them (2^-16 of a term), weighted scores
+ *    and outputs are rounded to bf16 once.  SV_F32: fp32 products.
  *  - Tokens of a sequence, states and log decays must be finite numbers (minus infinity apart): a NaN or infinity also reaches outputs of
  *    up to 63 tokens before it.
  *  - Outputs must not overlap inputs or each other, but for S_out = S_in where that is said.

@@ -29,15 +29,15 @@
 // 8 (r / 4) + 4 h + r % 4 of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to
 // the first operand of a product in the order decay_row, which makes eight accumulators in a row eight consecutive indices.
 //
-// Roundings (bf16 tokens): S enters o as two bf16 pieces (together within 2^-16), the weighted values l^{..} v_j enter S as two pieces, so
-// that the state stays an fp32 one (2.4e-6 off after 32 760 tokens; with one piece the call is 3 to 8 % faster and the output 2.4e-3 off
-// instead of 1.8e-3); the weighted scores l^{i-j} (q_i . k_j) are rounded to bf16 once, like the output (both 2^-8 of
-// a term at most).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix instructions).
+// Roundings (bf16 tokens): S enters o, and the weighted values l^{..} v_j enter S, as two bf16 pieces (together within 2^-16; with one the call is 3
+// to 8 % faster and the output 2.4e-3 off instead of 1.8e-3).  A state that the caller gets is an fp32 one: what goes into it, in the sums and in
+// the last segment's walk, is in three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; 246 us and 233).  The weighted scores l^{i-j}
+// (q_i . k_j) are rounded to bf16 once, like the output (both 2^-8 of a term at most).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix instructions).
 //
 // A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and
-// v twice: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.7 that do) 700 us = 215 + 8 + 470, 5.3 TB/s, which is more
+// v twice: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.7 that do) 711 us = 216 + 8 + 487, 5.2 TB/s, which is more
 // than a copy of that size reaches (4.9): bound by memory.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
-// take 228 us = 68 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
+// take 246 us = 80 + 10 + 154: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
 // memory accesses 114.  Calls that give each compute unit one or two workgroups are bound by a chunk's own run through LDS and the
 // matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
 // Measured and left: two chunks' rows on their way in decay_sums (the same, +-2 %) or in the walk (one workgroup less on a compute unit: 289 us
@@ -68,6 +68,7 @@ struct WalkProblem {
     float weight_update;       //   and of what goes into the state
     int back;                  // 1: tokens from the last to the first, G's weights
     int turned;                // 1: s_begin and slots hold the transpose of this walk's state
+    int kept;                  // 1: the state behind the walk is one that a caller may ask for (asked or not: outputs do not depend on it)
 };
 
 struct WalkArgs {
@@ -139,6 +140,18 @@ template <> struct Pieces<uint16_t> {
     __device__ __forceinline__ f32x16 second(const Oct<uint16_t> &b, f32x16 c) const { return oct_product(lo, b, c); }
     __device__ __forceinline__ f32x16 first_right(const Oct<uint16_t> &a, f32x16 c) const { return oct_product(a, hi, c); }
     __device__ __forceinline__ f32x16 second_right(const Oct<uint16_t> &a, f32x16 c) const { return oct_product(a, lo, c); }
+};
+
+// What two pieces leave of the values, as a third.
+struct Rest : Oct<uint16_t> {
+    __device__ __forceinline__ Rest(const float (&x)[8], const Pieces<uint16_t> &p)
+    {
+        const u32x4 h = __builtin_bit_cast(u32x4, p.hi.v), l = __builtin_bit_cast(u32x4, p.lo.v);
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2((x[2 * i] - bf16_lo(h[i])) - bf16_lo(l[i]), (x[2 * i + 1] - bf16_hi(h[i])) - bf16_hi(l[i]));
+        v = __builtin_bit_cast(bf16x8, w);
+    }
 };
 
 // Sizes of the walk for element type T and head dimension D (112 is computed as 128: missing features are zeros in LDS).
@@ -398,10 +411,10 @@ template <int SUBS> struct UpdateWeights {
     }
 };
 
-// S += sum over one sub-chunk of 16 tokens, weighted.  `values` is the wave's 32 value features of these tokens.
+// S += sum over one sub-chunk of 16 tokens, weighted.  `values` is the wave's 32 value features of these tokens; `kept`: for a state that is kept.
 template <typename T, int D>
 __device__ __forceinline__ void state_update(StatePanel<D> &S, const unsigned char *tileK, const Oct<T> &values, const UpdateWeights<WalkShape<T, D>::kTokSubs> &w,
-                                             int sub, int lane)
+                                             int sub, int lane, bool kept)
 {
     using W = WalkShape<T, D>;
     float x[8];
@@ -409,13 +422,19 @@ __device__ __forceinline__ void state_update(StatePanel<D> &S, const unsigned ch
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= w.w[sub][e];
     const Pieces<T> v(x);
+    Oct<T> k[StatePanel<D>::kKeyTiles];
 #pragma unroll
     for (int kt = 0; kt < StatePanel<D>::kKeyTiles; ++kt) {
-        Oct<T> k;
-        token_operand<W, true>(tileK, 16 * sub, 32 * kt, lane, k);
-        S.s[kt] = v.first_right(k, S.s[kt]);
-        S.s[kt] = v.second_right(k, S.s[kt]);
+        token_operand<W, true>(tileK, 16 * sub, 32 * kt, lane, k[kt]);
+        S.s[kt] = v.first_right(k[kt], S.s[kt]);
+        S.s[kt] = v.second_right(k[kt], S.s[kt]);
     }
+    if constexpr (sizeof(T) == 2)
+        if (kept) {
+            const Rest rest(x, v);
+#pragma unroll
+            for (int kt = 0; kt < StatePanel<D>::kKeyTiles; ++kt) S.s[kt] = oct_product(k[kt], rest, S.s[kt]);
+        }
 }
 
 // ---- kernels -----------------------------------------------------------------------------------------------------------
@@ -472,7 +491,7 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
             Oct<T> v;
             token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
-            state_update<T, D>(S, tileK, v, uw, sub, lane);
+            state_update<T, D>(S, tileK, v, uw, sub, lane, p.kept != 0);
         }
     }
     S.store(p.slots + ((int64_t)task.bh * a.segments + task.segment + 1) * D * D, panel, lane);
@@ -564,7 +583,7 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
     StatePanel<D> S;
     if (begin) S.load(begin, p.turned, panel, own_lane);
     else S.clear();
-    const bool keep = last && p.s_end;                               // this workgroup's state is the sequence's last
+    const bool keep = last && p.s_end, fine = last && p.kept;        // this workgroup's state is the sequence's last
 
     const float g = a.log_decay[h];
     const DecayPower pw(g);
@@ -729,7 +748,7 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
             auto weights = [&](int t, int s) __attribute__((always_inline)) { return W::kShared ? scores[(2 * t + s) * 64 + lane] : own[W::kShared ? 0 : t][s]; };
             if (sub < 2) acc[0] = oct_product(v, weights(0, sub), acc[0]);
             if constexpr (W::kTiles == 2) acc[1] = oct_product(v, weights(1 + sub / 2, sub % 2), acc[1]);
-            state_update<T, D>(S, tileK, v, uw, sub, lane);
+            state_update<T, D>(S, tileK, v, uw, sub, lane, fine);
         }
         // the output's rows, for whole-row stores once all panels are in
 #pragma unroll

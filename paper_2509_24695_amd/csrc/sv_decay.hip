@@ -131,7 +131,7 @@ extern "C" sv_status sv_decay_linattn(const void *Q, const void *K, const void *
     if (O == Q || O == K || O == V || (S_in != S_out && overlaps(S_in, S_out, states))) return SV_ERR_SHAPE;
     if (workspace_bytes < slots_bytes(x.BH, x.N, x.d, 1)) return SV_ERR_WORKSPACE;
     WalkArgs a = walk_args(x, log_decay, lengths, plan_of(x.BH, x.N, x.d, x.bf16, 1), 1);
-    a.p[0] = WalkProblem{Q, K, V, O, x.st, x.st, x.st, y.st, S_in, S_out, static_cast<float *>(workspace), scale, scale, 1.f, 0, 0};
+    a.p[0] = WalkProblem{Q, K, V, O, x.st, x.st, x.st, y.st, S_in, S_out, static_cast<float *>(workspace), scale, scale, 1.f, 0, 0, 1};
     return run_walk(x.bf16, x.d, a, a, stream);
 }
 
@@ -155,11 +155,11 @@ extern "C" sv_status sv_decay_linattn_backward(const void *Q, const void *K, con
     float *states_fwd = static_cast<float *>(workspace), *states_back = states_fwd + half / sizeof(float);
     const DecayPlan plan = plan_of(x.BH, x.N, x.d, x.bf16, kBackwardWalks);
     WalkArgs sums = walk_args(x, log_decay, lengths, plan, 2), walks = walk_args(x, log_decay, lengths, plan, kBackwardWalks);
-    sums.p[0] = WalkProblem{nullptr, K, V, nullptr, x.st, x.st, x.st, y.st, S_in, nullptr, states_fwd, 0.f, 0.f, 1.f, 0, 0};
-    sums.p[1] = WalkProblem{nullptr, Q, dO, nullptr, x.st, x.st, y.st, y.st, dS_out, nullptr, states_back, 0.f, 0.f, scale, 1, 0};
-    walks.p[0] = WalkProblem{dO, V, K, dQ, y.st, x.st, x.st, x.st, S_in, nullptr, states_fwd, scale, scale, 1.f, 0, 1};
-    walks.p[1] = WalkProblem{K, Q, dO, dV, x.st, x.st, y.st, x.st, dS_out, dS_in, states_back, 1.f, scale, scale, 1, 0};
-    walks.p[2] = WalkProblem{V, dO, Q, dK, x.st, y.st, x.st, x.st, dS_out, nullptr, states_back, 1.f, scale, scale, 1, 1};
+    sums.p[0] = WalkProblem{nullptr, K, V, nullptr, x.st, x.st, x.st, y.st, S_in, nullptr, states_fwd, 0.f, 0.f, 1.f, 0, 0, 0};
+    sums.p[1] = WalkProblem{nullptr, Q, dO, nullptr, x.st, x.st, y.st, y.st, dS_out, nullptr, states_back, 0.f, 0.f, scale, 1, 0, 1};
+    walks.p[0] = WalkProblem{dO, V, K, dQ, y.st, x.st, x.st, x.st, S_in, nullptr, states_fwd, scale, scale, 1.f, 0, 1, 0};
+    walks.p[1] = WalkProblem{K, Q, dO, dV, x.st, x.st, y.st, x.st, dS_out, dS_in, states_back, 1.f, scale, scale, 1, 0, 1};
+    walks.p[2] = WalkProblem{V, dO, Q, dK, x.st, y.st, x.st, x.st, dS_out, nullptr, states_back, 1.f, scale, scale, 1, 1, 0};
     return run_walk(x.bf16, x.d, sums, walks, stream);
 }
 
