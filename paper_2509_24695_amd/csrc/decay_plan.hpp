@@ -61,8 +61,8 @@ inline int64_t decay_slots(int64_t BH, int n_tokens, int d, int walks)
 
 // The cut that takes least by decay_time.  Its figures were fitted to the times of 178 calls (both directions and types, d of 32 to 128, 2 to 224
 // heads, 100 to 75 600 tokens) each cut into one to 128 segments: over them it takes 1.6 % longer than the best cut of each, at most 13 %, where
-// "as many workgroups as run at once, segments of two chunks or more" takes 12 %, at most 92 %.  us, in one segment / as many as run at once /
-// this: bf16, d = 128, 224 heads of 2 400 tokens 156 / 184 / 156, 64 heads of 150 16.6 / 27.1 / 16.6, 4 heads of 600 38.6 / 24 / 19.0.
+// "as many workgroups as run at once, segments of two chunks or more" takes 12 %, at most 87 %.  us, in one segment / as many as run at once /
+// this: bf16, d = 128, 224 heads of 2 400 tokens 170 / 190 / 170, 64 heads of 150 17.9 / 28.8 / 17.9, 4 heads of 600 42.7 / 23.6 / 20.3.
 inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walks)
 {
     const int chunks = (int)(((int64_t)n_tokens + chunk - 1) / chunk);
