@@ -285,20 +285,27 @@ template <typename T, int D, bool BACK> struct ChunkRows {
         row0 = threadIdx.x / W::kRowVecs;
         off0 = c * W::kVec < D ? (uint32_t)row0 * (uint32_t)row_bytes + (uint32_t)c * 16u : kNoRow;
     }
-    // rows that are no tokens (the lead of the first chunk; all of them unless `live`) read as zeros
-    template <bool NT = false> __device__ __forceinline__ void load(int64_t c, bool live, int chunks, int lead, u32x4 (&reg)[W::kSteps]) const
+    // Rows that are no tokens (the lead of the first chunk; all of them unless `live`) read as zeros.  BEGIN: chunk c may be the first.  (Left to the
+    // comparison c == 0 the compiler finds out by an addition with carry whether c + 1 is zero, the resource is no longer a scalar one for
+    // it, and each load gets a loop of its own over the resources of the lanes.)
+    template <bool NT, bool BEGIN> __device__ __forceinline__ void load(int64_t c, bool live, int chunks, int lead, u32x4 (&reg)[W::kSteps]) const
     {
         const int64_t base = BACK ? (int64_t)(chunks - 1 - c) * W::kChunk : c * W::kChunk - lead;
         const rsrc_t r = make_rsrc(head + base * row_bytes, live ? (uint32_t)((W::kChunk - 1) * row_bytes + D * (int)sizeof(T)) : 0u);
-        const int nothing = c == 0 ? lead : 0;                         // rows in front of the first token
         // the steps' offsets are worked out anew for every chunk: kept over the loop they are twelve registers too many
         uint32_t off = off0;
         asm volatile("" : "+v"(off));
+        constexpr int kStep = W::kRowsPerStep;
+        if constexpr (BEGIN) {
+            const int nothing = c == 0 ? lead : 0;                     // rows in front of the first token
 #pragma unroll
-        for (int i = 0; i < W::kSteps; ++i) {
-            constexpr int kStep = W::kRowsPerStep;
-            const bool is = BACK ? row0 < W::kChunk - nothing - i * kStep : row0 >= nothing - i * kStep;
-            reg[i] = load_stream16<NT>(r, is ? off + (uint32_t)(i * kStep) * (uint32_t)row_bytes : kNoRow);
+            for (int i = 0; i < W::kSteps; ++i) {
+                const bool is = BACK ? row0 < W::kChunk - nothing - i * kStep : row0 >= nothing - i * kStep;
+                reg[i] = load_stream16<NT>(r, is ? off + (uint32_t)(i * kStep) * (uint32_t)row_bytes : kNoRow);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W::kSteps; ++i) reg[i] = load_stream16<NT>(r, off + (uint32_t)(i * kStep) * (uint32_t)row_bytes);
         }
     }
     __device__ __forceinline__ void put(unsigned char *tile, const u32x4 (&reg)[W::kSteps]) const
@@ -456,7 +463,7 @@ struct WalkTask {
 __device__ __forceinline__ int walk_length(const WalkArgs &a, int b)
 {
     if (!a.lengths) return a.N;
-    const int n = a.lengths[b];
+    const int n = __builtin_amdgcn_readfirstlane(a.lengths[b]);
     return n < 0 ? 0 : n > a.N ? a.N : n;
 }
 
@@ -475,8 +482,8 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
     const ChunkDecay decay(W::kChunk, g);
     const ChunkRows<T, D, BACK> rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
     u32x4 nk[W::kSteps], nv[W::kSteps];
-    rk.template load<false>(c0, true, walk.chunks, walk.lead, nk);
-    rv.template load<false>(c0, true, walk.chunks, walk.lead, nv);
+    rk.template load<false, true>(c0, true, walk.chunks, walk.lead, nk);
+    rv.template load<false, true>(c0, true, walk.chunks, walk.lead, nv);
     StatePanel<D> S;
     S.clear();
     for (int c = c0; c < c1; ++c) {
@@ -484,8 +491,8 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
         rk.put(tileK, nk);
         rv.put(tileV, nv);
         lds_barrier();
-        rk.template load<false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
-        rv.template load<false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
+        rk.template load<false, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
+        rv.template load<false, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
         S.scale(decay(c));
 #pragma unroll
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
@@ -602,9 +609,9 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
 
     const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h), ro(p.o, p.so, b, h);
     u32x4 nq[W::kSteps], nk[W::kSteps], nv[W::kSteps];
-    rq.template load<NT>(c0, c0 < c1, walk.chunks, walk.lead, nq);
-    rk.template load<NT>(c0, c0 < c1, walk.chunks, walk.lead, nk);
-    rv.template load<NT>(c0, c0 < c1, walk.chunks, walk.lead, nv);
+    rq.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nq);
+    rk.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nk);
+    rv.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nv);
 
     for (int c = c0; c < c1; ++c) {
         lds_barrier();
@@ -613,9 +620,9 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
         rk.put(tileK, nk);
         rv.put(tileV, nv);
         lds_barrier();
-        rq.template load<NT>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nq);
-        rk.template load<NT>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
-        rv.template load<NT>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
+        rq.template load<NT, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nq);
+        rk.template load<NT, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
+        rv.template load<NT, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
         // addresses are worked out anew for every chunk: kept over the loop they take the registers that the products need
         int lane = own_lane;
         asm volatile("" : "+v"(lane));
