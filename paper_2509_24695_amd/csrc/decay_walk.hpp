@@ -29,19 +29,22 @@
 // 8 (r / 4) + 4 h + r % 4 of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to
 // the first operand of a product in the order decay_row, which makes eight accumulators in a row eight consecutive indices.
 //
-// Roundings (bf16 tokens): S enters o, and the weighted values l^{..} v_j enter S, as two bf16 pieces (together within 2^-16; with one the call is 3
-// to 8 % faster and the output 2.4e-3 off instead of 1.8e-3).  A state that the caller gets is an fp32 one: what goes into it, in the sums and in
-// the last segment's walk, is in three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; 246 us and 233).  The weighted scores l^{i-j}
-// (q_i . k_j) are rounded to bf16 once, like the output (both 2^-8 of a term at most).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix instructions).
+// Roundings (bf16 tokens): S enters o, and the weighted values l^{..} v_j enter S, as two bf16 pieces (together within 2^-16; with one the call is
+// 3 to 8 % faster and the output 2.4e-3 off instead of 1.8e-3).  A state that the caller gets is an fp32 one: what goes into it, in the sums and in
+// the last segment's walk, is in three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; 246 us and 233).  The weighted scores l^{i-j} (q_i
+// . k_j) are rounded to bf16 once (score_pieces has the exception), like the output (both 2^-8 of a term at most).  fp32 tokens: fp32 products
+// throughout (32 x 32 x 2 matrix instructions).
 //
 // A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and
-// v twice: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.7 that do) 711 us = 216 + 8 + 487, 5.2 TB/s, which is more
+// v twice: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.7 that do) 704 us = 216 + 8 + 480, 5.3 TB/s, which is more
 // than a copy of that size reaches (4.9): bound by memory.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
-// take 246 us = 80 + 10 + 154: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
+// take 242 us = 80 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
 // memory accesses 114.  Calls that give each compute unit one or two workgroups are bound by a chunk's own run through LDS and the
 // matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
-// Measured and left: two chunks' rows on their way in decay_sums (the same, +-2 %) or in the walk (one workgroup less on a compute unit: 289 us
-// instead of 252); heads in groups whose k and v fit the memory side's cache, one group after the other (702 us instead of 718).
+// Measured and left: LDS rows whose 16-byte pieces change places, so that no read conflicts (of decay_sums' LDS cycles at d = 112 62 % are
+// conflicts, the walk's 39 %): 1 to 3 % slower by the addresses' arithmetic, as LDS is busy for a sixth of the time; two chunks' rows on their way
+// in decay_sums (the same, +-2 %) or in the walk (one workgroup less on a compute unit: 289 us instead of 252); heads in groups whose k and v fit
+// the memory side's cache, one group after the other (702 us instead of 718).
 #pragma once
 
 #include "common.hpp"
@@ -169,6 +172,15 @@ template <typename T, int D> struct WalkShape {
     // who works the scores out: tile by tile for each other (kShared), each a part of the features (kSplit), or every wave for itself
     static constexpr bool kShared = sizeof(T) == 2 && kPanels == 4, kSplit = sizeof(T) == 4 && kPanels > 1;
     static constexpr int kOwnTiles = kShared ? 1 : kScoreTiles, kScoreBytes = kShared ? kScoreTiles * 2 * 64 * 8 * (int)sizeof(T) : 0;
+    // The weighted scores are one bf16 value each, but two where no sequence is longer than a chunk: a few tokens then come out as exactly as they do
+    // one by one, which costs nothing in a call that is mostly its launch (8 heads
+    // of 64 or 128, 1 to 64 tokens: 8 to 9 us either way) and little in a large one (us with two / one: 2 000 heads of 64, one token 23.0 / 21.9, 64
+    // tokens 27.7 / 27.2; of 128, 64 tokens 79.9 / 79.6).  Outputs are then 1.66e-3 off instead of 2.3e-3 (root of the mean square).
+    static constexpr int score_pieces(bool is_short) { return is_short && sizeof(T) == 2 ? 2 : 1; }
+    // Tiles in LDS: queries, keys, values and outputs.  With shared scores the waves meet after their last look at the queries, so that the outputs of
+    // a walk of one chunk take their place, and the second pieces of the scores do not cost the compute unit its second workgroup (2 000
+    // heads of 128, one token: 55 us, with a tile of their own 83).
+    static constexpr int tiles(bool is_short) { return is_short && kShared ? 3 : 4; }
     static_assert(kSteps * kRowsPerStep == kChunk && D % 16 == 0, "whole rows");
 };
 
@@ -571,12 +583,14 @@ template <typename W> __device__ __forceinline__ void put_features(unsigned char
     for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(row + (8 * x + 4 * half) * 4) = f32x4{acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]};
 }
 
-template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
+template <typename T, int D, bool BACK, bool NT, bool SHORT> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
 {
     using W = WalkShape<T, D>;
-    unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes, *tileO = lds + 3 * W::kTileBytes;
-    Oct<T> *scores = reinterpret_cast<Oct<T> *>(lds + 4 * W::kTileBytes);
-    float *table = reinterpret_cast<float *>(lds + 4 * W::kTileBytes + W::kScoreBytes), *from_state = table + 96;
+    unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes;
+    unsigned char *tileO = W::tiles(SHORT) == 4 ? lds + 3 * W::kTileBytes : tileQ, *behind = lds + W::tiles(SHORT) * W::kTileBytes;
+    Oct<T> *scores = reinterpret_cast<Oct<T> *>(behind);
+    constexpr int kPieces = W::score_pieces(SHORT);
+    float *table = reinterpret_cast<float *>(behind + kPieces * W::kScoreBytes), *from_state = table + 96;
     const int b = task.bh / a.H, h = task.bh % a.H, own_lane = threadIdx.x & 63, panel = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const DecayWalk walk(walk_length(a, b), W::kChunk);
     const int c0 = task.segment * a.per_segment;
@@ -632,14 +646,20 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
         // tokens) from the state.  SHARED: each tile of the scores is one wave's work (another one's with every chunk) for all waves, through LDS,
         // in one run over the features with the products of the state; otherwise every wave has its own, worked out before.
         f32x16 acc[W::kTiles];
-        Oct<T> own[W::kOwnTiles][2];
-        auto weigh = [&](const f32x16 &p, const float *near, Oct<T> (&o)[2]) __attribute__((always_inline)) {
+        Oct<T> own[W::kOwnTiles][2][kPieces];
+        auto weigh = [&](const f32x16 &p, const float *near, Oct<T> (&o)[2][kPieces]) __attribute__((always_inline)) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = p[8 * s + e] * near[16 * s + e];
-                oct_from(x, o[s]);
+                if constexpr (kPieces == 2) {
+                    const Pieces<T> both(x);
+                    o[s][0] = both.hi;
+                    o[s][1] = both.lo;
+                } else {
+                    oct_from(x, o[s][0]);
+                }
             }
         };
         f32x16 part;                                                   // kSplit: this wave's sum over its features
@@ -682,7 +702,9 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
 #pragma unroll
             for (int t = 0; t < W::kScoreTiles; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) settle(own[t][s]);
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int x = 0; x < kPieces; ++x) settle(own[t][s][x]);
         }
         // the tile that is this wave's (SHARED): none from kScoreTiles on, which is worked out all the same to keep the run free of branches
         f32x16 P;
@@ -718,7 +740,9 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
             if (mine < W::kScoreTiles) {
                 weigh(P, distance + (mine == 1 ? 0 : 32), own[0]);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) scores[(2 * mine + s) * 64 + lane] = own[0][s];
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int x = 0; x < kPieces; ++x) scores[((2 * mine + s) * kPieces + x) * 64 + lane] = own[0][s][x];
             }
             lds_barrier();
         }
@@ -752,9 +776,14 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
             Oct<T> v;
             token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
-            auto weights = [&](int t, int s) __attribute__((always_inline)) { return W::kShared ? scores[(2 * t + s) * 64 + lane] : own[W::kShared ? 0 : t][s]; };
-            if (sub < 2) acc[0] = oct_product(v, weights(0, sub), acc[0]);
-            if constexpr (W::kTiles == 2) acc[1] = oct_product(v, weights(1 + sub / 2, sub % 2), acc[1]);
+            auto weights = [&](int t, int s, int x) __attribute__((always_inline)) {
+                return W::kShared ? scores[((2 * t + s) * kPieces + x) * 64 + lane] : own[W::kShared ? 0 : t][s][x];
+            };
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x) {
+                if (sub < 2) acc[0] = oct_product(v, weights(0, sub, x), acc[0]);
+                if constexpr (W::kTiles == 2) acc[1] = oct_product(v, weights(1 + sub / 2, sub % 2, x), acc[1]);
+            }
             state_update<T, D>(S, tileK, v, uw, sub, lane, fine);
         }
         // the output's rows, for whole-row stores once all panels are in
@@ -765,15 +794,17 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
     if (c0 < c1) ro.store(c1 - 1, true, walk.chunks, walk.lead, tileO);
     if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, own_lane);
 }
-template <typename T, int D, bool NT> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
+// NT: tokens are read past the caches.  SHORT: no sequence is longer than a chunk.
+template <typename T, int D, bool NT, bool SHORT> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
 {
-    __shared__ __align__(16) unsigned char lds[4 * WalkShape<T, D>::kTileBytes + WalkShape<T, D>::kScoreBytes + kDecayTableBytes];
+    using W = WalkShape<T, D>;
+    __shared__ __align__(16) unsigned char lds[W::tiles(SHORT) * W::kTileBytes + W::score_pieces(SHORT) * W::kScoreBytes + kDecayTableBytes];
     const int BH = a.B * a.H;
     const WalkTask task(a.problems * BH * a.segments, BH, a.segments, a.together);
     if (!task.any) return;
     const WalkProblem &p = a.p[task.problem];
-    if (p.back) walk_segment<T, D, true, NT>(a, p, task, lds);
-    else walk_segment<T, D, false, NT>(a, p, task, lds);
+    if (p.back) walk_segment<T, D, true, NT, SHORT>(a, p, task, lds);
+    else walk_segment<T, D, false, NT, SHORT>(a, p, task, lds);
 }
 
 }  // namespace sv

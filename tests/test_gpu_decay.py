@@ -6,10 +6,10 @@ counted (1 + n |log_decay|) times for the n decays it passed through (oracle/dec
   fp32    sums of at most N tokens, d features and a state, in any order, of products rounded a few times: (N + 2 d + 64) e M.
   bf16    the same; states are built up from three bf16 pieces, u^3 = e: one more rounding of each product; what outputs come from enters
           and leaves the state in two, each product off by u^2 = 2^-16 at most: 2 u^2 M; the weighted scores are rounded once, u M at
-          most, and the output once, u |o|.
+          most (N <= 64: in two pieces, u^2 M), and the output once, u |o|.
 
 For random data the roundings are independent, so that in the 2-norm over many elements those of scores and outputs come to at most
-u / sqrt 3 each, sqrt 2 / sqrt 3 u = 3.2e-3 together."""
+u / sqrt 3 each, sqrt 2 / sqrt 3 u = 3.2e-3 together, u / sqrt 3 = 2.26e-3 where only the output is rounded."""
 import numpy as np
 import pytest
 
@@ -81,11 +81,11 @@ def _check(got, ref, mag, N, d, dtype, what, state=False, random=True):
     if dtype == "f32" or state:
         tol = (rest + E) * mag
     else:
-        tol = U * np.abs(ref) + (U + 2 * U * U + rest) * mag
+        tol = U * np.abs(ref) + ((U if N > 64 else U * U) + 2 * U * U + rest) * mag
     bad = ~(np.abs(got - ref) <= tol + 1e-37)
     assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} beyond the bound, worst by {np.nanmax((np.abs(got - ref) - tol)[bad])}"
     if random and got.size >= 2048:
-        most = 3e-6 if dtype == "f32" or state else 3.5e-3
+        most = 3e-6 if dtype == "f32" or state else 3.5e-3 if N > 64 else 2.3e-3
         assert metrics.rel_l2(got, ref) <= most, f"{what}: {metrics.rel_l2(got, ref)}"
 
 
