@@ -36,9 +36,9 @@
 // throughout (32 x 32 x 2 matrix instructions).
 //
 // A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and
-// v twice: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.7 that do) 704 us = 216 + 8 + 480, 5.3 TB/s, which is more
-// than a copy of that size reaches (4.9): bound by memory.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
-// take 242 us = 80 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
+// v twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.3 that do) 637 us = 150 + 8 + 480, 5.2 TB/s,
+// which is more than a copy of that size reaches (4.9): bound by memory.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
+// take 233 us = 70 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
 // memory accesses 114.  Calls that give each compute unit one or two workgroups are bound by a chunk's own run through LDS and the
 // matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
 // Measured and left: LDS rows whose 16-byte pieces change places, so that no read conflicts (of decay_sums' LDS cycles at d = 112 62 % are
@@ -428,6 +428,13 @@ template <int SUBS> struct UpdateWeights {
             for (int e = 0; e < 8; ++e) w[s][e] = base * pw.uniform(7 - e);
         }
     }
+    __device__ __forceinline__ void scale(float f)
+    {
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[s][e] *= f;
+    }
 };
 
 // S += sum over one sub-chunk of 16 tokens, weighted.  `values` is the wave's 32 value features of these tokens; `kept`: for a state that is kept.
@@ -479,7 +486,10 @@ __device__ __forceinline__ int walk_length(const WalkArgs &a, int b)
     return n < 0 ? 0 : n > a.N ? a.N : n;
 }
 
-// What each segment but the last adds to the state, starting from zero: into slot segment + 1 of its head.
+// What each segment but the last adds to the state, starting from zero: into slot segment + 1 of its head.  From the segment's end to its beginning:
+// what a chunk loses to the decay until then is taken into its tokens' weights (32 of them, where the state would be 64 numbers of a lane), and
+// the walk ends where the weights have come to zero: with a memory of 14 tokens (l = exp(-0.073)) 1 450 tokens back, l^1450 < 2^-150, half the
+// smallest fp32 number (heads whose memories run from one token to a thousand: 75 600 tokens of 64 heads 216 us to the end, 150 so).
 template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_sum(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
 {
     using W = WalkShape<T, D>;
@@ -490,28 +500,33 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
     if (c1 >= walk.chunks) return;                                   // the last segment of this sequence, or one behind it
     const float g = a.log_decay[h];
     const DecayPower pw(g);
-    const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
+    UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
     const ChunkDecay decay(W::kChunk, g);
     const ChunkRows<T, D, BACK> rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
     u32x4 nk[W::kSteps], nv[W::kSteps];
-    rk.template load<false, true>(c0, true, walk.chunks, walk.lead, nk);
-    rv.template load<false, true>(c0, true, walk.chunks, walk.lead, nv);
+    rk.template load<false, true>(c1 - 1, true, walk.chunks, walk.lead, nk);
+    rv.template load<false, true>(c1 - 1, true, walk.chunks, walk.lead, nv);
     StatePanel<D> S;
     S.clear();
-    for (int c = c0; c < c1; ++c) {
+    float most = p.weight_update;                                    // no weight of a decaying head is larger
+    for (int c = c1 - 1;; --c) {
         lds_barrier();
         rk.put(tileK, nk);
         rv.put(tileV, nv);
         lds_barrier();
-        rk.template load<false, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nk);
-        rv.template load<false, false>(c + 1, c + 1 < c1, walk.chunks, walk.lead, nv);
-        S.scale(decay(c));
+        rk.template load<false, true>(c - 1, c > c0, walk.chunks, walk.lead, nk);
+        rv.template load<false, true>(c - 1, c > c0, walk.chunks, walk.lead, nv);
 #pragma unroll
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
             Oct<T> v;
             token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
             state_update<T, D>(S, tileK, v, uw, sub, lane, p.kept != 0);
         }
+        if (c == c0) break;
+        const float f = decay(c1 - 1 - c);
+        uw.scale(f);
+        most *= f;
+        if (most == 0.f) break;
     }
     S.store(p.slots + ((int64_t)task.bh * a.segments + task.segment + 1) * D * D, panel, lane);
 }

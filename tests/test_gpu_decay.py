@@ -130,6 +130,9 @@ CASES = [   # B, H, N, d, dtype, layout, lengths, state, decays
     (5, 2, 321, 128, "bf16", "packed", [65, 320, 0, 5000, -3], True, "mixed"),     # held to [0, N]
     (4, 3, 230, 112, "f32", "packed", [129, 1, 0, 97], False, "mixed"),
     (13, 40, 200, 32, "bf16", "bhnd", None, True, "mixed"),          # one workgroup per head
+    (2, 32, 3000, 32, "bf16", "bnhd", [3000, 1777], True, "mixed"),  # segments of several chunks, whose first ones weigh nothing for some heads
+    (1, 40, 1500, 32, "f32", "bhnd", None, True, "mixed"),
+    (1, 60, 1200, 64, "bf16", "bhnd", None, True, "edge"),
     (9, 60, 67, 64, "f32", "bnhd", [67, 3, 0, 66, 32, 33, 1, 64, 65], True, "mixed"),
 ]
 
