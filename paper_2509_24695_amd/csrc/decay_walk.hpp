@@ -36,8 +36,8 @@
 // throughout (32 x 32 x 2 matrix instructions).
 //
 // A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and
-// v twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.3 that do) 637 us = 150 + 8 + 480, 5.2 TB/s,
-// which is more than a copy of that size reaches (4.9): bound by memory.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
+// v twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.2 that do) 637 us = 180 + 8 + 450, 5.0 TB/s,
+// as much as a copy of that size reaches (4.9): the walk is bound by memory, the sums by the heads that forget nothing.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
 // take 233 us = 70 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
 // memory accesses 114.  Calls that give each compute unit one or two workgroups are bound by a chunk's own run through LDS and the
 // matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
@@ -489,7 +489,9 @@ __device__ __forceinline__ int walk_length(const WalkArgs &a, int b)
 // What each segment but the last adds to the state, starting from zero: into slot segment + 1 of its head.  From the segment's end to its beginning:
 // what a chunk loses to the decay until then is taken into its tokens' weights (32 of them, where the state would be 64 numbers of a lane), and
 // the walk ends where the weights have come to zero: with a memory of 14 tokens (l = exp(-0.073)) 1 450 tokens back, l^1450 < 2^-150, half the
-// smallest fp32 number (heads whose memories run from one token to a thousand: 75 600 tokens of 64 heads 216 us to the end, 150 so).
+// smallest fp32 number (75 600 tokens of 64 heads whose memories run from one token to a thousand: 1.16 GB read and 216 us to the end, 0.70 GB and
+// 180 so).  Sums of half a segment or less, for shorter walks and more workgroups, take longer (697 us a call instead of 650): less of them weighs
+// nothing.
 template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_sum(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
 {
     using W = WalkShape<T, D>;
