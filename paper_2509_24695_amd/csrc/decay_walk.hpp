@@ -35,12 +35,12 @@
 // . k_j) are rounded to bf16 once (score_pieces has the exception), like the output (both 2^-8 of a term at most).  fp32 tokens: fp32 products
 // throughout (32 x 32 x 2 matrix instructions).
 //
-// A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and
-// v twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.2 that do) 637 us = 180 + 8 + 450, 5.0 TB/s,
-// as much as a copy of that size reaches (4.9): the walk is bound by memory, the sums by the heads that forget nothing.  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88)
-// take 233 us = 70 + 10 + 150: rows of 224 bytes begin and end inside lines of 128, and the walk alone without its products takes 138 us, without its
-// memory accesses 114.  Calls that give each compute unit one or two workgroups are bound by a chunk's own run through LDS and the
-// matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
+// A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and v
+// twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.2 that do) 637 us = 180 + 8 + 450, 5.0
+// TB/s, as much as a copy of that size reaches (4.9): the walk is bound by memory, the sums by the heads that forget nothing.  Heads of 112 whose
+// rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88) take 233 us = 70 + 10 + 150: rows of 224 bytes begin and end inside lines of 128,
+// and the walk alone without its products takes 138 us, without its memory accesses 114.  Calls that give each compute unit one or two workgroups
+// are bound by a chunk's own run through LDS and the matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
 // Measured and left: LDS rows whose 16-byte pieces change places, so that no read conflicts (of decay_sums' LDS cycles at d = 112 62 % are
 // conflicts, the walk's 39 %): 1 to 3 % slower by the addresses' arithmetic, as LDS is busy for a sixth of the time; two chunks' rows on their way
 // in decay_sums (the same, +-2 %) or in the walk (one workgroup less on a compute unit: 289 us instead of 252); heads in groups whose k and v fit
