@@ -497,17 +497,18 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
     using W = WalkShape<T, D>;
     unsigned char *tileK = lds, *tileV = lds + W::kTileBytes;
     const int b = task.bh / a.H, h = task.bh % a.H, lane = threadIdx.x & 63, panel = threadIdx.x >> 6;
+    const float g = a.log_decay[h];
     const DecayWalk walk(walk_length(a, b), W::kChunk);
     const int c0 = task.segment * a.per_segment, c1 = c0 + a.per_segment;
     if (c1 >= walk.chunks) return;                                   // the last segment of this sequence, or one behind it
-    const float g = a.log_decay[h];
-    const DecayPower pw(g);
-    UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
-    const ChunkDecay decay(W::kChunk, g);
+    // the first tokens are on their way while the powers are worked out
     const ChunkRows<T, D, BACK> rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h);
     u32x4 nk[W::kSteps], nv[W::kSteps];
     rk.template load<false, true>(c1 - 1, true, walk.chunks, walk.lead, nk);
     rv.template load<false, true>(c1 - 1, true, walk.chunks, walk.lead, nv);
+    const DecayPower pw(g);
+    UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, lane);
+    const ChunkDecay decay(W::kChunk, g);
     StatePanel<D> S;
     S.clear();
     float most = p.weight_update;                                    // no weight of a decaying head is larger
@@ -609,12 +610,19 @@ template <typename T, int D, bool BACK, bool NT, bool SHORT> __device__ __forcei
     constexpr int kPieces = W::score_pieces(SHORT);
     float *table = reinterpret_cast<float *>(behind + kPieces * W::kScoreBytes), *from_state = table + 96;
     const int b = task.bh / a.H, h = task.bh % a.H, own_lane = threadIdx.x & 63, panel = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const float g = a.log_decay[h];
     const DecayWalk walk(walk_length(a, b), W::kChunk);
     const int c0 = task.segment * a.per_segment;
     int c1 = c0 + a.per_segment;
     const bool last = c1 >= walk.chunks;
     if (c1 > walk.chunks) c1 = walk.chunks;
     if (c0 >= c1 && task.segment > 0) return;
+    // the first tokens and the state are on their way while the powers are worked out
+    const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h), ro(p.o, p.so, b, h);
+    u32x4 nq[W::kSteps], nk[W::kSteps], nv[W::kSteps];
+    rq.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nq);
+    rk.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nk);
+    rv.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nv);
     const float *begin = a.segments > 1 && walk.chunks > 0 && (task.segment > 0 || p.s_begin) ? p.slots + ((int64_t)task.bh * a.segments + task.segment) * D * D
                          : p.s_begin                                                          ? p.s_begin + (int64_t)task.bh * D * D
                                                                                               : nullptr;
@@ -623,7 +631,6 @@ template <typename T, int D, bool BACK, bool NT, bool SHORT> __device__ __forcei
     else S.clear();
     const bool keep = last && p.s_end, fine = last && p.kept;        // this workgroup's state is the sequence's last
 
-    const float g = a.log_decay[h];
     const DecayPower pw(g);
     const UpdateWeights<W::kTokSubs> uw(pw, W::kChunk, BACK, p.weight_update, own_lane);
     const ChunkDecay decay(W::kChunk, g);
@@ -637,12 +644,6 @@ template <typename T, int D, bool BACK, bool NT, bool SHORT> __device__ __forcei
     // weights of the scores by distance: table[63 - distance], zeros where the row lies behind.  Row 32 it + col and row 32 jt + 16 s + 8 half
     // + e are 32 (it - jt) + col - 16 s - 8 half - e apart.  In LDS: sixteen registers that every chunk needs for a moment only.
     for (int i = threadIdx.x; i < 96; i += W::kWalkThreads) table[i] = i < 64 ? p.weight_chunk * pw(63 - i) : 0.f;
-
-    const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h), ro(p.o, p.so, b, h);
-    u32x4 nq[W::kSteps], nk[W::kSteps], nv[W::kSteps];
-    rq.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nq);
-    rk.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nk);
-    rv.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nv);
 
     for (int c = c0; c < c1; ++c) {
         lds_barrier();
