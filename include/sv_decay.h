@@ -26,8 +26,8 @@
  *    Rows behind a sequence's last token are neither read nor written, whatever they hold.  A sequence of length zero has
  *    S_out = S_in.
  *  - SV_BF16: bf16 products with fp32 accumulation; S_out and dS_in are fp32 states (what enters them goes through three bf16 values, 2^-24 of
- *    a term), what comes out of a state on its way to O, dQ, dK and dV goes through pairs of them (2^-16 of a term), weighted scores
- *    are rounded to bf16 once (N <= 64: taken as pairs too), outputs once.  SV_F32: fp32 products.
+ *    a term), what comes out of a state on its way to O, dQ, dK and dV and the weighted scores go through pairs of them (2^-16 of a
+ *    term), outputs are rounded once.  SV_F32: fp32 products.
  *  - A token's weight l^n in a state many tokens later is an fp32 number: where it has come to zero the token may be passed over.
  *  - Tokens of a sequence, states and log decays must be finite numbers (minus infinity apart): a NaN or infinity also reaches outputs of
  *    up to 63 tokens before it.

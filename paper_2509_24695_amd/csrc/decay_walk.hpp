@@ -29,11 +29,13 @@
 // 8 (r / 4) + 4 h + r % 4 of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to
 // the first operand of a product in the order decay_row, which makes eight accumulators in a row eight consecutive indices.
 //
-// Roundings (bf16 tokens): S enters o, and the weighted values l^{..} v_j enter S, as two bf16 pieces (together within 2^-16; with one the call is
-// 3 to 8 % faster and the output 2.4e-3 off instead of 1.8e-3).  A state that the caller gets is an fp32 one: what goes into it, in the sums and in
-// the last segment's walk, is in three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; 246 us and 233).  The weighted scores l^{i-j} (q_i
-// . k_j) are rounded to bf16 once (score_pieces has the exception), like the output (both 2^-8 of a term at most).  fp32 tokens: fp32 products
-// throughout (32 x 32 x 2 matrix instructions).
+// Roundings (bf16 tokens): S enters o, the weighted scores l^{i-j} (q_i . k_j) enter o, and the weighted values l^{..} v_j enter S, as two bf16
+// pieces (together within 2^-16), so that outputs are off by their own rounding, 1.66e-3 in the 2-norm.  (S in one piece: calls 3 to 8 % shorter, outputs
+// 2.4e-3 off.  Scores in one: 2.3e-3 off for heads that remember up to some twenty tokens, 1.8e-3 over heads that remember 1 to 1 000; us with two / one:
+// 32 760 tokens of 20 heads of 112 243 / 236, 75 600 of 64 heads of 64 644 / 639, backward pass of 4 680 of 32 heads of 64 66.4 / 62.5, 300 tokens of 224
+// heads of 64 18.0 / 16.8.)  A state that the caller gets is an fp32 one: what goes into it, in the sums and in the last segment's walk, is in
+// three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; 246 us and 233).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix
+// instructions).
 //
 // A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and v
 // twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.2 that do) 637 us = 180 + 8 + 450, 5.0
@@ -171,16 +173,14 @@ template <typename T, int D> struct WalkShape {
     static constexpr int kScoreTiles = kTiles == 2 ? 3 : 1;
     // who works the scores out: tile by tile for each other (kShared), each a part of the features (kSplit), or every wave for itself
     static constexpr bool kShared = sizeof(T) == 2 && kPanels == 4, kSplit = sizeof(T) == 4 && kPanels > 1;
-    static constexpr int kOwnTiles = kShared ? 1 : kScoreTiles, kScoreBytes = kShared ? kScoreTiles * 2 * 64 * 8 * (int)sizeof(T) : 0;
-    // The weighted scores are one bf16 value each, but two where no sequence is longer than a chunk: a few tokens then come out as exactly as they do
-    // one by one, which costs nothing in a call that is mostly its launch (8 heads
-    // of 64 or 128, 1 to 64 tokens: 8 to 9 us either way) and little in a large one (us with two / one: 2 000 heads of 64, one token 23.0 / 21.9, 64
-    // tokens 27.7 / 27.2; of 128, 64 tokens 79.9 / 79.6).  Outputs are then 1.66e-3 off instead of 2.3e-3 (root of the mean square).
-    static constexpr int score_pieces(bool is_short) { return is_short && sizeof(T) == 2 ? 2 : 1; }
-    // Tiles in LDS: queries, keys, values and outputs.  With shared scores the waves meet after their last look at the queries, so that the outputs of
-    // a walk of one chunk take their place, and the second pieces of the scores do not cost the compute unit its second workgroup (2 000
-    // heads of 128, one token: 55 us, with a tile of their own 83).
-    static constexpr int tiles(bool is_short) { return is_short && kShared ? 3 : 4; }
+    static constexpr int kOwnTiles = kShared ? 1 : kScoreTiles, kScoreBytes = kShared ? kScoreTiles * 2 * 2 * 64 * 8 * (int)sizeof(T) : 0;
+    // bf16 pieces of a weighted score.  One would put 2^-8 of a term into the output beside the output's own rounding, which shows where a few terms
+    // make up an output: heads that remember up to some twenty tokens, or short sequences (2.3e-3 off instead of 1.66e-3).
+    static constexpr int kPieces = sizeof(T) == 2 ? 2 : 1;
+    // Tiles in LDS: queries, keys, values and outputs.  With shared scores the waves meet after their last look at the queries, so that the outputs
+    // take their place: a fourth tile and two pieces of each score would cost the compute unit its second workgroup (2 000 heads of 128, one
+    // token: 83 us instead of 55).  A thread fetches those pieces of the outputs from there that it then overwrites with the next queries.
+    static constexpr int kTilesInLds = kShared ? 3 : 4;
     static_assert(kSteps * kRowsPerStep == kChunk && D % 16 == 0, "whole rows");
 };
 
@@ -601,14 +601,14 @@ template <typename W> __device__ __forceinline__ void put_features(unsigned char
     for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(row + (8 * x + 4 * half) * 4) = f32x4{acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]};
 }
 
-template <typename T, int D, bool BACK, bool NT, bool SHORT> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
+template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
 {
     using W = WalkShape<T, D>;
     unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes;
-    unsigned char *tileO = W::tiles(SHORT) == 4 ? lds + 3 * W::kTileBytes : tileQ, *behind = lds + W::tiles(SHORT) * W::kTileBytes;
+    unsigned char *tileO = W::kTilesInLds == 4 ? lds + 3 * W::kTileBytes : tileQ, *behind = lds + W::kTilesInLds * W::kTileBytes;
     Oct<T> *scores = reinterpret_cast<Oct<T> *>(behind);
-    constexpr int kPieces = W::score_pieces(SHORT);
-    float *table = reinterpret_cast<float *>(behind + kPieces * W::kScoreBytes), *from_state = table + 96;
+    constexpr int kPieces = W::kPieces;
+    float *table = reinterpret_cast<float *>(behind + W::kScoreBytes), *from_state = table + 96;
     const int b = task.bh / a.H, h = task.bh % a.H, own_lane = threadIdx.x & 63, panel = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const float g = a.log_decay[h];
     const DecayWalk walk(walk_length(a, b), W::kChunk);
@@ -812,17 +812,17 @@ template <typename T, int D, bool BACK, bool NT, bool SHORT> __device__ __forcei
     if (c0 < c1) ro.store(c1 - 1, true, walk.chunks, walk.lead, tileO);
     if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, own_lane);
 }
-// NT: tokens are read past the caches.  SHORT: no sequence is longer than a chunk.
-template <typename T, int D, bool NT, bool SHORT> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
+// NT: tokens are read past the caches.
+template <typename T, int D, bool NT> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
 {
     using W = WalkShape<T, D>;
-    __shared__ __align__(16) unsigned char lds[W::tiles(SHORT) * W::kTileBytes + W::score_pieces(SHORT) * W::kScoreBytes + kDecayTableBytes];
+    __shared__ __align__(16) unsigned char lds[W::kTilesInLds * W::kTileBytes + W::kScoreBytes + kDecayTableBytes];
     const int BH = a.B * a.H;
     const WalkTask task(a.problems * BH * a.segments, BH, a.segments, a.together);
     if (!task.any) return;
     const WalkProblem &p = a.p[task.problem];
-    if (p.back) walk_segment<T, D, true, NT, SHORT>(a, p, task, lds);
-    else walk_segment<T, D, false, NT, SHORT>(a, p, task, lds);
+    if (p.back) walk_segment<T, D, true, NT>(a, p, task, lds);
+    else walk_segment<T, D, false, NT>(a, p, task, lds);
 }
 
 }  // namespace sv

@@ -73,12 +73,10 @@ template <typename T, int D> sv_status run_walk(WalkArgs sums, const WalkArgs &w
         if (launched() != SV_OK) return SV_ERR_LAUNCH;
     }
     const unsigned grid = decay_grid(walks.problems * BH * walks.segments, walks.together);
-    if (sizeof(T) == 2 && walks.N <= W::kChunk)
-        decay_walk<T, D, false, sizeof(T) == 2><<<grid, W::kWalkThreads, 0, stream>>>(walks);
-    else if (walks.problems == 1 && (int64_t)2 * BH * walks.N * D * (int)sizeof(T) > kLastCacheBytes)
-        decay_walk<T, D, true, false><<<grid, W::kWalkThreads, 0, stream>>>(walks);
+    if (walks.problems == 1 && (int64_t)2 * BH * walks.N * D * (int)sizeof(T) > kLastCacheBytes)
+        decay_walk<T, D, true><<<grid, W::kWalkThreads, 0, stream>>>(walks);
     else
-        decay_walk<T, D, false, false><<<grid, W::kWalkThreads, 0, stream>>>(walks);
+        decay_walk<T, D, false><<<grid, W::kWalkThreads, 0, stream>>>(walks);
     return launched();
 }
 
