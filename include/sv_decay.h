@@ -20,8 +20,8 @@
  *  - `qkv` describes Q, K and V (and dQ, dK, dV), `o` describes O (and dO): same B, H, N, d and dtype, strides of their own, so that
  *    q, k and v may be views of one projection's output.  64 rows must span less than 2 GiB (else SV_ERR_UNSUPPORTED); heads may
  *    span any number of bytes.
- *  - log_decay is fp32 [H]: 0 keeps everything, minus infinity (l = 0) nothing but the token itself.  Values above 0 grow and may
- *    overflow.
+ *  - log_decay is fp32 [H]: 0 keeps everything, minus infinity (l = 0) nothing but the token itself.  Values above 0 grow: a power of l past
+ *    the largest fp32 number counts as that number, and results are finite where the formulas' terms are.
  *  - lengths is int32 [B] or NULL: sequence b has the tokens [0, lengths[b]) of its row (values are held to [0, N]); NULL: N each.
  *    Rows behind a sequence's last token are neither read nor written, whatever they hold.  A sequence of length zero has
  *    S_out = S_in.

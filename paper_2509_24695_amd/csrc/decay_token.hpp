@@ -64,7 +64,7 @@ template <typename T, int D, int SPLIT> __global__ __launch_bounds__(256) void d
     if (a.slots)
         for (int r = threadIdx.x; r < b; r += W::kTokThreads) taken |= a.slots[r] == slot;
     if (__syncthreads_or(taken)) return;
-    const float l = expf(a.log_decay[h]);
+    const float grown = expf(a.log_decay[h]), l = grown > 3.40282347e38f ? 3.40282347e38f : grown;       // a state of nothing stays one
     const bool elsewhere = a.s_out != a.s_in;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

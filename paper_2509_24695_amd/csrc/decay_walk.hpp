@@ -8,7 +8,7 @@
 //   S  <- l^C S + sum_j l^{C-1-j} k_j v_j^T
 //
 // All four products run on the matrix cores; every power of l that occurs has an exponent >= 0, so nothing overflows however strong the
-// decay is.  The backward pass is the same walk three times, on other operands (WalkProblem):
+// decay is (and a growing head's weights are held to finite ones).  The backward pass is the same walk three times, on other operands (WalkProblem):
 //
 //   dq   q, k, v = dO, V, K from the transposed state        forwards
 //   dv             K, Q, dO from the gradient of the state   backwards in time
@@ -252,11 +252,21 @@ __device__ __forceinline__ void settle(Oct<float> &o)
 
 // ---- powers of the decay ---------------------------------------------------------------------------------------------
 
+// A weight that meets zeros (rows that are no tokens, a state of nothing) has to stay a number: a growing head's powers, l > 1, end at the largest.
+__device__ __forceinline__ float held(float x)
+{
+    constexpr float kMost = 3.40282347e38f;
+    return x > kMost ? kMost : x < -kMost ? -kMost : x;
+}
+
 // l^e for e >= 0.  A log decay of minus infinity is a decay of zero: l^0 = 1, all other powers 0.
 struct DecayPower {
     float lg;
     __device__ __forceinline__ explicit DecayPower(float log_decay) : lg((log_decay < -1e30f ? -1e30f : log_decay) * 1.44269504088896f) {}
-    __device__ __forceinline__ float operator()(int e) const { return exp2f(lg * (float)e); }
+    __device__ __forceinline__ float operator()(int e) const { return held(power(e)); }
+    // not held: infinite where it is too large
+    __device__ __forceinline__ float power(int e) const { return exp2f(lg * (float)e); }
+    __device__ __forceinline__ bool grows() const { return lg > 0.f; }
     // for exponents that are the same in all lanes: kept in scalar registers
     __device__ __forceinline__ float uniform(int e) const { return scalar((*this)(e)); }
     static __device__ __forceinline__ float scalar(float x)
@@ -272,9 +282,9 @@ struct ChunkDecay {
     __device__ __forceinline__ ChunkDecay(int chunk, float log_decay)
     {
         const double x = exp((double)(log_decay < -1e30f ? -1e30f : log_decay) * (double)chunk);
-        const float f = (float)x;
+        const float f = held((float)x);
         usual = DecayPower::scalar(f);
-        eighth = DecayPower::scalar((float)(x + 7.0 * (x - (double)f)));
+        eighth = DecayPower::scalar(x < 1e38 ? (float)(x + 7.0 * (x - (double)f)) : f);
     }
     __device__ __forceinline__ float operator()(int nth) const { return (nth & 7) == 7 ? eighth : usual; }
 };
@@ -418,15 +428,23 @@ template <int D> struct StatePanel {
 // A row's weight in the new state, by lane half: l^{C-1-j} for j = 16 sub + 8 h + e.
 template <int SUBS> struct UpdateWeights {
     float w[SUBS][8];
+    // (a branch for growing heads: holding all of them costs a short call up to 1 us)
     __device__ __forceinline__ UpdateWeights(const DecayPower &pw, int chunk, int back, float factor, int lane)
     {
         const int h = lane >> 5;
+        auto fill = [&](auto hold) __attribute__((always_inline)) {
+            float near[8];
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s) {
-            const float base = factor * pw(chunk - 8 - 16 * s - 8 * h + back);
+            for (int e = 0; e < 8; ++e) near[e] = DecayPower::scalar(hold(pw.power(7 - e)));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[s][e] = base * pw.uniform(7 - e);
-        }
+            for (int s = 0; s < SUBS; ++s) {
+                const float base = hold(factor * hold(pw.power(chunk - 8 - 16 * s - 8 * h + back)));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[s][e] = hold(base * near[e]);
+            }
+        };
+        if (pw.grows()) fill([](float x) { return held(x); });
+        else fill([](float x) { return x; });
     }
     __device__ __forceinline__ void scale(float f)
     {
@@ -434,6 +452,12 @@ template <int SUBS> struct UpdateWeights {
         for (int s = 0; s < SUBS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[s][e] *= f;
+        if (f > 1.f) {
+#pragma unroll
+            for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[s][e] = held(w[s][e]);
+        }
     }
 };
 
@@ -638,12 +662,12 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
     // a row's weight on what comes out of the state, whole chunks and the first one
     for (int i = threadIdx.x; i < W::kChunk; i += W::kWalkThreads) {
         const int e = i + 1 - (int)BACK;
-        from_state[i] = p.weight_state * pw(e);
-        from_state[64 + i] = p.weight_state * pw(e < walk.lead ? 0 : e - walk.lead);
+        from_state[i] = held(p.weight_state * pw(e));
+        from_state[64 + i] = held(p.weight_state * pw(e < walk.lead ? 0 : e - walk.lead));
     }
     // weights of the scores by distance: table[63 - distance], zeros where the row lies behind.  Row 32 it + col and row 32 jt + 16 s + 8 half
     // + e are 32 (it - jt) + col - 16 s - 8 half - e apart.  In LDS: sixteen registers that every chunk needs for a moment only.
-    for (int i = threadIdx.x; i < 96; i += W::kWalkThreads) table[i] = i < 64 ? p.weight_chunk * pw(63 - i) : 0.f;
+    for (int i = threadIdx.x; i < 96; i += W::kWalkThreads) table[i] = i < 64 ? held(p.weight_chunk * pw(63 - i)) : 0.f;
 
     for (int c = c0; c < c1; ++c) {
         lds_barrier();
