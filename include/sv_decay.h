@@ -29,8 +29,9 @@
  *    a term), what comes out of a state on its way to O, dQ, dK and dV and the weighted scores go through pairs of them (2^-16 of a
  *    term), outputs are rounded once.  SV_F32: fp32 products.
  *  - A token's weight l^n in a state many tokens later is an fp32 number: where it has come to zero the token may be passed over.
- *  - Tokens of a sequence, states and log decays must be finite numbers (minus infinity apart): a NaN or infinity also reaches outputs of
- *    up to 63 tokens before it.
+ *  - A NaN or an infinity in a token, a gradient or a state makes what depends on it by the formulas NaN or infinite, and nothing else: outputs
+ *    of earlier tokens are what they would be without it (such a segment is walked twice).  The products q . k of tokens up to 63
+ *    apart must stay in the range of fp32, and log decays must be numbers (minus infinity among them).
  *  - Outputs must not overlap inputs or each other, but for S_out = S_in where that is said.
  */
 #ifndef SV_DECAY_H

@@ -54,7 +54,7 @@
 
 namespace sv {
 
-constexpr int kDecayTableBytes = (96 + 2 * 64) * 4;
+constexpr int kDecayTableBytes = (96 + 2 * 64 + 4) * 4;     // weights of scores and of the state's share; a word of each wave
 constexpr uint32_t kNoRow = 0x80000000u;      // past every resource: the host keeps 64 rows below 2 GiB
 
 // Row m of a 32-row operand serves index decay_row(m): bits 2 and 3 change places.
@@ -423,6 +423,15 @@ template <int D> struct StatePanel {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[sub / 2][8 * (sub % 2) + e];
     }
+    __device__ __forceinline__ bool finite() const
+    {
+        float zero[4] = {0.f, 0.f, 0.f, 0.f};                           // zero times a number is zero
+#pragma unroll
+        for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) zero[r & 3] = __builtin_fmaf(s[kt][r], 0.f, zero[r & 3]);
+        return (zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f;
+    }
 };
 
 // A row's weight in the new state, by lane half: l^{C-1-j} for j = 16 sub + 8 h + e.
@@ -463,14 +472,14 @@ template <int SUBS> struct UpdateWeights {
 
 // S += sum over one sub-chunk of 16 tokens, weighted.  `values` is the wave's 32 value features of these tokens; `kept`: for a state that is kept.
 template <typename T, int D>
-__device__ __forceinline__ void state_update(StatePanel<D> &S, const unsigned char *tileK, const Oct<T> &values, const UpdateWeights<WalkShape<T, D>::kTokSubs> &w,
-                                             int sub, int lane, bool kept)
+__device__ __forceinline__ void state_update(StatePanel<D> &S, const unsigned char *tileK, const Oct<T> &values, const float (&w)[8], int sub,
+                                             int lane, bool kept)
 {
     using W = WalkShape<T, D>;
     float x[8];
     oct_to(values, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= w.w[sub][e];
+    for (int e = 0; e < 8; ++e) x[e] *= w[e];
     const Pieces<T> v(x);
     Oct<T> k[StatePanel<D>::kKeyTiles];
 #pragma unroll
@@ -547,7 +556,7 @@ template <typename T, int D, bool BACK> __device__ __forceinline__ void segment_
         for (int sub = 0; sub < W::kTokSubs; ++sub) {
             Oct<T> v;
             token_operand<W, false>(tileV, 16 * sub, 32 * panel, lane, v);
-            state_update<T, D>(S, tileK, v, uw, sub, lane, p.kept != 0);
+            state_update<T, D>(S, tileK, v, uw.w[sub], sub, lane, p.kept != 0);
         }
         if (c == c0) break;
         const float f = decay(c1 - 1 - c);
@@ -625,14 +634,154 @@ template <typename W> __device__ __forceinline__ void put_features(unsigned char
     for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(row + (8 * x + 4 * half) * 4) = f32x4{acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]};
 }
 
+// Where a walk's things lie in LDS.
+template <typename T, int D> struct WalkLds {
+    using W = WalkShape<T, D>;
+    unsigned char *q, *k, *v, *o;       // tiles
+    Oct<T> *scores;
+    float *table, *from_state;
+    int *votes;                         // of each wave
+    __device__ __forceinline__ explicit WalkLds(unsigned char *lds)
+        : q(lds), k(lds + W::kTileBytes), v(lds + 2 * W::kTileBytes), o(W::kTilesInLds == 4 ? lds + 3 * W::kTileBytes : q),
+          scores(reinterpret_cast<Oct<T> *>(lds + W::kTilesInLds * W::kTileBytes)),
+          table(reinterpret_cast<float *>(lds + W::kTilesInLds * W::kTileBytes + W::kScoreBytes)), from_state(table + 96),
+          votes(reinterpret_cast<int *>(from_state + 128)) {}
+};
+
+// The state that a segment begins from, or NULL: zeros.
+template <int D> __device__ __forceinline__ const float *begin_of(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, int chunks)
+{
+    return a.segments > 1 && chunks > 0 && (task.segment > 0 || p.s_begin) ? p.slots + ((int64_t)task.bh * a.segments + task.segment) * D * D
+           : p.s_begin                                                     ? p.s_begin + (int64_t)task.bh * D * D
+                                                                           : nullptr;
+}
+
+// What a value adds to products: itself, or nothing and a mark where it is no number.
+template <typename T> __device__ __forceinline__ void part_numbers(const Oct<T> &o, Oct<T> &numbers, Oct<T> &marks)
+{
+    float x[8], n[8], m[8];
+    oct_to(o, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bool is = __builtin_isfinite(x[e]);
+        n[e] = is ? x[e] : 0.f;
+        m[e] = is ? 0.f : 1.f;
+    }
+    oct_from(n, numbers);
+    oct_from(m, marks);
+}
+
+// The walk of a segment into which a NaN or an infinity has come, once more.  A product over a chunk multiplies what lies ahead of a row by zero,
+// and zero times such a value is NaN: in the walk proper it reaches outputs of up to 63 tokens before its own.  Here scores ahead of a row are taken
+// out by their place, and values that are no numbers add nothing, but marks, whose products with ones at and behind their tokens tell
+// which outputs see one of them.  `table` and `from_state` are as the walk has left them.  Nothing here is for speed; looking for such values
+// in the state, once at a segment's end, takes 0.2 to 0.4 us of a call.
+template <typename T, int D, bool BACK> __device__ __forceinline__ void walk_again(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
+{
+    using W = WalkShape<T, D>;
+    const WalkLds<T, D> at(lds);
+    const int b = task.bh / a.H, h = task.bh % a.H, lane = threadIdx.x & 63, panel = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int half = lane >> 5, col = lane & 31;
+    const float g = a.log_decay[h];
+    const DecayWalk walk(walk_length(a, b), W::kChunk);
+    const int c0 = task.segment * a.per_segment, c1 = c0 + a.per_segment < walk.chunks ? c0 + a.per_segment : walk.chunks;
+    const bool last = c0 + a.per_segment >= walk.chunks;
+    const ChunkRows<T, D, BACK> rq(p.q, p.sq, b, h), rk(p.k, p.sk, b, h), rv(p.v, p.sv, b, h), ro(p.o, p.so, b, h);
+    const float *begin = begin_of<D>(a, p, task, walk.chunks);
+    StatePanel<D> S;
+    if (begin) S.load(begin, p.turned, panel, lane);
+    else S.clear();
+    const DecayPower pw(g);
+    const ChunkDecay decay(W::kChunk, g);
+    const float first_decay = pw.uniform(W::kChunk - walk.lead);
+#pragma unroll 1
+    for (int c = c0; c < c1; ++c) {
+        u32x4 next[W::kSteps];
+        lds_barrier();
+        rq.template load<false, true>(c, true, walk.chunks, walk.lead, next);
+        rq.put(at.q, next);
+        rk.template load<false, true>(c, true, walk.chunks, walk.lead, next);
+        rk.put(at.k, next);
+        rv.template load<false, true>(c, true, walk.chunks, walk.lead, next);
+        rv.put(at.v, next);
+        lds_barrier();
+#pragma unroll 1
+        for (int it = 0; it < W::kTiles; ++it) {
+            f32x16 acc, marked;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = marked[r] = 0.f;
+            const unsigned char *rows = at.q + (32 * it + col) * W::kRowBytes + 8 * half * (int)sizeof(T);
+#pragma unroll
+            for (int sub = 0; sub < W::kSubs; ++sub) {
+                Oct<T> q;
+                row_operand(rows + 16 * sub * (int)sizeof(T), q);
+                float x[8];
+                S.eight(sub, x);
+                // (taken apart anew for each tile: all of the state's pieces are as many registers as the state)
+                asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
+                const Pieces<T> s(x);
+                acc = s.second(q, s.first(q, acc));
+            }
+            const float weight = at.from_state[(c == 0 ? 64 : 0) + 32 * it + col];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] *= weight;
+#pragma unroll 1
+            for (int jt = 0; jt <= it; ++jt) {
+                f32x16 P;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) P[r] = 0.f;
+#pragma unroll 1
+                for (int sub = 0; sub < W::kSubs; ++sub) {
+                    Oct<T> q, k;
+                    row_operand(rows + 16 * sub * (int)sizeof(T), q);
+                    row_operand(at.k + (32 * jt + decay_row(col)) * W::kRowBytes + (16 * sub + 8 * half) * (int)sizeof(T), k);
+                    P = oct_product(k, q, P);
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    float x[8], one[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int distance = 32 * (it - jt) + col - 16 * s - 8 * half - e;
+                        x[e] = distance < 0 ? 0.f : P[8 * s + e] * at.table[63 - distance];
+                        one[e] = distance < 0 ? 0.f : 1.f;
+                    }
+                    Oct<T> v, numbers, marks, ones;
+                    token_operand<W, false>(at.v, 32 * jt + 16 * s, 32 * panel, lane, v);
+                    part_numbers(v, numbers, marks);
+                    oct_from(one, ones);
+                    const Pieces<T> both(x);
+                    acc = both.second_right(numbers, both.first_right(numbers, acc));
+                    marked = oct_product(marks, ones, marked);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = marked[r] > 0.f ? __builtin_nanf("") : acc[r];
+            lds_barrier();                                             // rows of this tile are read here only: outputs may take their place
+            put_features<W>(at.o + (32 * it + col) * W::kRowBytes + 32 * panel * (int)sizeof(T), acc, half, T{});
+        }
+        S.scale(c == 0 ? first_decay : decay(c));
+#pragma unroll 1
+        for (int sub = 0; sub < W::kTokSubs; ++sub) {
+            Oct<T> v;
+            token_operand<W, false>(at.v, 16 * sub, 32 * panel, lane, v);
+            const UpdateWeights<1> uw(pw, W::kChunk - 16 * sub, BACK, p.weight_update, lane);
+            state_update<T, D>(S, at.k, v, uw.w[0], sub, lane, last && p.kept);
+        }
+        lds_barrier();
+        ro.store(c, true, walk.chunks, walk.lead, at.o);
+    }
+    if (last && p.s_end) S.store(p.s_end + (int64_t)task.bh * D * D, panel, lane);
+}
+
 template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void walk_segment(const WalkArgs &a, const WalkProblem &p, const WalkTask &task, unsigned char *lds)
 {
     using W = WalkShape<T, D>;
-    unsigned char *tileQ = lds, *tileK = lds + W::kTileBytes, *tileV = lds + 2 * W::kTileBytes;
-    unsigned char *tileO = W::kTilesInLds == 4 ? lds + 3 * W::kTileBytes : tileQ, *behind = lds + W::kTilesInLds * W::kTileBytes;
-    Oct<T> *scores = reinterpret_cast<Oct<T> *>(behind);
+    const WalkLds<T, D> at(lds);
+    unsigned char *const tileQ = at.q, *const tileK = at.k, *const tileV = at.v, *const tileO = at.o;
+    Oct<T> *const scores = at.scores;
+    float *const table = at.table, *const from_state = at.from_state;
     constexpr int kPieces = W::kPieces;
-    float *table = reinterpret_cast<float *>(behind + W::kScoreBytes), *from_state = table + 96;
     const int b = task.bh / a.H, h = task.bh % a.H, own_lane = threadIdx.x & 63, panel = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const float g = a.log_decay[h];
     const DecayWalk walk(walk_length(a, b), W::kChunk);
@@ -647,9 +796,7 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
     rq.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nq);
     rk.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nk);
     rv.template load<NT, true>(c0, c0 < c1, walk.chunks, walk.lead, nv);
-    const float *begin = a.segments > 1 && walk.chunks > 0 && (task.segment > 0 || p.s_begin) ? p.slots + ((int64_t)task.bh * a.segments + task.segment) * D * D
-                         : p.s_begin                                                          ? p.s_begin + (int64_t)task.bh * D * D
-                                                                                              : nullptr;
+    const float *begin = begin_of<D>(a, p, task, walk.chunks);
     StatePanel<D> S;
     if (begin) S.load(begin, p.turned, panel, own_lane);
     else S.clear();
@@ -826,15 +973,27 @@ template <typename T, int D, bool BACK, bool NT> __device__ __forceinline__ void
                 if (sub < 2) acc[0] = oct_product(v, weights(0, sub, x), acc[0]);
                 if constexpr (W::kTiles == 2) acc[1] = oct_product(v, weights(1 + sub / 2, sub % 2, x), acc[1]);
             }
-            state_update<T, D>(S, tileK, v, uw, sub, lane, fine);
+            state_update<T, D>(S, tileK, v, uw.w[sub], sub, lane, fine);
         }
         // the output's rows, for whole-row stores once all panels are in
 #pragma unroll
         for (int it = 0; it < W::kTiles; ++it) put_features<W>(tileO + (32 * it + col) * W::kRowBytes + 32 * panel * (int)sizeof(T), acc[it], half, T{});
     }
+    // a token that is no number leaves its trace in the state
+    const bool clean = __all(S.finite());
+    if (own_lane == 0) at.votes[panel] = clean;
     lds_barrier();
     if (c0 < c1) ro.store(c1 - 1, true, walk.chunks, walk.lead, tileO);
-    if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, own_lane);
+    int all = 1;
+#pragma unroll
+    for (int w = 0; w < W::kPanels; ++w) all &= at.votes[w];
+    if (__builtin_amdgcn_readfirstlane(all) || c0 >= c1) {
+        if (keep) S.store(p.s_end + (int64_t)task.bh * D * D, panel, own_lane);
+    } else {
+        WalkTask same = task;                                          // nothing of the walk is kept for this
+        asm volatile("" : "+s"(same.bh), "+s"(same.segment));
+        walk_again<T, D, BACK>(a, p, same, lds);
+    }
 }
 // NT: tokens are read past the caches.
 template <typename T, int D, bool NT> __global__ __launch_bounds__((WalkShape<T, D>::kWalkThreads), 2) void decay_walk(WalkArgs a)
