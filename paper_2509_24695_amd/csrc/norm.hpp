@@ -116,6 +116,7 @@ struct NormPlace {
     }
 };
 
+// (d == 0: nothing, zeros)
 template <typename T, int LANES, int VECS> __device__ __forceinline__ void load_row(const void *base, int64_t at, int lane, int d, u32x4 (&v)[VECS])
 {
     const T *p = static_cast<const T *>(base) + at;
@@ -215,8 +216,11 @@ template <typename T, int LANES, int VECS, bool PARAMS> __global__ __launch_boun
     float nmean, nrstd;
     auto request = [&](int64_t row) {
         const NormPlace p(a, walk.group, row < last ? row : last);
-        load_row<T, LANES, VECS>(a.x, p.a, walk.lane, a.d, nx);
-        load_row<T, LANES, VECS>(a.dy, p.b, walk.lane, a.d, ndy);
+        // a row past the last is one of zeros: the last row's gradient times nothing would be NaN where that gradient is infinite, and dX may
+        // already have taken its place
+        const int d = row <= last ? a.d : 0;
+        load_row<T, LANES, VECS>(a.x, p.a, walk.lane, d, nx);
+        load_row<T, LANES, VECS>(a.dy, p.b, walk.lane, d, ndy);
         nmean = a.mean[p.stat];
         nrstd = a.rstd[p.stat];
     };
@@ -246,7 +250,7 @@ template <typename T, int LANES, int VECS, bool PARAMS> __global__ __launch_boun
                 along = __builtin_fmaf(t, xh, along);
                 if (PARAMS) {
                     dw[i][e] = __builtin_fmaf(g[e], xh, dw[i][e]);
-                    db[i][e] += live ? g[e] : 0.f;
+                    db[i][e] += g[e];
                 }
             }
         }
