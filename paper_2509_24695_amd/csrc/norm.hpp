@@ -154,13 +154,17 @@ template <typename T, int LANES, int VECS> __global__ __launch_bounds__((NormWal
     const float over = 1.f / (float)a.d;
     const int64_t last = a.rows - 1;
     u32x4 next[VECS];
-    load_row<T, LANES, VECS>(a.x, NormPlace(a, walk.group, walk.row < last ? walk.row : last).a, walk.lane, a.d, next);
+    // (nothing of a row past the last, which another workgroup may be writing where Y is X)
+    auto request = [&](int64_t row) {
+        load_row<T, LANES, VECS>(a.x, NormPlace(a, walk.group, row < last ? row : last).a, walk.lane, row <= last ? a.d : 0, next);
+    };
+    request(walk.row);
     for (int64_t at = first; at < a.rows; at += walk.step) {
-        const int64_t row = at + threadIdx.x / LANES, ahead = row + walk.step;
+        const int64_t row = at + threadIdx.x / LANES;
         u32x4 v[VECS];
 #pragma unroll
         for (int i = 0; i < VECS; ++i) v[i] = next[i];
-        if (at + walk.step < a.rows) load_row<T, LANES, VECS>(a.x, NormPlace(a, walk.group, ahead < last ? ahead : last).a, walk.lane, a.d, next);
+        if (at + walk.step < a.rows) request(row + walk.step);
         float sum = 0.f, x[VECS][kN];
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
