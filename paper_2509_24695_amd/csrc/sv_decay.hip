@@ -13,10 +13,6 @@ namespace {
 using namespace sv;
 
 constexpr int64_t kMostHeads = 1 << 24;
-// The memory side's cache.  A call whose k and v do not fit there reads its tokens past the caches in the walk, as nothing of them is met again (us
-// so / else: 64 heads of 75 600 tokens of 64 697 / 727, 20 of 32 760 of 112 227 / 232); a smaller one finds there what the sums have read (32 heads
-// of 4 680 tokens of 128 75.4 / 70.9, 7 x 8 of up to 1 501 49.4 / 44.9).
-constexpr int64_t kLastCacheBytes = (int64_t)256 << 20;
 constexpr int kBackwardWalks = 3;              // dq, dv and dk, in one launch
 
 bool overlaps(const void *a, const void *b, size_t bytes)
@@ -73,7 +69,7 @@ template <typename T, int D> sv_status run_walk(WalkArgs sums, const WalkArgs &w
         if (launched() != SV_OK) return SV_ERR_LAUNCH;
     }
     const unsigned grid = decay_grid(walks.problems * BH * walks.segments, walks.together);
-    if (walks.problems == 1 && (int64_t)2 * BH * walks.N * D * (int)sizeof(T) > kLastCacheBytes)
+    if (decay_past_caches(BH, walks.N, D, (int)sizeof(T), walks.problems))
         decay_walk<T, D, true><<<grid, W::kWalkThreads, 0, stream>>>(walks);
     else
         decay_walk<T, D, false><<<grid, W::kWalkThreads, 0, stream>>>(walks);
