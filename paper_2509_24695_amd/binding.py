@@ -181,6 +181,8 @@ class _CtypesCalls:
         fn = getattr(self._functions, name)
         types, last = fn.argtypes, len(fn.argtypes) - 1
         flag = 6 - (types[3] is ctypes.c_int32) if name.startswith("sv_linattn_state") else -1      # `accumulate`
+        if name == "sv_rope3d_rotate":
+            flag = 5                                                                                # `inverse`
 
         def convert(args, i):
             x, t = args[i], types[i]
