@@ -86,12 +86,13 @@ inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walk
 }
 
 // The memory side's cache.  A prompt whose k and v do not fit there reads its tokens past the caches in the walk, as nothing of them is met again (us
-// so / else: 64 heads of 75 600 tokens of 64 697 / 727, 20 of 32 760 of 112 227 / 232); a smaller one finds there what the sums have read (32 heads
-// of 4 680 tokens of 128 75.4 / 70.9, 7 x 8 of up to 1 501 49.4 / 44.9).
+// so / else: 64 heads of 75 600 tokens of 64 656 / 688, 16 of 128 420 / 432, 20 of 112, heads outside tokens, 482 / 488); a smaller one finds there
+// what the sums have read (32 heads of 4 680 tokens of 128 79.0 / 71.5, of 64 44.5 / 38.0, 7 x 8 of up to 1 501 of 128 52.1 / 49.0), and heads that
+// share lines find each other's (views of one projection's output, 20 heads of 75 600 tokens of 112 561 / 531, 40 of 32 760 473 / 459).
 constexpr int64_t kLastCacheBytes = (int64_t)256 << 20;
-inline bool decay_past_caches(int64_t BH, int n_tokens, int d, int elem_bytes, int walks)
+inline bool decay_past_caches(int64_t BH, int n_tokens, int d, int elem_bytes, int walks, bool shares_lines)
 {
-    return walks == 1 && 2 * BH * n_tokens * d * elem_bytes > kLastCacheBytes;
+    return walks == 1 && !shares_lines && 2 * BH * n_tokens * d * elem_bytes > kLastCacheBytes;
 }
 
 // The chunks of one sequence of `length` tokens: whole ones at its end, so that every chunk's last row is a token and only the first

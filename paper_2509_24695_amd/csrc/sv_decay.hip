@@ -69,7 +69,7 @@ template <typename T, int D> sv_status run_walk(WalkArgs sums, const WalkArgs &w
         if (launched() != SV_OK) return SV_ERR_LAUNCH;
     }
     const unsigned grid = decay_grid(walks.problems * BH * walks.segments, walks.together);
-    if (decay_past_caches(BH, walks.N, D, (int)sizeof(T), walks.problems))
+    if (decay_past_caches(BH, walks.N, D, (int)sizeof(T), walks.problems, walks.together > 1))
         decay_walk<T, D, true><<<grid, W::kWalkThreads, 0, stream>>>(walks);
     else
         decay_walk<T, D, false><<<grid, W::kWalkThreads, 0, stream>>>(walks);
@@ -95,8 +95,8 @@ WalkArgs walk_args(const Shape &s, const float *log_decay, const int32_t *length
     a.segments = plan.segments;
     a.per_segment = plan.per_segment;
     a.problems = problems;
-    // four neighbouring heads that share lines on one die (20 heads of 32 760
-    // tokens of 112 228 us, dealt singly 234; backward of 2 x 20 heads of 14 040 418 and 423)
+    // four neighbouring heads that share lines on one die (20 heads of 32 760 tokens of 112 247 us, dealt singly 249; backward of 2 x 20 heads of
+    // 14 040 446 and 454)
     a.together = TokenLayout{s.BH, s.H, s.d, s.elem_bytes, s.st.h, s.st.n}.shares_lines() ? 4 : 1;
     return a;
 }

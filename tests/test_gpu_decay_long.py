@@ -21,9 +21,10 @@ PROMPTS = [
     (2, 32, 33000, 32, "bf16", "bhnd", [33000, 20011], True),
     (1, 32, 33001, 64, "bf16", "bhnd", None, True),
     (1, 20, 30001, 112, "bf16", "packed", None, False),
+    (1, 20, 30001, 112, "bf16", "bhnd", None, True),
     (2, 8, 33001, 128, "bf16", "bnhd", [32700, 33001], True),
     (1, 16, 33001, 64, "f32", "packed", None, True),
-    (1, 10, 33001, 112, "f32", "bnhd", None, True),
+    (1, 10, 33001, 112, "f32", "bhnd", None, True),
     (1, 8, 33001, 128, "f32", "bhnd", None, False),
 ]
 BACKWARDS = [
