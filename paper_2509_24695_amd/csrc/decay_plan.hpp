@@ -51,7 +51,7 @@ inline double decay_time(const DecayCost &cost, int64_t BH, int segments, int pe
 
 // States that the segments of all heads together begin from: no more than this, where there are fewer heads (eight workgroups of a walk on a compute
 // unit, four at d > 64; twice the figure, or none, gains nothing, half of it costs up to 33 %).  A call with fewer batches, heads or tokens
-// needs no more than one with more.
+// needs no more than one with more.  (With as many heads or more a call is one segment and touches none of them.)
 inline int64_t decay_slots(int64_t BH, int n_tokens, int d, int walks)
 {
     const int64_t most = (d <= 64 ? 2048 : 1024) / walks, chunks = ((int64_t)n_tokens + kDecayChunkF32 - 1) / kDecayChunkF32;
@@ -60,9 +60,11 @@ inline int64_t decay_slots(int64_t BH, int n_tokens, int d, int walks)
 }
 
 // The cut that takes least by decay_time.  Its figures were fitted to the times of 178 calls (both directions and types, d of 32 to 128, 2 to 224
-// heads, 100 to 75 600 tokens) each cut into one to 128 segments: over them it takes 1.6 % longer than the best cut of each, at most 13 %, where
-// "as many workgroups as run at once, segments of two chunks or more" takes 12 %, at most 87 %.  us, in one segment / as many as run at once /
-// this: bf16, d = 128, 224 heads of 2 400 tokens 170 / 190 / 170, 64 heads of 150 17.9 / 28.8 / 17.9, 4 heads of 600 42.7 / 23.6 / 20.3.
+// heads, 100 to 75 600 tokens) each cut into one to 128 segments, with kernels that took the scores in one piece and the sums to their
+// end: 1.6 % longer than the best cut of each, at most 13 %, where "as many workgroups as run at once, segments of two chunks or more" took
+// 12 %, at most 87 %.  On the present kernels, 157 calls (2 to 224 heads, 100 to 32 760 tokens, memories of one token to a thousand): 1.4 % longer than the
+// best cut, at most 16 % (backward, d = 32, 224 heads of 2 400 tokens 100 us, one segment 86); 39 of them with memories of 10 000 tokens: 0.8
+// %, at most 9 %.
 inline DecayPlan decay_plan(int64_t BH, int n_tokens, int d, int chunk, int walks)
 {
     const int chunks = (int)(((int64_t)n_tokens + chunk - 1) / chunk);

@@ -4,8 +4,12 @@
 //
 // A call moves the states, 2 d^2 fp32 per row and head, and next to nothing else: a workgroup takes the columns of one head's state
 // (all, or a quarter where there are few heads), each thread a column group of four of every R-th row, all of its loads in flight at once.
-// 187 rows of 16 heads of 128: 395 MB in 60 us, 6.6 TB/s.  States that go to another pool are written past the caches (81 us without the hint);
-// states that are written in place are not (61 us with it, 59 without).
+// 187 rows of 16 heads of 128, 395 MB, with pools that change from call to call: 79 us, 5.0 TB/s (60 on one pair of pools, part of which
+// the 256 MB cache then holds).  States that go to another pool are written past the caches (82.5 us without the hint); states that are written in
+// place are not (86 us, on one pool 61 with the hint and 59 without).
+//
+// Row b looks through the slots of the rows before it: 4 b bytes for each of its heads.  256 rows of 16 heads of 128 87 us, without slots 86; 16 384 of 16
+// heads of 64 1 871 and 1 581; 16 384 of 2 heads of 32, whose states are as many bytes as that, 124 and 45.
 #pragma once
 
 #include "common.hpp"

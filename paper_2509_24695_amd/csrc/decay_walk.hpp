@@ -20,10 +20,10 @@
 //
 // One workgroup walks one segment of one head's sequence, a wave per 32 value features: the wave keeps its 32 columns of S as fp32
 // accumulators over the whole segment.  The chunk's C x C products are the same for all of the workgroup's waves: at bf16 and four waves each
-// wave works one of the three 32 x 32 tiles out for all (32 760 tokens of 20 heads of 112 228 us, every wave for itself, 24 of its 94 matrix
-// instructions, 243; 7 x 8 heads of up to 1 501 tokens of 128 46 and 51), at fp32 each adds up a part of the features (4 680 tokens of 32 heads
-// of 64 73.6 us, every wave for itself 76.5; 8 000 tokens of 20 heads of 112 176 and 195), at bf16 with fewer waves every wave has its own
-// (4 680 tokens of 32 heads of 64, backward: 60 us, shared 72).
+// wave works one of the three 32 x 32 tiles out for all (with scores in one piece: 32 760 tokens of 20 heads of 112 228 us, every wave for itself,
+// 24 of its 94 matrix instructions, 243; 7 x 8 heads of up to 1 501 tokens of 128 46 and 51; with two pieces the latter would not fit the registers), at fp32
+// each adds up a part of the features (4 680 tokens of 32 heads of 64 73.2 us, every wave for itself 76.6; 8 000 tokens of 20 heads of 112 195
+// and 216), at bf16 with fewer waves every wave has its own (4 680 tokens of 32 heads of 64, backward, with scores in one piece: 60 us, shared 72).
 //
 // Products are arranged so that a product's accumulators are the next one's operands as they lie: the lane of a 32 x 32 accumulator holds rows
 // 8 (r / 4) + 4 h + r % 4 of one column, the lane of an operand eight consecutive indices 8 h .. 8 h + 7 of the contraction, so rows are dealt to
@@ -34,16 +34,17 @@
 // 2.4e-3 off.  Scores in one: 2.3e-3 off for heads that remember up to some twenty tokens, 1.8e-3 over heads that remember 1 to 1 000; us with two / one:
 // 32 760 tokens of 20 heads of 112 243 / 236, 75 600 of 64 heads of 64 644 / 639, backward pass of 4 680 of 32 heads of 64 66.4 / 62.5, 300 tokens of 224
 // heads of 64 18.0 / 16.8.)  A state that the caller gets is an fp32 one: what goes into it, in the sums and in the last segment's walk, is in
-// three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; 246 us and 233).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix
+// three pieces (2.7e-7 off after 32 760 tokens, with two 2.4e-6; with scores in one piece 246 us and 233).  fp32 tokens: fp32 products throughout (32 x 32 x 2 matrix
 // instructions).
 //
 // A call of several segments is three launches: what each segment adds to the state, the scan over a head's segments, the walk.  It reads k and v
-// twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.2 that do) 637 us = 180 + 8 + 450, 5.0
-// TB/s, as much as a copy of that size reaches (4.9): the walk is bound by memory, the sums by the heads that forget nothing.  Heads of 112 whose
-// rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.88) take 233 us = 70 + 10 + 150: rows of 224 bytes begin and end inside lines of 128,
-// and the walk alone without its products takes 138 us, without its memory accesses 114.  Calls that give each compute unit one or two workgroups
-// are bound by a chunk's own run through LDS and the matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
-// Measured and left: LDS rows whose 16-byte pieces change places, so that no read conflicts (of decay_sums' LDS cycles at d = 112 62 % are
+// twice, but for what weighs nothing any more: 64 heads of 75 600 tokens of 64 (2.5 GB that must move, 3.2 that do, where memories run from one token to
+// a thousand) 640 to 658 us by device, 4.9 to 5.1 TB/s, as much as a copy of that size reaches: the walk is bound by memory, the sums by the heads that
+// forget nothing (710 to 717 us where none forgets).  Heads of 112 whose rows lie between others' (32 760 tokens of 20; 0.59 GB, 0.82) take 236 to 248
+// us (245 to 251): rows of 224 bytes begin and end inside lines of 128, the walk's reads are 1.13 times its bytes, and the walk alone took 138
+// of 150 us without its products, 114 without its memory accesses (scores in one piece).  Calls that give each compute unit one or two
+// workgroups are bound by a chunk's own run through LDS and the matrix cores (2.4 us at d = 64, 3.5 at 128; decay_plan.hpp).
+// Measured with scores in one piece, and left: LDS rows whose 16-byte pieces change places, so that no read conflicts (of decay_sums' LDS cycles at d = 112 62 % are
 // conflicts, the walk's 39 %): 1 to 3 % slower by the addresses' arithmetic, as LDS is busy for a sixth of the time; two chunks' rows on their way
 // in decay_sums (the same, +-2 %) or in the walk (one workgroup less on a compute unit: 289 us instead of 252); heads in groups whose k and v fit
 // the memory side's cache, one group after the other (702 us instead of 718).

@@ -6,8 +6,9 @@
 // Bound by memory: a row is read once into registers (16 bytes per lane and piece), its sums go across the lanes that hold it, and it is
 // written from there, while the next one is on its way (two and four rows at a time gained nothing).  A lane keeps the same features for all
 // rows that its workgroup walks, so the parameters stay in registers too, and the backward pass adds up dw and db of its features there: a
-// workgroup leaves one partial sum of each, norm_fold adds these up in order.  32 760 rows of 2 240 features of bf16: forwards 48 us, backwards 93
-// (440 MB, 4.7 TB/s, the fold of 9 MB of partial sums included).
+// workgroup leaves one partial sum of each, norm_fold adds these up in order.  32 760 rows of 2 240 features, with buffers that change from
+// call to call: bf16 forwards 55 us (294 MB, 5.4 TB/s), backwards 88 (441 MB, 5.0 TB/s, the fold of 9 MB of partial sums included), fp32 111 (587 MB, 5.3
+// TB/s) and 157 (881 MB, 5.6 TB/s).
 #pragma once
 
 #include "common.hpp"

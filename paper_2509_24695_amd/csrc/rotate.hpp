@@ -3,8 +3,8 @@
 // A copy with four multiplications per pair: bound by memory.  A thread owns 16 bytes of one token's rows (four pairs of bf16, two of fp32),
 // works the token's place out and fetches its angles once, and then runs over the heads, first of q, then of k, whose rows all take the
 // same angles.  Sixteen heads at a time (32 760 tokens of 20 heads of 112, views of one projection's output, 587 MB: 122 us, 4.8 TB/s; four at a
-// time 132).  Heads that share no cache lines are written past the caches (3 519 tokens of 3 x 16 heads of 128 in fp32 50 us, 6.6 TB/s, without the
-// hint 61); heads that do, do without (133 with it).
+// time 132).  Heads that share no cache lines are written past the caches (with buffers that change from call to call 3 519 tokens of 3 x 16 heads of
+// 128 in fp32 63.4 us, 5.2 TB/s, without the hint 65.9; 32 760 tokens of 32 heads of 64 104.3 and 106.6); heads that do, do without (133 with it).
 #pragma once
 
 #include "common.hpp"
