@@ -15,4 +15,5 @@ from .binding import (  # noqa: F401
     sv_mfma_stream, sv_measure_tconv_variant,
     sv_decay_linattn_workspace_bytes, sv_decay_linattn_backward_workspace_bytes, sv_decay_linattn, sv_decay_linattn_token,
     sv_decay_linattn_backward, sv_rope3d_rotate, sv_layernorm, sv_layernorm_backward_workspace_bytes, sv_layernorm_backward,
+    sv_causal_conv, sv_causal_conv_token, sv_causal_conv_backward_workspace_bytes, sv_causal_conv_backward,
 )

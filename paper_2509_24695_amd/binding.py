@@ -3,7 +3,7 @@ the module _sventry (csrc/py_entry.cpp), which takes 1.2 us per call for it wher
 for one interpreter; another one that imports the package makes these calls through ctypes as well.
 
 The functions carry the names and argument order of the C ABI
-(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_rope.h, include/sv_norm.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
+(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_rope.h, include/sv_norm.h, include/sv_conv.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
 device addresses); nothing here computes, and there is no fallback: if the
 shared library is missing, loading raises.
 """
@@ -30,6 +30,7 @@ EXPORTS = (
     "sv_decay_linattn_workspace_bytes", "sv_decay_linattn_backward_workspace_bytes", "sv_decay_linattn",
     "sv_decay_linattn_token", "sv_decay_linattn_backward", "sv_rope3d_rotate", "sv_layernorm",
     "sv_layernorm_backward_workspace_bytes", "sv_layernorm_backward",
+    "sv_causal_conv", "sv_causal_conv_token", "sv_causal_conv_backward_workspace_bytes", "sv_causal_conv_backward",
 )
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -128,6 +129,13 @@ def load_library():
     lib.sv_layernorm_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.sv_layernorm_backward_workspace_bytes.restype = sz
     lib.sv_layernorm_backward.argtypes = [vp, dp, vp, dp, vp, i32, vp, vp, vp, dp, vp, vp, vp, sz, vp]
+    lib.sv_causal_conv.argtypes = [vp, dp, vp, vp, i32, i32, vp, vp, vp, vp, dp, vp]
+    lib.sv_causal_conv_token.argtypes = [vp, dp, vp, vp, i32, i32, vp, i32, vp, vp, vp, dp, vp]
+    lib.sv_causal_conv_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.sv_causal_conv_backward_workspace_bytes.restype = sz
+    lib.sv_causal_conv_backward.argtypes = [vp, dp, vp, dp, vp, vp, i32, i32, vp, vp, vp, vp, dp, vp, vp, vp, vp, sz, vp]
+    for f in (lib.sv_causal_conv, lib.sv_causal_conv_token, lib.sv_causal_conv_backward):
+        f.restype = ctypes.c_int
     for f in (lib.sv_decay_linattn, lib.sv_decay_linattn_token, lib.sv_decay_linattn_backward, lib.sv_rope3d_rotate, lib.sv_layernorm,
               lib.sv_layernorm_backward):
         f.restype = ctypes.c_int
@@ -181,8 +189,7 @@ class _CtypesCalls:
         fn = getattr(self._functions, name)
         types, last = fn.argtypes, len(fn.argtypes) - 1
         flag = 6 - (types[3] is ctypes.c_int32) if name.startswith("sv_linattn_state") else -1      # `accumulate`
-        if name == "sv_rope3d_rotate":
-            flag = 5                                                                                # `inverse`
+        flag = {"sv_rope3d_rotate": 5, "sv_causal_conv": 5, "sv_causal_conv_token": 5, "sv_causal_conv_backward": 7}.get(name, flag)   # `inverse`, `silu`
 
         def convert(args, i):
             x, t = args[i], types[i]
@@ -461,6 +468,32 @@ def sv_layernorm_backward(X, x: TensorDesc, dY, dy: TensorDesc, weight, weight_h
         workspace_bytes = 0
     _check((_entry or _calls()).sv_layernorm_backward(X, x, dY, dy, weight, weight_heads, mean, rstd, dX, dx, dweight, dbias, workspace,
                                                       workspace_bytes, stream), "sv_layernorm_backward")
+
+
+def sv_causal_conv(X, x: TensorDesc, weight, bias, taps: int, silu, lengths, cache_in, cache_out, Y, y: TensorDesc, stream=None) -> None:
+    """Short causal convolution of each channel along tokens, with its activation (include/sv_conv.h): weight [taps][H][d], bias [H][d]
+    fp32, lengths [B] int32 or None, caches [B][H][taps-1][d] or None."""
+    _check((_entry or _calls()).sv_causal_conv(X, x, weight, bias, taps, silu, lengths, cache_in, cache_out, Y, y, stream), "sv_causal_conv")
+
+
+def sv_causal_conv_token(X, x: TensorDesc, weight, bias, taps: int, silu, slots, n_slots: int, cache_in, cache_out, Y, y: TensorDesc,
+                         stream=None) -> None:
+    """The same for one token of each row of a batch, on caches of a pool [n_slots][H][taps-1][d]: slots [B] int32 or None."""
+    _check((_entry or _calls()).sv_causal_conv_token(X, x, weight, bias, taps, silu, slots, n_slots, cache_in, cache_out, Y, y, stream),
+           "sv_causal_conv_token")
+
+
+def sv_causal_conv_backward_workspace_bytes(B: int, H: int, n_tokens: int, d: int) -> int:
+    return int(load_library().sv_causal_conv_backward_workspace_bytes(int(B), int(H), int(n_tokens), int(d)))
+
+
+def sv_causal_conv_backward(X, x: TensorDesc, dY, dy: TensorDesc, weight, bias, taps: int, silu, lengths, cache_in, dcache_out, dX,
+                            dx: TensorDesc, dcache_in, dweight, dbias, workspace, workspace_bytes: int | None = None, stream=None) -> None:
+    """Gradients of sv_causal_conv for X, weight, bias and cache_in (include/sv_conv.h)."""
+    if workspace is None and workspace_bytes is None:
+        workspace_bytes = 0
+    _check((_entry or _calls()).sv_causal_conv_backward(X, x, dY, dy, weight, bias, taps, silu, lengths, cache_in, dcache_out, dX, dx, dcache_in,
+                                                        dweight, dbias, workspace, workspace_bytes, stream), "sv_causal_conv_backward")
 
 
 def sv_measure_apply_variant(variant: int, Q, q: TensorDesc, tok_begin: int, tok_end: int, S, z, eps: float, O,

@@ -1,0 +1,341 @@
+// Short causal convolution of each channel along tokens, and its backward pass.
+//
+//   a_t = bias + sum_j W[j] x_{t-(K-1)+j},  y = a or silu(a);   da = dy or dy silu'(a)
+//   dx_t = sum_j W[j] da_{t+(K-1)-j},  dW[j] = sum da_t x_{t-(K-1)+j},  db = sum da_t
+//
+// Bound by memory: a thread owns one 16-byte piece of the channels, whose taps it keeps in registers, and walks a run of tokens with the last
+// K-1 of them in registers too, so that a token is read once (and K-1 more times at the runs' edges, out of the caches).
+#pragma once
+
+#include "activation.hpp"
+#include "common.hpp"
+#include "conv_plan.hpp"
+#include "piece.hpp"
+
+namespace sv {
+
+struct ConvArgs {
+    const void *x, *dy;
+    void *y;                           // backward: dx
+    TokStrides sx, sdy, sy;
+    const float *weight, *bias;
+    const int32_t *lengths;            // or NULL; tokens: slots
+    const void *cache_in, *dcache_out;
+    void *cache_out;                   // backward: dcache_in
+    float *partial;
+    int B, H, N, d, run, runs;         // runs of a sequence (backward: workgroups along one)
+    int across, n_slots;
+    int silu, whole_lines;
+    NormDivisor pieces, head_pieces, run_div;
+};
+
+// A thread's channels: head, feature, and place among all channels.
+template <typename T> struct ConvPlace {
+    int h, i, c;
+    __device__ __forceinline__ ConvPlace(const ConvArgs &a, uint32_t piece)
+    {
+        h = (int)a.head_pieces.quotient(piece);
+        i = (int)(piece - (uint32_t)h * a.head_pieces.extent) * Piece<T>::kN;
+        c = h * a.d + i;
+    }
+};
+
+template <int N> __device__ __forceinline__ void load_floats(const float *p, float (&x)[N])
+{
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(p + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * q + e] = v[e];
+    }
+}
+
+// Taps and bias of a piece.
+template <typename T, int K> struct ConvWeights {
+    static constexpr int kN = Piece<T>::kN;
+    float w[K][kN], b[kN];
+    __device__ __forceinline__ ConvWeights(const ConvArgs &a, int c)
+    {
+        const int64_t channels = (int64_t)a.H * a.d;
+#pragma unroll
+        for (int j = 0; j < K; ++j) load_floats<kN>(a.weight + j * channels + c, w[j]);
+        if (a.bias) load_floats<kN>(a.bias + c, b);
+        else
+#pragma unroll
+            for (int e = 0; e < kN; ++e) b[e] = 0.f;
+    }
+    // a_t from the K - 1 tokens before t and t itself
+    __device__ __forceinline__ float mix(const float (&before)[K - 1][kN], const float (&now)[kN], int e) const
+    {
+        float s = b[e];
+#pragma unroll
+        for (int j = 0; j < K - 1; ++j) s = __builtin_fmaf(w[j][e], before[j][e], s);
+        return __builtin_fmaf(w[K - 1][e], now[e], s);
+    }
+};
+
+// Row m of the cache and the tokens one after the other (m = 0: the cache's first); nothing where there is neither.
+template <typename T, int K>
+__device__ __forceinline__ u32x4 conv_row(const ConvArgs &a, const T *x, const void *cache, int64_t cache_at, int64_t m, int length)
+{
+    if (m < K - 1) return cache ? *reinterpret_cast<const u32x4 *>(static_cast<const T *>(cache) + cache_at + m * a.d) : u32x4{0u, 0u, 0u, 0u};
+    const int64_t t = m - (K - 1);
+    return t < length ? *reinterpret_cast<const u32x4 *>(x + t * a.sx.n) : u32x4{0u, 0u, 0u, 0u};
+}
+
+template <int K, int N> __device__ __forceinline__ void conv_shift(float (&w)[K][N], const float (&now)[N])
+{
+#pragma unroll
+    for (int j = 0; j + 1 < K; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[j][e] = w[j + 1][e];
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[K - 1][e] = now[e];
+}
+
+__device__ __forceinline__ int held_length(const int32_t *lengths, int b, int N)
+{
+    if (!lengths) return N;
+    const int n = lengths[b];
+    return n < 0 ? 0 : n > N ? N : n;
+}
+
+template <typename T, int K, bool SILU> __global__ __launch_bounds__(kConvThreads) void conv_rows(ConvArgs a)
+{
+    constexpr int kN = Piece<T>::kN, kAhead = 4;
+    const uint32_t id = blockIdx.x * kConvThreads + threadIdx.x, all = a.pieces.quotient(id), piece = id - all * a.pieces.extent;
+    const uint32_t b = a.run_div.quotient(all), run = all - b * a.run_div.extent;
+    if ((int)b >= a.B) return;
+    const int length = held_length(a.lengths, (int)b, a.N);
+    const int64_t first = (int64_t)run * a.run, last = first + a.run < length ? first + a.run : length;
+    if (first >= length && run > 0) return;
+    const ConvPlace<T> at(a, piece);
+    const T *x = static_cast<const T *>(a.x) + b * a.sx.b + at.h * a.sx.h + at.i;
+    T *y = static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i;
+    const int64_t cache_at = ((int64_t)b * a.H + at.h) * (K - 1) * a.d + at.i;
+    u32x4 next[kAhead] = {};
+    auto request = [&](int64_t t) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (t + i < last) next[i] = *reinterpret_cast<const u32x4 *>(x + (t + i) * a.sx.n);
+    };
+    request(first);
+    float before[K - 1][kN];
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) Piece<T>::open(conv_row<T, K>(a, x, a.cache_in, cache_at, first + j, length), before[j]);
+    const ConvWeights<T, K> w(a, at.c);
+    for (int64_t t = first; t < last; t += kAhead) {
+        u32x4 v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = next[i];
+        request(t + kAhead);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            float now[kN], out[kN];
+            Piece<T>::open(v[i], now);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                out[e] = w.mix(before, now, e);
+                if (SILU) out[e] = silu(out[e]);
+            }
+            if (t + i < last) store16(y + (t + i) * a.sy.n, Piece<T>::close(out), a.whole_lines);
+            conv_shift(before, now);
+        }
+    }
+    // the run that read the old cache writes the new one, which may be the same memory
+    if (run == 0 && a.cache_out) {
+        u32x4 rows[K - 1];
+#pragma unroll
+        for (int r = 0; r < K - 1; ++r) rows[r] = conv_row<T, K>(a, x, a.cache_in, cache_at, (int64_t)length + r, length);
+#pragma unroll
+        for (int r = 0; r < K - 1; ++r) *reinterpret_cast<u32x4 *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r];
+    }
+}
+
+// Has an earlier row of the batch the same slot?  For all threads of a workgroup.
+__device__ __forceinline__ bool slot_taken(const int32_t *slots, int b, int slot)
+{
+    bool taken = false;
+    if (slots)
+        for (int r = threadIdx.x; r < b; r += blockDim.x) taken |= slots[r] == slot;
+    return __syncthreads_or(taken);
+}
+
+// One token of each row of a batch: a workgroup has `across` pieces of one row.
+template <typename T, int K, bool SILU> __global__ __launch_bounds__(kConvThreads) void conv_token(ConvArgs a)
+{
+    constexpr int kN = Piece<T>::kN;
+    const int b = (int)(blockIdx.x / a.runs);
+    const uint32_t piece = blockIdx.x % a.runs * a.across + threadIdx.x;
+    const int slot = a.lengths ? a.lengths[b] : b;
+    if (slot < 0 || slot >= a.n_slots) return;
+    const bool mine = threadIdx.x < (unsigned)a.across && piece < a.pieces.extent;
+    const ConvPlace<T> at(a, mine ? piece : 0);
+    const int64_t cache_at = ((int64_t)slot * a.H + at.h) * (K - 1) * a.d + at.i;
+    const T *x = static_cast<const T *>(a.x) + b * a.sx.b + at.h * a.sx.h + at.i;
+    u32x4 rows[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) rows[j] = conv_row<T, K>(a, x, a.cache_in, cache_at, j, 1);
+    const ConvWeights<T, K> w(a, at.c);
+    if (slot_taken(a.lengths, b, slot) || !mine) return;
+    float before[K - 1][kN], now[kN], out[kN];
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) Piece<T>::open(rows[j], before[j]);
+    Piece<T>::open(rows[K - 1], now);
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+        out[e] = w.mix(before, now, e);
+        if (SILU) out[e] = silu(out[e]);
+    }
+    *reinterpret_cast<u32x4 *>(static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i) = Piece<T>::close(out);
+#pragma unroll
+    for (int r = 0; r < K - 1; ++r) *reinterpret_cast<u32x4 *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r + 1];
+}
+
+// dx of a run of tokens (of the cache too, for a sequence's first run), and the workgroup's part of dW and db.  With da_t known for the last
+// K tokens, row m of cache and tokens together gets sum_j W[j] da_{m-j}; so a run goes on for K - 1 tokens of the next.
+template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds__(kConvThreads) void conv_rows_backward(ConvArgs a)
+{
+    constexpr int kN = Piece<T>::kN, kAhead = 4;
+    const uint32_t tiles = (a.pieces.extent + a.across - 1) / a.across, tile = blockIdx.x % tiles, rest = blockIdx.x / tiles;
+    const int block = (int)(rest % a.runs), b = (int)(rest / a.runs), down = kConvThreads / a.across;
+    const int col = (int)threadIdx.x % a.across, line = (int)threadIdx.x / a.across;
+    const uint32_t piece = tile * a.across + col;
+    const bool mine = piece < a.pieces.extent;
+    const int length = held_length(a.lengths, b, a.N);
+    const int64_t run = (int64_t)block * down + line, first = run * a.run, last = first + a.run < length ? first + a.run : length;
+    const ConvPlace<T> at(a, mine ? piece : 0);
+    float dw[K][kN], db[kN];
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+        db[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < K; ++j) dw[j][e] = 0.f;
+    }
+    if (mine && (first < length || run == 0)) {
+        const T *x = static_cast<const T *>(a.x) + b * a.sx.b + at.h * a.sx.h + at.i;
+        const T *dy = static_cast<const T *>(a.dy) + b * a.sdy.b + at.h * a.sdy.h + at.i;
+        T *dx = static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i;
+        const int64_t cache_at = ((int64_t)b * a.H + at.h) * (K - 1) * a.d + at.i;
+        const T *dcache_out = a.dcache_out ? static_cast<const T *>(a.dcache_out) + cache_at : nullptr;
+        T *dcache_in = a.cache_out ? static_cast<T *>(a.cache_out) + cache_at : nullptr;
+        const int64_t end = last + K - 1, live = end < length ? end : length;      // rows [first, end) of da, tokens up to `live`
+        u32x4 nx[kAhead], ndy[kAhead];
+        auto request = [&](int64_t t) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                nx[i] = ndy[i] = u32x4{0u, 0u, 0u, 0u};
+                if (t + i < live) {
+                    nx[i] = *reinterpret_cast<const u32x4 *>(x + (t + i) * a.sx.n);
+                    ndy[i] = *reinterpret_cast<const u32x4 *>(dy + (t + i) * a.sdy.n);
+                }
+            }
+        };
+        request(first);
+        float before[K - 1][kN], da[K][kN];
+#pragma unroll
+        for (int j = 0; j < K - 1; ++j) Piece<T>::open(conv_row<T, K>(a, x, a.cache_in, cache_at, first + j, length), before[j]);
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int e = 0; e < kN; ++e) da[j][e] = 0.f;
+        const ConvWeights<T, K> w(a, at.c);
+        for (int64_t t = first; t < end; t += kAhead) {
+            u32x4 vx[kAhead], vdy[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                vx[i] = nx[i];
+                vdy[i] = ndy[i];
+            }
+            request(t + kAhead);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t m = t + i;                              // da_m is the newest that row m gets
+                float now[kN], g[kN], out[kN];
+                Piece<T>::open(vx[i], now);
+                Piece<T>::open(vdy[i], g);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    if (SILU) {
+                        const float y = w.mix(before, now, e);
+                        g[e] = m < live ? g[e] * silu_slope(y, sigmoid(y)) : 0.f;
+                    }
+                    if (PARAMS && m < last) {
+#pragma unroll
+                        for (int j = 0; j < K - 1; ++j) dw[j][e] = __builtin_fmaf(g[e], before[j][e], dw[j][e]);
+                        dw[K - 1][e] = __builtin_fmaf(g[e], now[e], dw[K - 1][e]);
+                        db[e] += g[e];
+                    }
+                }
+                conv_shift(da, g);
+                conv_shift(before, now);
+                const bool cached = m < K - 1, write = m < end && (cached ? run == 0 : m - (K - 1) >= first);
+                if (!write || (cached && !dcache_in)) continue;
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    out[e] = w.w[0][e] * da[K - 1][e];
+#pragma unroll
+                    for (int j = 1; j < K; ++j) out[e] = __builtin_fmaf(w.w[j][e], da[K - 1 - j][e], out[e]);
+                }
+                if (dcache_out && m >= length) {
+                    float more[kN];
+                    Piece<T>::open(*reinterpret_cast<const u32x4 *>(dcache_out + (m - length) * a.d), more);
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) out[e] += more[e];
+                }
+                if (cached) *reinterpret_cast<u32x4 *>(dcache_in + m * a.d) = Piece<T>::close(out);
+                else store16(dx + (m - (K - 1)) * a.sy.n, Piece<T>::close(out), a.whole_lines);
+            }
+        }
+    }
+    if constexpr (PARAMS) {
+        // lanes with the same channels are added up in order of their runs
+        __shared__ float sums[kConvThreads * kN];
+        const int64_t channels = (int64_t)a.H * a.d;
+        float *partial = a.partial + rest * channels * (K + 1);
+        const int width = a.across * kN;
+#pragma unroll
+        for (int j = 0; j <= K; ++j) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kN; ++e) sums[(line * kN + e) * a.across + col] = j < K ? dw[j < K ? j : 0][e] : db[e];
+            __syncthreads();
+            for (int q = threadIdx.x; q < width; q += kConvThreads) {
+                float s = sums[q];
+                for (int r = 1; r < down; ++r) s += sums[r * width + q];
+                const uint32_t p = tile * a.across + q % a.across;
+                if (p < a.pieces.extent) partial[j * channels + ConvPlace<T>(a, p).c + q / a.across] = s;
+            }
+        }
+    }
+}
+
+// Partial sums [parts][floats], added up in sixteen runs and these in order; the first `split` numbers go to one place, the rest to another.
+struct FoldArgs {
+    const float *partial;
+    int64_t parts, floats, split;
+    float *first, *second;             // either may be NULL
+};
+__global__ __launch_bounds__(256) void fold_parts(FoldArgs a)
+{
+    constexpr int kRuns = 16, kQuads = 16;
+    __shared__ f32x4 runs[kRuns][kQuads];
+    const int64_t quads = a.floats / 4, q = (int64_t)blockIdx.x * kQuads + threadIdx.x % kQuads;
+    const int run = threadIdx.x / kQuads;
+    const f32x4 *p = reinterpret_cast<const f32x4 *>(a.partial);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (q < quads) {
+#pragma unroll 8
+        for (int64_t w = run; w < a.parts; w += kRuns) s += p[w * quads + q];
+    }
+    runs[run][threadIdx.x % kQuads] = s;
+    __syncthreads();
+    if (run == 0 && q < quads) {
+#pragma unroll
+        for (int r = 1; r < kRuns; ++r) s += runs[r][threadIdx.x];
+        float *out = q * 4 < a.split ? a.first : a.second;
+        if (out) *reinterpret_cast<f32x4 *>(out + (q * 4 < a.split ? q * 4 : q * 4 - a.split)) = s;
+    }
+}
+
+}  // namespace sv

@@ -1,0 +1,48 @@
+// How a short causal convolution's tokens are dealt to threads.  Plain C++ (no device code), shared by the launchers and host-side tests.
+#pragma once
+
+#include <stdint.h>
+
+#include "norm_plan.hpp"
+
+namespace sv {
+
+// Forwards a thread owns one 16-byte piece of the channels and walks a run of tokens; threads are numbered pieces first, then runs.
+constexpr int kConvThreads = 256;
+inline int conv_run(int64_t BN, int pieces)
+{
+    for (int run = 32; run > 4; run /= 2)
+        if (BN * pieces / run >= (int64_t)256 * 1024) return run;
+    return 4;
+}
+
+// Backwards a workgroup is `across` pieces by `down` runs of tokens, so that one partial sum of the parameters' gradients is left for all
+// of its runs.
+struct ConvCut {
+    int across, down, run;             // run: tokens of a thread
+    int64_t tiles, blocks;             // workgroups across the channels; workgroups along one sequence
+};
+constexpr int kConvMostRun = 64;
+inline ConvCut conv_cut(int64_t B, int64_t N, int64_t pieces)
+{
+    ConvCut c{};
+    c.across = 32;
+    while (c.across > 4 && c.across / 2 >= pieces) c.across /= 2;
+    c.down = kConvThreads / c.across;
+    c.tiles = (pieces + c.across - 1) / c.across;
+    c.run = 4;
+    while (c.run < kConvMostRun && B * ((N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run)) * c.tiles > 1024) c.run *= 2;
+    c.blocks = (N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run);
+    return c;
+}
+// Partial sums of a call; and of the largest call with no more batches, tokens and channels: with more than 1 024 workgroups runs are as long as they
+// get, with fewer these leave at most 1 024 sums of 256 channels.
+inline int64_t conv_partial_floats(int64_t B, int64_t blocks, int64_t channels, int taps) { return B * blocks * channels * (taps + 1); }
+inline int64_t conv_workspace_floats(int64_t B, int64_t N, int64_t channels)
+{
+    const int64_t shortest = B * ((N + 31) / 32) * channels, longest = B * ((N + 511) / 512) * channels;
+    const int64_t most = longest > 1024 * 256 ? longest : 1024 * 256;
+    return 5 * (shortest < most ? shortest : most);
+}
+
+}  // namespace sv

@@ -71,4 +71,40 @@ inline sv_status check_desc(const sv_tensor_desc *t, Shape *s, bool any_width = 
     return SV_OK;
 }
 
+constexpr int64_t kMostHeads = 1 << 24;        // batches times heads of the operators that deal rows, not heads, to the grid
+constexpr int kMostRowWidth = 8192;            // features of their widest row
+
+// A tensor of rows of any width that is whole 16-byte pieces.
+inline sv_status check_rows(const sv_tensor_desc *t, Shape *s)
+{
+    const sv_status rc = check_desc(t, s, true, kMostHeads);
+    if (rc != SV_OK) return rc;
+    const int per = 16 / s->elem_bytes;
+    if (s->d <= 0 || s->d % per || s->d > kMostRowWidth) return SV_ERR_UNSUPPORTED;
+    return (int64_t)s->BH * s->N >= (int64_t)1 << 31 ? SV_ERR_SHAPE : SV_OK;
+}
+inline bool same_shape(const Shape &x, const Shape &y) { return x.B == y.B && x.H == y.H && x.N == y.N && x.d == y.d && x.bf16 == y.bf16; }
+inline bool same_rows(const Shape &x, const Shape &y) { return x.st.b == y.st.b && x.st.h == y.st.h && x.st.n == y.st.n; }
+
+// Is every row a run of whole 128-byte lines (given a tensor that begins with one)?
+inline bool lines_whole(const Shape &s)
+{
+    const int64_t line = 128 / s.elem_bytes;
+    return s.d % line == 0 && s.st.n % line == 0 && (s.H == 1 || s.st.h % line == 0) && (s.B == 1 || s.st.b % line == 0);
+}
+
+inline bool overlaps(const void *a, const void *b, size_t bytes)
+{
+    const auto pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    return a && b && pa < pb + bytes && pb < pa + bytes;
+}
+template <size_t N> bool all_aligned(const void *const (&p)[N])
+{
+    for (const void *x : p)
+        if (!aligned16(x)) return false;
+    return true;
+}
+
+inline sv_status launched() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
+
 }  // namespace sv

@@ -13,6 +13,7 @@
 
 #include "common.hpp"
 #include "norm_plan.hpp"
+#include "piece.hpp"
 
 namespace sv {
 
@@ -34,35 +35,6 @@ struct NormArgs {
     int d, groups, workgroups;     // workgroups of a group
     int whole_lines;               // rows are whole 128-byte lines: written past the caches
     float eps;
-};
-
-template <typename T> struct Piece;
-template <> struct Piece<uint16_t> {
-    static constexpr int kN = 8;
-    static __device__ __forceinline__ void open(u32x4 v, float (&x)[8])
-    {
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            x[2 * p] = bf16_lo(v[p]);
-            x[2 * p + 1] = bf16_hi(v[p]);
-        }
-    }
-    static __device__ __forceinline__ u32x4 close(const float (&x)[8])
-    {
-        return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-    }
-};
-template <> struct Piece<float> {
-    static constexpr int kN = 4;
-    static __device__ __forceinline__ void open(u32x4 v, float (&x)[4])
-    {
-#pragma unroll
-        for (int p = 0; p < 4; ++p) x[p] = __uint_as_float(v[p]);
-    }
-    static __device__ __forceinline__ u32x4 close(const float (&x)[4])
-    {
-        return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
-    }
 };
 
 // Sum over the LANES lanes that hold a row; every one of them gets it, added in the same order.

@@ -12,21 +12,7 @@ namespace {
 
 using namespace sv;
 
-constexpr int64_t kMostHeads = 1 << 24;
 constexpr int kBackwardWalks = 3;              // dq, dv and dk, in one launch
-
-bool overlaps(const void *a, const void *b, size_t bytes)
-{
-    const auto pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-    return a && b && pa < pb + bytes && pb < pa + bytes;
-}
-
-template <size_t N> bool all_aligned(const void *const (&p)[N])
-{
-    for (const void *x : p)
-        if (!aligned16(x)) return false;
-    return true;
-}
 
 // Checks `qkv` and `o`, which must agree in everything but their strides.
 sv_status check_pair(const sv_tensor_desc *qkv, const sv_tensor_desc *o, Shape *x, Shape *y)
@@ -52,8 +38,6 @@ bool sizes_ok(int32_t B, int32_t H, int32_t N, int32_t d)
 {
     return B > 0 && H > 0 && N > 0 && head_dim_ok(d) && (int64_t)B * H <= kMostHeads;
 }
-
-sv_status launched() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
 
 // Sums, scan and walk: `sums` holds the problems whose states the walks of `walks` begin from (the same slots).
 template <typename T, int D> sv_status run_walk(WalkArgs sums, const WalkArgs &walks, hipStream_t stream)

@@ -10,20 +10,6 @@ namespace {
 
 using namespace sv;
 
-constexpr int64_t kMostHeads = 1 << 24;
-
-sv_status check_rows(const sv_tensor_desc *t, Shape *s)
-{
-    const sv_status rc = check_desc(t, s, true, kMostHeads);
-    if (rc != SV_OK) return rc;
-    const int per = 16 / s->elem_bytes;
-    if (s->d <= 0 || s->d % per || s->d > kNormMostWidth) return SV_ERR_UNSUPPORTED;
-    return (int64_t)s->BH * s->N >= (int64_t)1 << 31 ? SV_ERR_SHAPE : SV_OK;
-}
-
-bool same_shape(const Shape &x, const Shape &y) { return x.B == y.B && x.H == y.H && x.N == y.N && x.d == y.d && x.bf16 == y.bf16; }
-bool same_rows(const Shape &x, const Shape &y) { return x.st.b == y.st.b && x.st.h == y.st.h && x.st.n == y.st.n; }
-
 // The rows of x's shape as groups (heads with parameters of their own, or one) of rows, walked in the order in which x lies in memory.
 void set_rows(NormArgs &g, const Shape &x, const Shape &b, const Shape &c, int groups)
 {
@@ -42,15 +28,6 @@ void set_rows(NormArgs &g, const Shape &x, const Shape &b, const Shape &c, int g
     g.rows = (int64_t)x.BH * x.N / groups;
     g.d = x.d;
 }
-
-// Is every row a run of whole 128-byte lines (given a tensor that begins with one)?
-bool lines_whole(const Shape &s)
-{
-    const int64_t line = 128 / s.elem_bytes;
-    return s.d % line == 0 && s.st.n % line == 0 && (s.H == 1 || s.st.h % line == 0) && (s.B == 1 || s.st.b % line == 0);
-}
-
-sv_status launched() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
 
 // Calls f(lanes, vecs) with the constants of a form.
 template <typename F> void with_form(const NormForm &form, F &&f)

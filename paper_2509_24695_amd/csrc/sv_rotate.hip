@@ -9,12 +9,7 @@ namespace {
 
 using namespace sv;
 
-constexpr int64_t kMostHeads = 1 << 24;
-
 bool aligned8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
-
-// Do x and y describe the same rows?
-bool same_rows(const Shape &x, const Shape &y) { return x.st.b == y.st.b && x.st.h == y.st.h && x.st.n == y.st.n; }
 
 }  // namespace
 
