@@ -3,7 +3,7 @@ the module _sventry (csrc/py_entry.cpp), which takes 1.2 us per call for it wher
 for one interpreter; another one that imports the package makes these calls through ctypes as well.
 
 The functions carry the names and argument order of the C ABI
-(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_rope.h, include/sv_norm.h, include/sv_conv.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
+(include/sv_linattn.h, include/sv_tconv.h, include/sv_decay.h, include/sv_rope.h, include/sv_norm.h, include/sv_conv.h, include/sv_scan.h, include/sv_measure.h).  Device buffers are torch tensors (or raw integer
 device addresses); nothing here computes, and there is no fallback: if the
 shared library is missing, loading raises.
 """
@@ -31,6 +31,8 @@ EXPORTS = (
     "sv_decay_linattn_token", "sv_decay_linattn_backward", "sv_rope3d_rotate", "sv_layernorm",
     "sv_layernorm_backward_workspace_bytes", "sv_layernorm_backward",
     "sv_causal_conv", "sv_causal_conv_token", "sv_causal_conv_backward_workspace_bytes", "sv_causal_conv_backward",
+    "sv_selective_scan_workspace_bytes", "sv_selective_scan_backward_workspace_bytes", "sv_selective_scan", "sv_selective_scan_token",
+    "sv_selective_scan_backward",
 )
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -135,6 +137,15 @@ def load_library():
     lib.sv_causal_conv_backward_workspace_bytes.restype = sz
     lib.sv_causal_conv_backward.argtypes = [vp, dp, vp, dp, vp, vp, i32, i32, vp, vp, vp, vp, dp, vp, vp, vp, vp, sz, vp]
     for f in (lib.sv_causal_conv, lib.sv_causal_conv_token, lib.sv_causal_conv_backward):
+        f.restype = ctypes.c_int
+    lib.sv_selective_scan_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.sv_selective_scan_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+    for f in (lib.sv_selective_scan_workspace_bytes, lib.sv_selective_scan_backward_workspace_bytes):
+        f.restype = sz
+    lib.sv_selective_scan.argtypes = [vp, vp, dp, vp, dp, vp, vp, dp, vp, vp, vp, vp, vp, vp, vp, dp, vp, sz, vp]
+    lib.sv_selective_scan_token.argtypes = [vp, vp, dp, vp, dp, vp, vp, dp, vp, vp, vp, vp, i32, vp, vp, vp, dp, vp]
+    lib.sv_selective_scan_backward.argtypes = [vp, vp, dp, vp, dp, vp, vp, dp, vp, dp] + [vp] * 15 + [vp, sz, vp]
+    for f in (lib.sv_selective_scan, lib.sv_selective_scan_token, lib.sv_selective_scan_backward):
         f.restype = ctypes.c_int
     for f in (lib.sv_decay_linattn, lib.sv_decay_linattn_token, lib.sv_decay_linattn_backward, lib.sv_rope3d_rotate, lib.sv_layernorm,
               lib.sv_layernorm_backward):
@@ -494,6 +505,39 @@ def sv_causal_conv_backward(X, x: TensorDesc, dY, dy: TensorDesc, weight, bias, 
         workspace_bytes = 0
     _check((_entry or _calls()).sv_causal_conv_backward(X, x, dY, dy, weight, bias, taps, silu, lengths, cache_in, dcache_out, dX, dx, dcache_in,
                                                         dweight, dbias, workspace, workspace_bytes, stream), "sv_causal_conv_backward")
+
+
+def sv_selective_scan_workspace_bytes(B: int, H: int, n_tokens: int, d: int, n: int) -> int:
+    return int(load_library().sv_selective_scan_workspace_bytes(int(B), int(H), int(n_tokens), int(d), int(n)))
+
+
+def sv_selective_scan_backward_workspace_bytes(B: int, H: int, n_tokens: int, d: int, G: int, n: int) -> int:
+    return int(load_library().sv_selective_scan_backward_workspace_bytes(int(B), int(H), int(n_tokens), int(d), int(G), int(n)))
+
+
+def sv_selective_scan(U, DT, u: TensorDesc, Z, z: TensorDesc | None, Bm, Cm, bc: TensorDesc, A, dt_bias, skip, lengths, S_in, S_out, Y, y: TensorDesc,
+                      workspace, workspace_bytes: int | None = None, stream=None) -> None:
+    """Selective state space scan over whole sequences (include/sv_scan.h): Z gates the output or is None, Bm, Cm are [B][G][N][n], A [H][d][n],
+    dt_bias and skip [H][d] fp32 or None, lengths [B] int32 or None, S_in / S_out [B][H][d][n] fp32 or None."""
+    _check((_entry or _calls()).sv_selective_scan(U, DT, u, Z, z, Bm, Cm, bc, A, dt_bias, skip, lengths, S_in, S_out, Y, y, workspace, workspace_bytes,
+                                                  stream), "sv_selective_scan")
+
+
+def sv_selective_scan_token(U, DT, u: TensorDesc, Z, z: TensorDesc | None, Bm, Cm, bc: TensorDesc, A, dt_bias, skip, slots, n_slots: int, S_in, S_out,
+                            Y, y: TensorDesc, stream=None) -> None:
+    """One token of each row of a batch on states of a pool (include/sv_scan.h): slots [B] int32 or None, S_in / S_out
+    [n_slots][H][d][n] fp32, the same tensor or two."""
+    _check((_entry or _calls()).sv_selective_scan_token(U, DT, u, Z, z, Bm, Cm, bc, A, dt_bias, skip, slots, n_slots, S_in, S_out, Y, y, stream),
+           "sv_selective_scan_token")
+
+
+def sv_selective_scan_backward(U, DT, u: TensorDesc, Z, z: TensorDesc | None, Bm, Cm, bc: TensorDesc, dY, dy: TensorDesc, A, dt_bias, skip, lengths, S_in,
+                               dS_out, dU, dDT, dZ, dB, dC, dS_in, dA, ddt_bias, dskip, workspace, workspace_bytes: int | None = None,
+                               stream=None) -> None:
+    """Gradients of sv_selective_scan for all of its inputs (include/sv_scan.h)."""
+    _check((_entry or _calls()).sv_selective_scan_backward(U, DT, u, Z, z, Bm, Cm, bc, dY, dy, A, dt_bias, skip, lengths, S_in, dS_out, dU, dDT, dZ, dB,
+                                                           dC, dS_in, dA, ddt_bias, dskip, workspace, workspace_bytes, stream),
+           "sv_selective_scan_backward")
 
 
 def sv_measure_apply_variant(variant: int, Q, q: TensorDesc, tok_begin: int, tok_end: int, S, z, eps: float, O,

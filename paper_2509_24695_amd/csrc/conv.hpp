@@ -11,6 +11,7 @@
 #include "common.hpp"
 #include "conv_plan.hpp"
 #include "piece.hpp"
+#include "sequences.hpp"
 
 namespace sv {
 
@@ -93,13 +94,6 @@ template <int K, int N> __device__ __forceinline__ void conv_shift(float (&w)[K]
     for (int e = 0; e < N; ++e) w[K - 1][e] = now[e];
 }
 
-__device__ __forceinline__ int held_length(const int32_t *lengths, int b, int N)
-{
-    if (!lengths) return N;
-    const int n = lengths[b];
-    return n < 0 ? 0 : n > N ? N : n;
-}
-
 template <typename T, int K, bool SILU> __global__ __launch_bounds__(kConvThreads) void conv_rows(ConvArgs a)
 {
     constexpr int kN = Piece<T>::kN, kAhead = 4;
@@ -150,15 +144,6 @@ template <typename T, int K, bool SILU> __global__ __launch_bounds__(kConvThread
 #pragma unroll
         for (int r = 0; r < K - 1; ++r) *reinterpret_cast<u32x4 *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r];
     }
-}
-
-// Has an earlier row of the batch the same slot?  For all threads of a workgroup.
-__device__ __forceinline__ bool slot_taken(const int32_t *slots, int b, int slot)
-{
-    bool taken = false;
-    if (slots)
-        for (int r = threadIdx.x; r < b; r += blockDim.x) taken |= slots[r] == slot;
-    return __syncthreads_or(taken);
 }
 
 // One token of each row of a batch: a workgroup has `across` pieces of one row.

@@ -15,6 +15,7 @@
 #include "../../include/sv_linattn.h"
 #include "../../include/sv_norm.h"
 #include "../../include/sv_rope.h"
+#include "../../include/sv_scan.h"
 #include "../../include/sv_tconv.h"
 
 namespace {
@@ -244,6 +245,9 @@ ENTRY(sv_layernorm_backward, P, Desc, P, Desc, P, Int, P, P, P, Desc, P, P, P, B
 ENTRY(sv_causal_conv, P, Desc, P, P, Int, Flag, P, P, P, P, Desc, Stream)
 ENTRY(sv_causal_conv_token, P, Desc, P, P, Int, Flag, P, Int, P, P, P, Desc, Stream)
 ENTRY(sv_causal_conv_backward, P, Desc, P, Desc, P, P, Int, Flag, P, P, P, P, Desc, P, P, P, P, Bytes, Stream)
+ENTRY(sv_selective_scan, P, P, Desc, P, Desc, P, P, Desc, P, P, P, P, P, P, P, Desc, P, Bytes, Stream)
+ENTRY(sv_selective_scan_token, P, P, Desc, P, Desc, P, P, Desc, P, P, P, P, Int, P, P, P, Desc, Stream)
+ENTRY(sv_selective_scan_backward, P, P, Desc, P, Desc, P, P, Desc, P, Desc, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, Bytes, Stream)
 
 // attach(handle): the entry points of the loaded library with this dlopen handle.
 PyObject *attach(PyObject *, PyObject *handle)
@@ -265,7 +269,8 @@ PyObject *attach(PyObject *, PyObject *handle)
     X(sv_block_linattn_lookahead_rope) X(sv_linattn_state_rope3d) X(sv_linattn_apply_rope3d)                           \
     X(sv_block_linattn_step_rope3d) X(sv_block_linattn_lookahead_rope3d) X(sv_tconv_block_step)        \
     X(sv_decay_linattn) X(sv_decay_linattn_token) X(sv_decay_linattn_backward) X(sv_rope3d_rotate) X(sv_layernorm)     \
-    X(sv_layernorm_backward) X(sv_causal_conv) X(sv_causal_conv_token) X(sv_causal_conv_backward)
+    X(sv_layernorm_backward) X(sv_causal_conv) X(sv_causal_conv_token) X(sv_causal_conv_backward) \
+    X(sv_selective_scan) X(sv_selective_scan_token) X(sv_selective_scan_backward)
     EACH(ATTACH)
     Py_RETURN_NONE;
 }

@@ -1,0 +1,259 @@
+// Selective state space scan: per channel c and state number i
+//
+//   D_t = softplus(dt_t + dt_bias),  h_t[i] = exp(D_t A[i]) h_{t-1}[i] + D_t u_t B_t[i],  y_t = (sum_i C_t[i] h_t[i] + skip u_t) silu(z_t)
+//
+// A lane owns a channel and holds its n states; B_t and C_t are the same for all lanes of a wave and come through the scalar cache.  Bound
+// by the vector unit: an exponential and four other instructions for each state, with softplus and the gate beside them.  A long sequence
+// is cut into segments that are walked side by side: scan_sums finds what each segment adds to a state of nothing and its sum of steps,
+// scan_states turns these into the states the segments begin from (what a segment keeps of its state is exp(A sum D)), and scan_walk
+// walks from there.
+#pragma once
+
+#include "activation.hpp"
+#include "common.hpp"
+#include "scan_plan.hpp"
+#include "sequences.hpp"
+
+namespace sv {
+
+struct ScanArgs {
+    const void *u, *dt, *z, *bm, *cm, *dy;
+    void *y;
+    TokStrides su, sz, sbc, sy;              // sy: y, or dy
+    const float *A, *dt_bias, *skip;
+    const int32_t *lengths;
+    const float *s_in, *ds_out;
+    float *s_out;
+    float *states, *grads, *steps;           // [B][segments][n][C], the same, [B][segments][C]
+    float *marks, *mark_steps;               // [B][runs][n][C], [B][runs][C]: local states before each run of tokens
+    float *shared, *params;                  // [B][blocks][N][2][n]; [B][segments][n + 2][C]
+    void *du, *ddt, *dz, *db, *dc;
+    float *ds_in, *dA, *ddt_bias, *dskip;
+    int B, H, N, d, G, channels, group_channels, group_blocks, blocks;
+    int segments, per_segment, runs;
+};
+
+// Where a wave's lanes work: a block of 64 channels of one group.  Lanes past the group's last channel double it and store nothing.
+struct ScanPlace {
+    int b, segment, group, block, channel, length, first, last;
+    bool mine;
+    int64_t u, z, y;                         // elements of token 0
+    __device__ __forceinline__ ScanPlace(const ScanArgs &a, uint32_t id)
+    {
+        block = (int)(id % (uint32_t)a.blocks);
+        id /= (uint32_t)a.blocks;
+        segment = (int)(id % (uint32_t)a.segments);
+        b = (int)(id / (uint32_t)a.segments);
+        group = block / a.group_blocks;
+        int c = (block - group * a.group_blocks) * kScanWave + (int)threadIdx.x % kScanWave;
+        mine = c < a.group_channels;
+        c = mine ? c : a.group_channels - 1;
+        channel = group * a.group_channels + c;
+        const int h = channel / a.d, i = channel - h * a.d;
+        u = b * a.su.b + h * a.su.h + i;
+        z = b * a.sz.b + h * a.sz.h + i;
+        y = b * a.sy.b + h * a.sy.h + i;
+        length = held_length(a.lengths, b, a.N);
+        first = segment * a.per_segment;
+        const int64_t end = (int64_t)first + a.per_segment;
+        last = end < length ? (int)end : length;
+    }
+    __device__ __forceinline__ int64_t slot(const ScanArgs &a) const { return (int64_t)b * a.segments + segment; }
+};
+
+// n numbers that are the same for all lanes, out of the scalar cache.
+template <typename T, int n> struct Scalars;
+template <int n> struct Scalars<float, n> {
+    uint32_t w[n];
+    __device__ __forceinline__ void load(const void *base, int64_t at)
+    {
+        const auto *p = (const __attribute__((address_space(4))) uint32_t *)(reinterpret_cast<uintptr_t>(base) + at * 4);
+#pragma unroll
+        for (int i = 0; i < n; ++i) w[i] = p[i];
+    }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
+};
+template <int n> struct Scalars<uint16_t, n> {
+    uint32_t w[n / 2];
+    __device__ __forceinline__ void load(const void *base, int64_t at)
+    {
+        const auto *p = (const __attribute__((address_space(4))) uint32_t *)(reinterpret_cast<uintptr_t>(base) + at * 2);
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) w[i] = p[i];
+    }
+    __device__ __forceinline__ float operator[](int i) const { return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]); }
+};
+
+// A channel's A, times log2(e): exp(D A) = 2^(D A2).
+template <int n> __device__ __forceinline__ void load_rates(const ScanArgs &a, int channel, float (&A2)[n])
+{
+#pragma unroll
+    for (int q = 0; q < n / 4; ++q) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.A + (int64_t)channel * n + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) A2[4 * q + e] = v[e] * kLog2E;
+    }
+}
+// A state as it lies in S_in: a channel's n numbers side by side.
+template <int n> __device__ __forceinline__ void load_state(const float *p, int64_t row, float (&h)[n])
+{
+#pragma unroll
+    for (int q = 0; q < n / 4; ++q) {
+        const f32x4 v = p ? *reinterpret_cast<const f32x4 *>(p + row * n + 4 * q) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[4 * q + e] = v[e];
+    }
+}
+template <int n> __device__ __forceinline__ void store_state(float *p, int64_t row, const float (&h)[n])
+{
+#pragma unroll
+    for (int q = 0; q < n / 4; ++q) *reinterpret_cast<f32x4 *>(p + row * n + 4 * q) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
+}
+// What a run of tokens with steps that sum to `steps` keeps of a state number: past the largest fp32 number that number, so that a state of
+// nothing stays one.
+__device__ __forceinline__ float kept(float A2, float steps) { return fminf(__builtin_amdgcn_exp2f(A2 * steps), 3.40282347e38f); }
+
+// Numbers of kAhead tokens on their way.
+template <typename T, int AHEAD> struct Ahead {
+    float x[AHEAD];
+    __device__ __forceinline__ void request(const void *base, int64_t at, int64_t stride, int t, int last)
+    {
+        const T *p = static_cast<const T *>(base) + at;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (t + i < last) x[i] = Elem<T>::load(p + (t + i) * stride);
+    }
+};
+
+constexpr int kScanAhead = 4;
+
+// What the tokens of a segment add to a state of nothing, and the sum of their steps.  MARKS: the local state before each run too.
+template <typename T, int n, bool MARKS> __device__ __forceinline__ void scan_sum_forward(const ScanArgs &a, const ScanPlace &at)
+{
+    float A2[n], h[n], steps = 0.f;
+    load_rates<n>(a, at.channel, A2);
+    const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f;
+#pragma unroll
+    for (int i = 0; i < n; ++i) h[i] = 0.f;
+    const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
+    Ahead<T, kScanAhead> u{}, dt{};
+    u.request(a.u, at.u, a.su.n, at.first, at.last);
+    dt.request(a.dt, at.u, a.su.n, at.first, at.last);
+    for (int t0 = at.first; t0 < at.last; t0 += kScanAhead) {
+        if (MARKS && t0 % kScanRun == 0 && t0 != at.first && at.mine) {
+            const int64_t mark = (int64_t)at.b * a.runs + t0 / kScanRun;
+#pragma unroll
+            for (int i = 0; i < n; ++i) a.marks[(mark * n + i) * a.channels + at.channel] = h[i];
+            a.mark_steps[mark * a.channels + at.channel] = steps;
+        }
+        const Ahead<T, kScanAhead> u0 = u, dt0 = dt;
+        u.request(a.u, at.u, a.su.n, t0 + kScanAhead, at.last);
+        dt.request(a.dt, at.u, a.su.n, t0 + kScanAhead, at.last);
+#pragma unroll
+        for (int k = 0; k < kScanAhead; ++k) {
+            const int t = t0 + k;
+            if (t >= at.last) break;
+            Scalars<T, n> B;
+            B.load(a.bm, bc + t * a.sbc.n);
+            const float D = softplus(dt0.x[k] + bias), x = D * u0.x[k];
+            steps += D;
+#pragma unroll
+            for (int i = 0; i < n; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
+        }
+    }
+    if (!at.mine) return;
+#pragma unroll
+    for (int i = 0; i < n; ++i) a.states[(at.slot(a) * n + i) * a.channels + at.channel] = h[i];
+    a.steps[at.slot(a) * a.channels + at.channel] = steps;
+}
+
+template <typename T, int n> __global__ __launch_bounds__(kScanWave) void scan_sums(ScanArgs a)
+{
+    // (the last segment's sum is not needed)
+    const uint32_t per_b = (uint32_t)a.blocks * (a.segments - 1), b = blockIdx.x / per_b;
+    const ScanPlace at(a, b * (uint32_t)a.blocks * a.segments + (blockIdx.x - b * per_b));
+    if (at.first >= at.length) return;
+    scan_sum_forward<T, n, false>(a, at);
+}
+
+// The states that the segments begin from, in place of what the segments before add; backwards (BACK) the gradients that arrive at their ends.
+template <int n, bool BACK> __device__ __forceinline__ void scan_state(const ScanArgs &a, int64_t id)
+{
+    const int c = (int)(id % a.channels), i = (int)(id / a.channels % n), b = (int)(id / a.channels / n);
+    const float A2 = a.A[(int64_t)c * n + i] * kLog2E;
+    const float *from = BACK ? a.ds_out : a.s_in;
+    float *slots = (BACK ? a.grads : a.states) + ((int64_t)b * a.segments * n + i) * a.channels + c;
+    const float *steps = a.steps + (int64_t)b * a.segments * a.channels + c;
+    float s = from ? from[((int64_t)b * a.channels + c) * n + i] : 0.f;
+    const int length = held_length(a.lengths, b, a.N), used = length ? (length - 1) / a.per_segment + 1 : 1;
+    const int64_t stride = (int64_t)n * a.channels;
+    constexpr int kAhead = 8;
+    for (int k0 = 0; k0 < used; k0 += kAhead) {
+        float add[kAhead], sum[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int seg = BACK ? used - 1 - k0 - k : k0 + k;
+            const bool in = BACK ? seg > 0 : seg + 1 < used;          // the walk's last segment hands nothing on
+            add[k] = in ? slots[seg * stride] : 0.f;
+            sum[k] = in ? steps[(int64_t)seg * a.channels] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int seg = BACK ? used - 1 - k0 - k : k0 + k;
+            if (k0 + k >= used) break;
+            slots[seg * stride] = s;
+            s = __builtin_fmaf(kept(A2, sum[k]), s, add[k]);
+        }
+    }
+}
+template <int n> __global__ __launch_bounds__(256) void scan_states(ScanArgs a)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id < (int64_t)a.B * a.channels * n) scan_state<n, false>(a, id);
+}
+
+template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_walk(ScanArgs a)
+{
+    const ScanPlace at(a, blockIdx.x);
+    if (at.first >= at.length && at.segment > 0) return;
+    float A2[n], h[n];
+    load_rates<n>(a, at.channel, A2);
+    const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f, skip = a.skip ? a.skip[at.channel] : 0.f;
+    if (a.segments == 1) load_state<n>(a.s_in, (int64_t)at.b * a.channels + at.channel, h);
+    else
+#pragma unroll
+        for (int i = 0; i < n; ++i) h[i] = a.states[(at.slot(a) * n + i) * a.channels + at.channel];
+    const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
+    T *y = static_cast<T *>(a.y) + at.y;
+    Ahead<T, kScanAhead> u{}, dt{}, z{};
+    auto request = [&](int t) {
+        u.request(a.u, at.u, a.su.n, t, at.last);
+        dt.request(a.dt, at.u, a.su.n, t, at.last);
+        if (GATE) z.request(a.z, at.z, a.sz.n, t, at.last);
+    };
+    request(at.first);
+    for (int t0 = at.first; t0 < at.last; t0 += kScanAhead) {
+        const Ahead<T, kScanAhead> u0 = u, dt0 = dt, z0 = z;
+        request(t0 + kScanAhead);
+#pragma unroll
+        for (int k = 0; k < kScanAhead; ++k) {
+            const int t = t0 + k;
+            if (t >= at.last) break;
+            Scalars<T, n> B, C;
+            B.load(a.bm, bc + t * a.sbc.n);
+            C.load(a.cm, bc + t * a.sbc.n);
+            const float D = softplus(dt0.x[k] + bias), x = D * u0.x[k];
+            float out = skip * u0.x[k];
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
+                out = __builtin_fmaf(C[i], h[i], out);
+            }
+            if (GATE) out *= silu(z0.x[k]);
+            if (at.mine) Elem<T>::store(y + t * a.sy.n, out);
+        }
+    }
+    if (a.s_out && at.mine && at.last == at.length) store_state<n>(a.s_out, (int64_t)at.b * a.channels + at.channel, h);
+}
+
+}  // namespace sv

@@ -1,0 +1,256 @@
+// The selective scan's backward pass.  With y' = dy silu(z) and g_t = C_t y'_t + exp(D_{t+1} A) g_{t+1}, token by token from the end:
+//
+//   dC = sum_c y' h_t,  dB = sum_c g D u,  e = sum_i g B,  p = g exp(D A) h_{t-1},  dD = sum_i A p + u e,  du = D e + skip y',
+//   ddt = dD sigmoid(dt + bias),  dz = dy (sum_i C h_t + skip u) silu'(z),  dA = sum_t D p,  dskip = sum_t y' u
+//
+// Cut into segments like the forward pass, with gradients handed on from segment to segment the same way from the end.  The states are
+// needed from the last to the first: scan_back_sums leaves the local state before every run of eight tokens, a wave adds what the
+// segment's first state has become by then, walks the run forwards with its eight states in registers, and then backwards.  The sums over channels (dB, dC)
+// go through the wave by exchanges that halve the number of values a lane holds with every step: 2 n values cost little more than 2 n additions.
+#pragma once
+
+#include "scan.hpp"
+
+namespace sv {
+
+// g = C y' of a segment's tokens from its last on, carried to before its first: what the segment adds to the gradient of the state it began from.
+template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum_back(const ScanArgs &a, const ScanPlace &at)
+{
+    float A2[n], g[n];
+    load_rates<n>(a, at.channel, A2);
+    const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f;
+#pragma unroll
+    for (int i = 0; i < n; ++i) g[i] = 0.f;
+    const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
+    // tokens from the last: token k of the walk is last - 1 - k
+    Ahead<T, kScanAhead> dy{}, dt{}, z{};
+    const int count = at.last - at.first;
+    auto request = [&](int k) {
+        const int64_t top = at.last - 1;
+        dy.request(a.dy, at.y + top * a.sy.n, -a.sy.n, k, count);
+        dt.request(a.dt, at.u + top * a.su.n, -a.su.n, k, count);
+        if (GATE) z.request(a.z, at.z + top * a.sz.n, -a.sz.n, k, count);
+    };
+    request(0);
+    for (int k0 = 0; k0 < count; k0 += kScanAhead) {
+        const Ahead<T, kScanAhead> dy0 = dy, dt0 = dt, z0 = z;
+        request(k0 + kScanAhead);
+#pragma unroll
+        for (int k = 0; k < kScanAhead; ++k) {
+            if (k0 + k >= count) break;
+            Scalars<T, n> C;
+            C.load(a.cm, bc + (at.last - 1 - k0 - k) * a.sbc.n);
+            const float D = softplus(dt0.x[k] + bias), v = GATE ? dy0.x[k] * silu(z0.x[k]) : dy0.x[k];
+#pragma unroll
+            for (int i = 0; i < n; ++i) g[i] = __builtin_amdgcn_exp2f(D * A2[i]) * __builtin_fmaf(C[i], v, g[i]);
+        }
+    }
+    if (!at.mine) return;
+#pragma unroll
+    for (int i = 0; i < n; ++i) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = g[i];
+}
+
+template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_back_sums(ScanArgs a)
+{
+    const uint32_t half = (uint32_t)a.blocks * a.segments * a.B;
+    const bool back = blockIdx.x >= half;
+    const ScanPlace at(a, back ? blockIdx.x - half : blockIdx.x);
+    if (at.first >= at.length) return;
+    if (!back) scan_sum_forward<T, n, true>(a, at);
+    else if (at.segment > 0) scan_sum_back<T, n, GATE>(a, at);
+}
+
+template <int n> __global__ __launch_bounds__(256) void scan_back_states(ScanArgs a)
+{
+    const int64_t count = (int64_t)a.B * a.channels * n, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id < count) scan_state<n, false>(a, id);
+    else if (id < 2 * count) scan_state<n, true>(a, id - count);
+}
+
+// Sums of V values over the wave: a lane ends with that of value wave_value<V>(lane), in v[0].
+template <int V> __device__ __forceinline__ void wave_sums(float (&v)[V])
+{
+    static_assert(V == 16 || V == 32, "two or one lane a value and four steps");
+    const int lane = threadIdx.x % kScanWave;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + V / 2]), false, false);
+        v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + V / 4]), false, false);
+        v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    // a lane keeps one of two values and gets its partner's of the same
+    auto step = [&](auto ctrl, int bit, float keep_low, float keep_high) {
+        const bool high = lane & bit;
+        const float own = high ? keep_high : keep_low, other = high ? keep_low : keep_high;
+        return own + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, other), ctrl(), 0xf, 0xf, true));
+    };
+#pragma unroll
+    for (int i = 0; i < V / 8; ++i) v[i] = step(std::integral_constant<int, 0x128>{}, 8, v[i], v[i + V / 8]);      // row_ror 8
+#pragma unroll
+    for (int i = 0; i < V / 16; ++i) v[i] = step(std::integral_constant<int, 0x141>{}, 4, v[i], v[i + V / 16]);    // row_half_mirror
+    if constexpr (V == 32) v[0] = step(std::integral_constant<int, 0x4e>{}, 2, v[0], v[1]);                        // quad_perm 2,3,0,1
+    else v[0] = dpp_add<0x4e>(v[0]);
+    v[0] = dpp_add<0xb1>(v[0]);
+}
+template <int V> __device__ __forceinline__ int wave_value(int lane)
+{
+    int i = (lane >> 5 & 1) * (V / 2) + (lane >> 4 & 1) * (V / 4) + (lane >> 3 & 1) * (V / 8) + (lane >> 2 & 1) * (V / 16);
+    if (V == 32) i += lane >> 1 & 1;
+    return i;
+}
+
+template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_back_walk(ScanArgs a)
+{
+    const ScanPlace at(a, blockIdx.x);
+    const int lane = threadIdx.x;
+    float *params = a.params + at.slot(a) * (n + 2) * a.channels + at.channel;
+    if (at.first >= at.length && at.segment > 0) {
+        if (at.mine)
+#pragma unroll
+            for (int i = 0; i < n + 2; ++i) params[(int64_t)i * a.channels] = 0.f;
+        return;
+    }
+    float A2[n], begin[n], g[n], dA[n], dbias = 0.f, dskip = 0.f;
+    load_rates<n>(a, at.channel, A2);
+    const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f, skip = a.skip ? a.skip[at.channel] : 0.f;
+    const int64_t row = (int64_t)at.b * a.channels + at.channel;
+    if (a.segments == 1) {
+        load_state<n>(a.s_in, row, begin);
+        load_state<n>(a.ds_out, row, g);
+    } else {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            begin[i] = a.states[(at.slot(a) * n + i) * a.channels + at.channel];
+            g[i] = a.grads[(at.slot(a) * n + i) * a.channels + at.channel];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < n; ++i) dA[i] = 0.f;
+    const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
+    float *shared = a.shared + ((int64_t)at.b * a.blocks + at.block) * a.N * 2 * n + wave_value<2 * n>(lane);
+    const bool sums_mine = lane % (64 / (2 * n)) == 0;
+    const int runs = (at.last - at.first + kScanRun - 1) / kScanRun;
+    Ahead<T, kScanRun> u{}, dt{}, z{}, dy{};
+    auto request = [&](int t) {
+        u.request(a.u, at.u, a.su.n, t, at.last);
+        dt.request(a.dt, at.u, a.su.n, t, at.last);
+        dy.request(a.dy, at.y, a.sy.n, t, at.last);
+        if (GATE) z.request(a.z, at.z, a.sz.n, t, at.last);
+    };
+    if (runs) request(at.first + (runs - 1) * kScanRun);
+    for (int r = runs - 1; r >= 0; --r) {
+        const int t0 = at.first + r * kScanRun, count = at.last - t0 < kScanRun ? at.last - t0 : kScanRun;
+        const Ahead<T, kScanRun> u0 = u, dt0 = dt, z0 = z, dy0 = dy;
+        if (r > 0) request(t0 - kScanRun);
+        float h[kScanRun + 1][n], D[kScanRun], raw[kScanRun];
+        if (r > 0) {
+            const int64_t mark = (int64_t)at.b * a.runs + t0 / kScanRun;
+            const float steps = a.mark_steps[mark * a.channels + at.channel];
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                h[0][i] = __builtin_fmaf(kept(A2[i], steps), begin[i], a.marks[(mark * n + i) * a.channels + at.channel]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < n; ++i) h[0][i] = begin[i];
+        }
+#pragma unroll
+        for (int k = 0; k < kScanRun; ++k) {
+            if (k < count) {
+                Scalars<T, n> B, C;
+                B.load(a.bm, bc + (t0 + k) * a.sbc.n);
+                if (GATE) C.load(a.cm, bc + (t0 + k) * a.sbc.n);
+                D[k] = softplus(dt0.x[k] + bias);
+                const float x = D[k] * u0.x[k];
+                raw[k] = skip * u0.x[k];
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    h[k + 1][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D[k] * A2[i]), h[k][i], x * B[i]);
+                    if (GATE) raw[k] = __builtin_fmaf(C[i], h[k + 1][i], raw[k]);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = kScanRun - 1; k >= 0; --k) {
+            if (k >= count) continue;
+            const int t = t0 + k;
+            Scalars<T, n> B, C;
+            B.load(a.bm, bc + t * a.sbc.n);
+            C.load(a.cm, bc + t * a.sbc.n);
+            float v = dy0.x[k];
+            if (GATE) {
+                const float s = sigmoid(z0.x[k]);
+                if (at.mine) Elem<T>::store(static_cast<T *>(a.dz) + at.z + t * a.sz.n, v * raw[k] * silu_slope(z0.x[k], s));
+                v *= z0.x[k] * s;
+            }
+            const float x = D[k] * u0.x[k];
+            float sums[2 * n], e = 0.f, along = 0.f;
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                g[i] = __builtin_fmaf(C[i], v, g[i]);
+                sums[i] = at.mine ? g[i] * x : 0.f;
+                sums[n + i] = at.mine ? v * h[k + 1][i] : 0.f;
+                e = __builtin_fmaf(g[i], B[i], e);
+                g[i] *= __builtin_amdgcn_exp2f(D[k] * A2[i]);
+                const float p = g[i] * h[k][i];
+                dA[i] = __builtin_fmaf(D[k], p, dA[i]);
+                along = __builtin_fmaf(A2[i], p, along);
+            }
+            float slope;
+            softplus(dt0.x[k] + bias, slope);
+            const float ddt = __builtin_fmaf(along, 1.f / kLog2E, u0.x[k] * e) * slope;
+            dbias += ddt;
+            dskip = __builtin_fmaf(v, u0.x[k], dskip);
+            if (at.mine) {
+                Elem<T>::store(static_cast<T *>(a.du) + at.u + t * a.su.n, __builtin_fmaf(D[k], e, skip * v));
+                Elem<T>::store(static_cast<T *>(a.ddt) + at.u + t * a.su.n, ddt);
+            }
+            wave_sums<2 * n>(sums);
+            if (sums_mine) shared[(int64_t)t * 2 * n] = sums[0];
+        }
+    }
+    if (!at.mine) return;
+#pragma unroll
+    for (int i = 0; i < n; ++i) params[(int64_t)i * a.channels] = dA[i];
+    params[(int64_t)n * a.channels] = dbias;
+    params[(int64_t)(n + 1) * a.channels] = dskip;
+    if (a.ds_in && at.segment == 0) store_state<n>(a.ds_in, row, g);
+}
+
+// dB and dC: the blocks' sums over their channels, added up in order and rounded.
+template <typename T, int n> __global__ __launch_bounds__(256) void scan_back_shared(ScanArgs a)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.N * 2 * n;
+    const int64_t bg = id / per, at = id - bg * per;
+    if (bg >= (int64_t)a.B * a.G) return;
+    const int b = (int)(bg / a.G), group = (int)(bg % a.G), t = (int)(at / (2 * n)), i = (int)(at % (2 * n));
+    if (t >= held_length(a.lengths, b, a.N)) return;
+    const float *p = a.shared + ((int64_t)b * a.blocks + group * a.group_blocks) * per + at;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < a.group_blocks; ++k) s += p[k * per];
+    T *out = static_cast<T *>(i < n ? a.db : a.dc) + b * a.sbc.b + group * a.sbc.h + t * a.sbc.n;
+    Elem<T>::store(out + i % n, s);
+}
+
+// dA, ddt_bias and dskip: the segments' sums, added up in order.
+template <int n> __global__ __launch_bounds__(256) void scan_back_params(ScanArgs a)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.channels * (n + 2);
+    if (id >= per) return;
+    const int i = (int)(id / a.channels), c = (int)(id % a.channels);
+    float s = 0.f;
+    const int64_t parts = (int64_t)a.B * a.segments;
+#pragma unroll 8
+    for (int64_t k = 0; k < parts; ++k) s += a.params[k * per + id];
+    if (i < n) {
+        if (a.dA) a.dA[(int64_t)c * n + i] = s;
+    } else if (float *out = i == n ? a.ddt_bias : a.dskip) {
+        out[c] = s;
+    }
+}
+
+}  // namespace sv

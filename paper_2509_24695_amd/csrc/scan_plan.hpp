@@ -1,0 +1,70 @@
+// How a selective scan is cut up: waves of channels, segments of tokens.  Plain C++ (no device code), shared by the launchers and host-side
+// tests.
+#pragma once
+
+#include <stdint.h>
+
+namespace sv {
+
+constexpr int kScanWave = 64;               // channels of a wave
+constexpr int kScanRun = 8;                 // tokens whose states the backward pass holds at once: segments are multiples of it
+constexpr int kScanShortest = 32;           // tokens of a segment, where there is more than one
+constexpr int kScanMostSegments = 128;      // what scan_states walks one after the other
+
+// A sequence is walked by `segments` waves per channel block, `per_segment` tokens each (the last fewer).
+struct ScanPlan {
+    int blocks;                             // waves across the channels of all groups
+    int segments, per_segment;
+};
+
+constexpr int64_t kScanForwardWaves = 4096, kScanBackwardWaves = 4096;
+
+inline int64_t scan_most_segments(int64_t B, int64_t n_tokens, int64_t blocks, int64_t waves)
+{
+    int64_t s = waves / (B * blocks);
+    const int64_t longest = (n_tokens + kScanShortest - 1) / kScanShortest;
+    if (s > longest) s = longest;
+    if (s > kScanMostSegments) s = kScanMostSegments;
+    return s < 1 ? 1 : s;
+}
+inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_tokens, int64_t waves)
+{
+    ScanPlan p{};
+    p.blocks = groups * ((group_channels + kScanWave - 1) / kScanWave);
+    const int64_t s = scan_most_segments(B, n_tokens, p.blocks, waves);
+    int64_t per = (n_tokens + s - 1) / s;
+    if (s > 1 && per < kScanShortest) per = kScanShortest;
+    per = (per + kScanRun - 1) / kScanRun * kScanRun;
+    p.per_segment = (int)per;
+    p.segments = (int)((n_tokens + per - 1) / per);
+    return p;
+}
+
+// Segments of all sequences together in the largest call with no more batches and tokens and the same channels.
+inline int64_t scan_slots(int64_t B, int64_t n_tokens, int64_t channels, int64_t waves)
+{
+    const int64_t blocks = (channels + kScanWave - 1) / kScanWave, longest = (n_tokens + kScanShortest - 1) / kScanShortest;
+    const int64_t most = B * (longest < kScanMostSegments ? longest : kScanMostSegments), full = waves / blocks > B ? waves / blocks : B;
+    return most < full ? most : full;
+}
+
+// Floats of the backward pass's workspace, part by part.
+struct ScanBackwardSpace {
+    int64_t forward, backward, steps, marks, mark_steps, shared, params, total;
+};
+inline ScanBackwardSpace scan_backward_space(int64_t B, int64_t groups, int64_t channels, int64_t n_tokens, int n, int64_t slots)
+{
+    const int64_t runs = (n_tokens + kScanRun - 1) / kScanRun, blocks = groups * ((channels / groups + kScanWave - 1) / kScanWave);
+    auto lines = [](int64_t floats) { return (floats + 63) / 64 * 64; };
+    ScanBackwardSpace s{};
+    s.forward = s.backward = lines(slots * channels * n);
+    s.steps = lines(slots * channels);
+    s.marks = lines(B * runs * channels * n);
+    s.mark_steps = lines(B * runs * channels);
+    s.shared = lines(B * blocks * n_tokens * 2 * n);
+    s.params = lines(slots * channels * (n + 2));
+    s.total = s.forward + s.backward + s.steps + s.marks + s.mark_steps + s.shared + s.params;
+    return s;
+}
+
+}  // namespace sv

@@ -1,0 +1,140 @@
+"""What the selective scan refuses, before any launch, and how its calls are cut up (csrc/scan_plan.hpp)."""
+import os
+import subprocess
+
+import pytest
+
+import paper_2509_24695_amd as sv
+from paper_2509_24695_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+A = [0x1000000 * (i + 1) for i in range(40)]         # aligned, never dereferenced: every call below fails before a launch
+BIG = 1 << 40
+
+
+@pytest.fixture(params=["module", "ctypes"])
+def route(request, monkeypatch):
+    lib = sv.load_library()
+    monkeypatch.setattr(binding, "_entry", binding._load_entry(lib) if request.param == "module" else binding._CtypesCalls(lib))
+
+
+def _desc(**kw):
+    return sv.TensorDesc(**{**dict(B=1, H=2, N=128, d=64, stride_b=2 * 128 * 64, stride_h=128 * 64, stride_n=64, dtype=sv.SV_BF16), **kw})
+
+
+def _bc(**kw):
+    return sv.TensorDesc(**{**dict(B=1, H=1, N=128, d=16, stride_b=128 * 16, stride_h=128 * 16, stride_n=16, dtype=sv.SV_BF16), **kw})
+
+
+def _status(f, *a, **kw):
+    with pytest.raises(sv.SvError) as e:
+        f(*a, **kw)
+    return e.value.status
+
+
+def _forward(**kw):
+    p = dict(U=A[0], DT=A[1], u=_desc(), Z=A[2], z=_desc(), Bm=A[3], Cm=A[4], bc=_bc(), A=A[5], bias=A[6], skip=A[7], lengths=None, si=A[8], so=A[9], Y=None,
+             y=_desc(), ws=A[10], wb=BIG)
+    p.update(kw)
+    return _status(sv.sv_selective_scan, *p.values())
+
+
+def _token(**kw):
+    one = _desc(N=1)
+    p = dict(U=A[0], DT=A[1], u=one, Z=A[2], z=one, Bm=A[3], Cm=A[4], bc=_bc(N=1), A=A[5], bias=A[6], skip=A[7], slots=None, n=4, si=A[8], so=A[9], Y=None, y=one)
+    p.update(kw)
+    return _status(sv.sv_selective_scan_token, *p.values())
+
+
+def _backward(**kw):
+    p = dict(U=A[0], DT=A[1], u=_desc(), Z=A[2], z=_desc(), Bm=A[3], Cm=A[4], bc=_bc(), dY=A[5], dy=_desc(), A=A[6], bias=A[7], skip=A[8], lengths=None, si=A[9],
+             dso=A[10], dU=None, dDT=A[12], dZ=A[13], dB=A[14], dC=A[15], dsi=A[16], dA=A[17], dbias=A[18], dskip=A[19], ws=A[20], wb=BIG)
+    p.update(kw)
+    return _status(sv.sv_selective_scan_backward, *p.values())
+
+
+def _tensors(call, given):
+    """Refusals that the three entry points share."""
+    assert call() == 1
+    for name in ("U", "DT", "Bm", "Cm", "A"):
+        assert call(**{**given, name: None}) == 1, name
+    for name in ("U", "DT", "Z", "Bm", "Cm", "A", "si"):
+        assert call(**{**given, name: A[30] + 8}) == 4, name
+    for name in ("bias", "skip"):
+        assert call(**{**given, name: A[30] + 2}) == 4, name
+    for name in ("u", "z", "bc"):
+        assert call(**{**given, name: None}) == 1, name
+    N = 1 if call is _token else 128
+    for kw, status in ((dict(d=0), 3), (dict(dtype=7), 3), (dict(N=0), 2), (dict(B=0), 2), (dict(stride_n=56), 2), (dict(stride_n=68), 4), (dict(stride_h=64), 2)):
+        if call is not _token or "stride_h" not in kw:
+            assert call(**{**given, "u": _desc(**{"N": N, **kw})}) == status, kw
+            assert call(**{**given, "z": _desc(**{"N": N, **kw})}) == status, kw
+    for kw in (dict(dtype=sv.SV_F32), dict(d=32), dict(N=64), dict(H=1)):
+        assert call(**{**given, "z": _desc(**{"N": N, **kw})}) == 2, kw
+    for kw, status in ((dict(d=12), 3), (dict(d=32, stride_n=32), 3), (dict(d=8, dtype=sv.SV_F32), 2), (dict(H=3, stride_h=1 << 20, stride_b=1 << 24), 2), (dict(N=N + 1), 2),
+                       (dict(B=2, stride_b=1 << 24), 2), (dict(stride_n=20), 4)):
+        assert call(**{**given, "bc": _bc(**{"N": N, **kw})}) == status, kw
+
+
+def test_forward(route):
+    given = dict(Y=A[30])
+    _tensors(_forward, given)
+    assert _forward(Y=A[30], ws=None) == 1 and _forward(Y=A[30], y=None) == 1
+    for name in ("so", "Y", "ws"):
+        assert _forward(**{**given, name: A[31] + 8}) == 4
+    assert _forward(Y=A[30], lengths=A[31] + 2) == 4
+    for same in range(5):
+        assert _forward(Y=A[same]) == 2
+    assert _forward(Y=A[30], so=A[8] + 16) == 2
+    assert _forward(Y=A[30], wb=64) == 6
+
+
+def test_token(route):
+    given = dict(Y=A[30])
+    _tensors(_token, given)
+    for name in ("si", "so"):
+        assert _token(**{**given, name: None}) == 1
+    assert _token(Y=A[30], slots=A[31] + 2) == 4
+    long = dict(u=_desc(), z=_desc(), y=_desc(), bc=_bc())
+    assert _token(Y=A[30], **long) == 2 and _token(Y=A[30], n=0) == 2
+    two = _desc(N=1, B=5, stride_b=1 << 20)
+    assert _token(Y=A[30], u=two, z=two, y=two, bc=_bc(N=1, B=5, stride_b=64)) == 2
+    for same in range(5):
+        assert _token(Y=A[same]) == 2
+    assert _token(Y=A[30], so=A[8] + 16) == 2
+
+
+def test_backward(route):
+    given = dict(dU=A[30])
+    _tensors(_backward, given)
+    for name in ("dY", "dDT", "dZ", "dB", "dC", "ws"):
+        assert _backward(**{**given, name: None}) == 1, name
+    for name in ("dY", "dU", "dDT", "dZ", "dB", "dC", "dso", "dsi", "dA", "ws"):
+        assert _backward(**{**given, name: A[31] + 8}) == 4, name
+    for name in ("dbias", "dskip"):
+        assert _backward(**{**given, name: A[31] + 2}) == 4, name
+    assert _backward(dU=A[30], dy=None) == 1 and _backward(dU=A[30], dy=_desc(N=64)) == 2
+    for name, at in (("dU", 0), ("dU", 1), ("dU", 5), ("dU", 12), ("dB", 3), ("dC", 14), ("dA", 6), ("dbias", 19), ("dskip", 8), ("dZ", 2), ("dsi", 9)):
+        assert _backward(**{**given, name: A[at]}) == 2, (name, at)
+    assert _backward(dU=A[30], dsi=A[10] + 64) == 2 and _backward(dU=A[30], dsi=A[9] + 64) == 2
+    assert _backward(dU=A[30], wb=1 << 10) == 6
+
+
+def test_workspaces():
+    f, g = sv.sv_selective_scan_workspace_bytes, sv.sv_selective_scan_backward_workspace_bytes
+    for bad in ((0, 1, 1, 8, 16), (1, 0, 1, 8, 16), (1, 1, 0, 8, 16), (1, 1, 1, 0, 16), (1, 1, 1, 6, 16), (1, 1, 1, 8196, 16), (1, 1, 1, 8, 12), (1 << 13, 1 << 12, 1, 8, 8)):
+        assert f(*bad) == 0 and g(*bad[:4], 1, bad[4]) == 0
+    assert g(1, 4, 10, 8, 3, 16) == 0 and g(1, 4, 10, 8, 0, 16) == 0
+    for B, H, d, G, n in ((1, 1, 2240, 1, 16), (2, 20, 112, 4, 8), (7, 2, 32, 2, 16)):
+        last = 0, 0
+        for N in (1, 31, 32, 33, 64, 500, 4680, 32760, 75600):         # never less for more tokens or batches
+            now = f(B, H, N, d, n), g(B, H, N, d, G, n)
+            assert now[0] >= last[0] and now[1] > last[1]
+            assert f(B + 1, H, N, d, n) >= now[0] and g(B + 1, H, N, d, G, n) > now[1]
+            last = now
+
+
+def test_plans(tmp_path):
+    exe = tmp_path / "plan"
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", os.path.join(ROOT, "tests", "host_scan_plan.cpp"), "-o", str(exe)], check=True)
+    subprocess.run([str(exe)], check=True)
