@@ -1,7 +1,7 @@
 /*
- * sv_norm.h - C ABI of layer norm and its backward pass (MI355X, gfx950; part of libsvlinattn.so).
+ * sv_norm.h - C ABI of layer norm and group norm and their backward passes (MI355X, gfx950; part of libsvlinattn.so).
  *
- * Over each row x of width d of a token tensor [B][H][N][d]:
+ * Layer norm, over each row x of width d of a token tensor [B][H][N][d]:
  *
  *     mean = sum x / d,   rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),   xh = (x - mean) rstd,   y = w xh + b
  *
@@ -12,6 +12,16 @@
  * Gradients, with t = w dy:
  *
  *     dx = rstd (t - sum t / d - xh sum (t xh) / d),   dw = sum over rows of dy xh,   db = sum over rows of dy
+ *
+ * Group norm of channels-last hidden states, with an activation: the N rows of a (b, h) - a frame, a clip - share a mean and an rstd in
+ * each of G groups of d / G neighbouring channels:
+ *
+ *     mean = sum x / (N d / G),   rstd = 1 / sqrt(sum (x - mean)^2 / (N d / G) + eps),   xh = (x - mean) rstd,   a = w xh + b
+ *     y = a  or  y = silu(a) = a / (1 + exp(-a))
+ *
+ * Gradients, with da = dy  or  dy silu'(a), and t = w da (means over the rows and channels of a group):
+ *
+ *     dx = rstd (t - mean of t - xh mean of (t xh)),   dw = sum over all rows of da xh,   db = sum over all rows of da
  */
 #ifndef SV_NORM_H
 #define SV_NORM_H
@@ -46,6 +56,32 @@ sv_status sv_layernorm_backward(const void *X, const sv_tensor_desc *x, const vo
                                 const float *weight, int32_t weight_heads, const float *mean, const float *rstd,
                                 void *dX, const sv_tensor_desc *dx, float *dweight, float *dbias,
                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of device workspace of sv_groupnorm and of sv_groupnorm_backward for hidden states [B][H][N][d] in G groups (either dtype); no
+ * preparation needed.  What a call needs does for every call with no more batches, heads and rows and the same d and G.  Pure host
+ * functions; 0 for unsupported sizes. */
+size_t sv_groupnorm_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t groups);
+size_t sv_groupnorm_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t groups);
+
+/* Forward.  x describes X, y describes Y: same B, H, N, d and dtype, strides of their own (frames of a clip [B][T][HW][D] are H = T, N =
+ * HW: statistics of each frame; H = 1, N = T HW: of the whole clip).  d is any multiple of 8 (SV_BF16) or 4 (SV_F32) up to 8192, groups any
+ * divisor of d (groups need not be whole 16-byte pieces).  Y may be X if x and y have the same strides.
+ *  weight, bias   fp32 [d] device, 16-byte aligned, or NULL (ones, zeros)
+ *  silu           0 or 1
+ *  mean, rstd     fp32 [B][H][groups] device, or both NULL: kept for the backward pass
+ *  eps            >= 0 and finite (0 with a group of equal values gives infinities or NaN)
+ * Sums are fp64.  Conventions and errors as in sv_linattn.h; plain kernels, which may be captured into a HIP graph from the first call
+ * on; two calls that overlap in time need a workspace each; results are bit-reproducible. */
+sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const float *weight, const float *bias, int32_t groups, float eps,
+                       int32_t silu, void *Y, const sv_tensor_desc *y, float *mean, float *rstd, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* Backward.  dY (described by dy), mean and rstd as the forward call left them, weight and bias as it had them.  dX (described by dx)
+ * may be dY if dy and dx have the same strides.  dweight, dbias: fp32 [d], overwritten; each may be NULL. */
+sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *x, const void *dY, const sv_tensor_desc *dy, const float *weight,
+                                const float *bias, int32_t groups, int32_t silu, const float *mean, const float *rstd, void *dX,
+                                const sv_tensor_desc *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                                void *stream);
 
 #ifdef __cplusplus
 }

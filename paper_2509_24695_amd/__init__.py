@@ -17,5 +17,5 @@ from .binding import (  # noqa: F401
     sv_decay_linattn_backward, sv_rope3d_rotate, sv_layernorm, sv_layernorm_backward_workspace_bytes, sv_layernorm_backward,
     sv_causal_conv, sv_causal_conv_token, sv_causal_conv_backward_workspace_bytes, sv_causal_conv_backward,
     sv_selective_scan_workspace_bytes, sv_selective_scan_backward_workspace_bytes, sv_selective_scan, sv_selective_scan_token,
-    sv_selective_scan_backward,
+    sv_selective_scan_backward, sv_groupnorm_workspace_bytes, sv_groupnorm_backward_workspace_bytes, sv_groupnorm, sv_groupnorm_backward,
 )

@@ -32,7 +32,7 @@ EXPORTS = (
     "sv_layernorm_backward_workspace_bytes", "sv_layernorm_backward",
     "sv_causal_conv", "sv_causal_conv_token", "sv_causal_conv_backward_workspace_bytes", "sv_causal_conv_backward",
     "sv_selective_scan_workspace_bytes", "sv_selective_scan_backward_workspace_bytes", "sv_selective_scan", "sv_selective_scan_token",
-    "sv_selective_scan_backward",
+    "sv_selective_scan_backward", "sv_groupnorm_workspace_bytes", "sv_groupnorm_backward_workspace_bytes", "sv_groupnorm", "sv_groupnorm_backward",
 )
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -147,6 +147,12 @@ def load_library():
     lib.sv_selective_scan_backward.argtypes = [vp, vp, dp, vp, dp, vp, vp, dp, vp, dp] + [vp] * 15 + [vp, sz, vp]
     for f in (lib.sv_selective_scan, lib.sv_selective_scan_token, lib.sv_selective_scan_backward):
         f.restype = ctypes.c_int
+    for f in (lib.sv_groupnorm_workspace_bytes, lib.sv_groupnorm_backward_workspace_bytes):
+        f.argtypes, f.restype = [i32, i32, i32, i32, i32], sz
+    lib.sv_groupnorm.argtypes = [vp, dp, vp, vp, i32, fl, i32, vp, dp, vp, vp, vp, sz, vp]
+    lib.sv_groupnorm_backward.argtypes = [vp, dp, vp, dp, vp, vp, i32, i32, vp, vp, vp, dp, vp, vp, vp, sz, vp]
+    for f in (lib.sv_groupnorm, lib.sv_groupnorm_backward):
+        f.restype = ctypes.c_int
     for f in (lib.sv_decay_linattn, lib.sv_decay_linattn_token, lib.sv_decay_linattn_backward, lib.sv_rope3d_rotate, lib.sv_layernorm,
               lib.sv_layernorm_backward):
         f.restype = ctypes.c_int
@@ -200,7 +206,8 @@ class _CtypesCalls:
         fn = getattr(self._functions, name)
         types, last = fn.argtypes, len(fn.argtypes) - 1
         flag = 6 - (types[3] is ctypes.c_int32) if name.startswith("sv_linattn_state") else -1      # `accumulate`
-        flag = {"sv_rope3d_rotate": 5, "sv_causal_conv": 5, "sv_causal_conv_token": 5, "sv_causal_conv_backward": 7}.get(name, flag)   # `inverse`, `silu`
+        flag = {"sv_rope3d_rotate": 5, "sv_causal_conv": 5, "sv_causal_conv_token": 5, "sv_causal_conv_backward": 7,
+                "sv_groupnorm": 6, "sv_groupnorm_backward": 7}.get(name, flag)   # `inverse`, `silu`
 
         def convert(args, i):
             x, t = args[i], types[i]
@@ -538,6 +545,28 @@ def sv_selective_scan_backward(U, DT, u: TensorDesc, Z, z: TensorDesc | None, Bm
     _check((_entry or _calls()).sv_selective_scan_backward(U, DT, u, Z, z, Bm, Cm, bc, dY, dy, A, dt_bias, skip, lengths, S_in, dS_out, dU, dDT, dZ, dB,
                                                            dC, dS_in, dA, ddt_bias, dskip, workspace, workspace_bytes, stream),
            "sv_selective_scan_backward")
+
+
+def sv_groupnorm_workspace_bytes(B: int, H: int, n_tokens: int, d: int, groups: int) -> int:
+    return int(load_library().sv_groupnorm_workspace_bytes(int(B), int(H), int(n_tokens), int(d), int(groups)))
+
+
+def sv_groupnorm_backward_workspace_bytes(B: int, H: int, n_tokens: int, d: int, groups: int) -> int:
+    return int(load_library().sv_groupnorm_backward_workspace_bytes(int(B), int(H), int(n_tokens), int(d), int(groups)))
+
+
+def sv_groupnorm(X, x: TensorDesc, weight, bias, groups: int, eps: float, silu, Y, y: TensorDesc, mean, rstd, workspace,
+                 workspace_bytes: int | None = None, stream=None) -> None:
+    """Group norm of channels-last hidden states, with its activation (include/sv_norm.h): weight, bias [d] fp32 or None, mean, rstd
+    [B][H][groups] fp32 or None."""
+    _check((_entry or _calls()).sv_groupnorm(X, x, weight, bias, groups, eps, silu, Y, y, mean, rstd, workspace, workspace_bytes, stream), "sv_groupnorm")
+
+
+def sv_groupnorm_backward(X, x: TensorDesc, dY, dy: TensorDesc, weight, bias, groups: int, silu, mean, rstd, dX, dx: TensorDesc, dweight, dbias,
+                          workspace, workspace_bytes: int | None = None, stream=None) -> None:
+    """Gradients of sv_groupnorm for X, weight and bias (include/sv_norm.h)."""
+    _check((_entry or _calls()).sv_groupnorm_backward(X, x, dY, dy, weight, bias, groups, silu, mean, rstd, dX, dx, dweight, dbias, workspace,
+                                                      workspace_bytes, stream), "sv_groupnorm_backward")
 
 
 def sv_measure_apply_variant(variant: int, Q, q: TensorDesc, tok_begin: int, tok_end: int, S, z, eps: float, O,

@@ -12,8 +12,8 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsvlinattn.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("sv_linattn.hip", "sv_tconv.hip", "sv_decay.hip", "sv_rotate.hip", "sv_norm.hip", "sv_conv.hip", "sv_scan.hip",
-                                              "sv_measure.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sv_linattn.hip", "sv_tconv.hip", "sv_decay.hip", "sv_rotate.hip", "sv_norm.hip", "sv_group.hip", "sv_conv.hip",
+                                              "sv_scan.hip", "sv_measure.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

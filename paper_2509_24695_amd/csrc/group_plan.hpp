@@ -1,0 +1,40 @@
+// How the rows of a group norm are dealt to workgroups.  Plain C++ (no device code), shared by the launchers and host-side tests.
+#pragma once
+
+#include <stdint.h>
+
+namespace sv {
+
+// A workgroup is `across` 16-byte pieces by `down` rows, and walks a chunk of the rows of one (b, h).
+constexpr int kGroupThreads = 256, kGroupAhead = 4;
+struct GroupCut {
+    int across, down;
+    int64_t tiles, chunks;             // workgroups across the channels; chunks of the N rows
+    int64_t rows;                      // of a chunk, a multiple of `down`
+};
+// As many chunks as give `most` workgroups, of at least kGroupAhead rows a thread.
+inline GroupCut group_cut(int64_t BH, int64_t N, int64_t pieces, int64_t most)
+{
+    GroupCut c{};
+    c.across = 32;
+    while (c.across > 4 && c.across / 2 >= pieces) c.across /= 2;
+    c.down = kGroupThreads / c.across;
+    c.tiles = (pieces + c.across - 1) / c.across;
+    const int64_t step = (int64_t)c.down * kGroupAhead, steps = (N + step - 1) / step;
+    int64_t chunks = most / (BH * c.tiles);
+    chunks = chunks > steps ? steps : chunks < 1 ? 1 : chunks;
+    c.rows = (steps + chunks - 1) / chunks * step;
+    c.chunks = (N + c.rows - 1) / c.rows;
+    return c;
+}
+constexpr int64_t kGroupSumWgs = 1024, kGroupApplyWgs = 4096;
+
+// Chunks times channels of all (b, h) together in the largest call with no more batches, heads and rows and the same d: with one chunk each
+// these are BH d, with more there are at most kGroupSumWgs workgroups of 32 pieces of at most eight channels; and a chunk has at least 32 rows.
+inline int64_t group_slots(int64_t BH, int64_t N, int64_t d)
+{
+    const int64_t most = BH * d > kGroupSumWgs * 256 ? BH * d : kGroupSumWgs * 256, all = BH * ((N + 31) / 32) * d;
+    return all < most ? all : most;
+}
+
+}  // namespace sv

@@ -248,6 +248,8 @@ ENTRY(sv_causal_conv_backward, P, Desc, P, Desc, P, P, Int, Flag, P, P, P, P, De
 ENTRY(sv_selective_scan, P, P, Desc, P, Desc, P, P, Desc, P, P, P, P, P, P, P, Desc, P, Bytes, Stream)
 ENTRY(sv_selective_scan_token, P, P, Desc, P, Desc, P, P, Desc, P, P, P, P, Int, P, P, P, Desc, Stream)
 ENTRY(sv_selective_scan_backward, P, P, Desc, P, Desc, P, P, Desc, P, Desc, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, Bytes, Stream)
+ENTRY(sv_groupnorm, P, Desc, P, P, Int, Eps, Flag, P, Desc, P, P, P, Bytes, Stream)
+ENTRY(sv_groupnorm_backward, P, Desc, P, Desc, P, P, Int, Flag, P, P, P, Desc, P, P, P, Bytes, Stream)
 
 // attach(handle): the entry points of the loaded library with this dlopen handle.
 PyObject *attach(PyObject *, PyObject *handle)
@@ -270,7 +272,7 @@ PyObject *attach(PyObject *, PyObject *handle)
     X(sv_block_linattn_step_rope3d) X(sv_block_linattn_lookahead_rope3d) X(sv_tconv_block_step)        \
     X(sv_decay_linattn) X(sv_decay_linattn_token) X(sv_decay_linattn_backward) X(sv_rope3d_rotate) X(sv_layernorm)     \
     X(sv_layernorm_backward) X(sv_causal_conv) X(sv_causal_conv_token) X(sv_causal_conv_backward) \
-    X(sv_selective_scan) X(sv_selective_scan_token) X(sv_selective_scan_backward)
+    X(sv_selective_scan) X(sv_selective_scan_token) X(sv_selective_scan_backward) X(sv_groupnorm) X(sv_groupnorm_backward)
     EACH(ATTACH)
     Py_RETURN_NONE;
 }

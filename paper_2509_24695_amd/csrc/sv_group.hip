@@ -1,0 +1,152 @@
+// C ABI of group norm (include/sv_norm.h): argument checks and launches.
+#include "../../include/sv_norm.h"
+
+#include <math.h>
+
+#include "desc_checks.hpp"
+#include "group.hpp"
+
+namespace {
+
+using namespace sv;
+
+sv_status check_hidden(const sv_tensor_desc *t, int groups, Shape *s)
+{
+    const sv_status rc = check_rows(t, s);
+    if (rc != SV_OK) return rc;
+    return groups <= 0 || s->d % groups ? SV_ERR_SHAPE : SV_OK;
+}
+
+bool sizes_ok(int32_t B, int32_t H, int32_t N, int32_t d, int32_t groups)
+{
+    return B > 0 && H > 0 && N > 0 && d > 0 && d % 4 == 0 && d <= kMostRowWidth && groups > 0 && d % groups == 0 && (int64_t)B * H <= kMostHeads;
+}
+
+int64_t lines(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+GroupArgs group_args(const Shape &x, int groups, void *workspace)
+{
+    GroupArgs a{};
+    a.sx = x.st;
+    a.H = x.H; a.N = x.N; a.d = x.d; a.G = groups; a.width = x.d / groups;
+    a.BH = x.BH;
+    a.level = static_cast<float *>(workspace);
+    a.scale = a.level + a.BH * groups;
+    a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + lines(2 * a.BH * groups * (int64_t)sizeof(float)));
+    return a;
+}
+// The workgroups of a launch; 0: more than a launch has.
+unsigned cut_args(GroupArgs &a, const GroupCut &c)
+{
+    a.across = c.across;
+    a.tiles = (int)c.tiles;
+    a.chunks = (int)c.chunks;
+    a.rows = c.rows;
+    const int64_t grid = a.BH * c.tiles * c.chunks;
+    return grid_ok(grid, kGroupThreads) ? (unsigned)grid : 0;
+}
+
+template <typename F> void with_group(bool bf16, int silu, F &&f)
+{
+    auto act = [&](auto t) {
+        if (silu) f(t, std::true_type{});
+        else f(t, std::false_type{});
+    };
+    if (bf16) act(uint16_t{});
+    else act(float{});
+}
+
+size_t workspace_bytes_of(int32_t B, int32_t H, int32_t N, int32_t d, int32_t groups, size_t number)
+{
+    if (!sizes_ok(B, H, N, d, groups)) return 0;
+    const int64_t BH = (int64_t)B * H;
+    return (size_t)lines(2 * BH * groups * (int64_t)sizeof(float)) + (size_t)group_slots(BH, N, d) * 2 * number;
+}
+
+}  // namespace
+
+extern "C" size_t sv_groupnorm_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t groups)
+{
+    return workspace_bytes_of(B, H, n_tokens, d, groups, sizeof(double));
+}
+
+extern "C" size_t sv_groupnorm_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t groups)
+{
+    return workspace_bytes_of(B, H, n_tokens, d, groups, sizeof(float));
+}
+
+extern "C" sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const float *weight, const float *bias, int32_t groups, float eps, int32_t silu,
+                                  void *Y, const sv_tensor_desc *y, float *mean, float *rstd, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!X || !Y || !workspace || (mean == nullptr) != (rstd == nullptr)) return SV_ERR_NULL;
+    Shape in, out;
+    sv_status rc = check_hidden(x, groups, &in);
+    if (rc != SV_OK) return rc;
+    rc = check_hidden(y, groups, &out);
+    if (rc != SV_OK) return rc;
+    if (!same_shape(in, out)) return SV_ERR_SHAPE;
+    if (!all_aligned({X, Y, weight, bias, mean, rstd, workspace})) return SV_ERR_ALIGN;
+    if (!isfinite(eps) || eps < 0.f || silu < 0 || silu > 1) return SV_ERR_RANGE;
+    if ((Y == X && !same_rows(in, out)) || (mean && mean == rstd)) return SV_ERR_SHAPE;
+    GroupArgs a = group_args(in, groups, workspace);
+    const int pieces = in.d * in.elem_bytes / 16;
+    const GroupCut sums = group_cut(a.BH, a.N, pieces, kGroupSumWgs), rows = group_cut(a.BH, a.N, pieces, kGroupApplyWgs);
+    if (workspace_bytes < (size_t)(reinterpret_cast<char *>(a.sums) - static_cast<char *>(workspace)) + (size_t)a.BH * sums.chunks * 2 * a.d * sizeof(double))
+        return SV_ERR_WORKSPACE;
+    a.x = X; a.y = Y; a.sy = out.st;
+    a.weight = weight; a.bias = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
+    a.whole_lines = lines_whole(out);
+    GroupArgs b = a;
+    const unsigned sum_grid = cut_args(a, sums), row_grid = cut_args(b, rows);
+    const int64_t fold = (a.BH * a.G + kGroupThreads / 64 - 1) / (kGroupThreads / 64);
+    if (!sum_grid || !row_grid || !grid_ok(fold, kGroupThreads)) return SV_ERR_SHAPE;
+    a.sum_chunks = b.sum_chunks = (int)sums.chunks;
+    const auto hs = static_cast<hipStream_t>(stream);
+    if (in.bf16) group_sums<uint16_t><<<sum_grid, kGroupThreads, 0, hs>>>(a);
+    else group_sums<float><<<sum_grid, kGroupThreads, 0, hs>>>(a);
+    if (launched() != SV_OK) return SV_ERR_LAUNCH;
+    group_fold<<<(unsigned)fold, kGroupThreads, 0, hs>>>(a);
+    if (launched() != SV_OK) return SV_ERR_LAUNCH;
+    with_group(in.bf16, silu, [&](auto t, auto s) { group_apply<decltype(t), s()><<<row_grid, kGroupThreads, 0, hs>>>(b); });
+    return launched();
+}
+
+extern "C" sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *x, const void *dY, const sv_tensor_desc *dy, const float *weight,
+                                           const float *bias, int32_t groups, int32_t silu, const float *mean, const float *rstd, void *dX,
+                                           const sv_tensor_desc *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!X || !dY || !mean || !rstd || !dX || !workspace) return SV_ERR_NULL;
+    Shape in, grad, out;
+    sv_status rc = check_hidden(x, groups, &in);
+    if (rc != SV_OK) return rc;
+    rc = check_hidden(dy, groups, &grad);
+    if (rc != SV_OK) return rc;
+    rc = check_hidden(dx, groups, &out);
+    if (rc != SV_OK) return rc;
+    if (!same_shape(in, grad) || !same_shape(in, out)) return SV_ERR_SHAPE;
+    if (!all_aligned({X, dY, weight, bias, mean, rstd, dX, dweight, dbias, workspace})) return SV_ERR_ALIGN;
+    if (silu < 0 || silu > 1) return SV_ERR_RANGE;
+    if (dX == X || (dX == dY && !same_rows(grad, out)) || (dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == bias)) return SV_ERR_SHAPE;
+    GroupArgs a = group_args(in, groups, workspace);
+    const int pieces = in.d * in.elem_bytes / 16;
+    const GroupCut sums = group_cut(a.BH, a.N, pieces, kGroupSumWgs), rows = group_cut(a.BH, a.N, pieces, kGroupApplyWgs);
+    if (workspace_bytes < (size_t)(reinterpret_cast<char *>(a.sums) - static_cast<char *>(workspace)) + (size_t)a.BH * sums.chunks * 2 * a.d * sizeof(float))
+        return SV_ERR_WORKSPACE;
+    a.x = X; a.dy = dY; a.y = dX; a.sdy = grad.st; a.sy = out.st;
+    a.weight = weight; a.bias = bias; a.dw = dweight; a.db = dbias;
+    a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
+    a.whole_lines = lines_whole(out);
+    GroupArgs b = a;
+    const unsigned sum_grid = cut_args(a, sums), row_grid = cut_args(b, rows);
+    int64_t fold = (a.BH * a.G + kGroupThreads / 64 - 1) / (kGroupThreads / 64);
+    if (dweight || dbias) fold += (2 * a.d + 15) / 16;
+    if (!sum_grid || !row_grid || !grid_ok(fold, kGroupThreads)) return SV_ERR_SHAPE;
+    a.sum_chunks = b.sum_chunks = (int)sums.chunks;
+    const auto hs = static_cast<hipStream_t>(stream);
+    with_group(in.bf16, silu, [&](auto t, auto s) { group_back_sums<decltype(t), s()><<<sum_grid, kGroupThreads, 0, hs>>>(a); });
+    if (launched() != SV_OK) return SV_ERR_LAUNCH;
+    group_back_fold<<<(unsigned)fold, kGroupThreads, 0, hs>>>(a);
+    if (launched() != SV_OK) return SV_ERR_LAUNCH;
+    with_group(in.bf16, silu, [&](auto t, auto s) { group_back_apply<decltype(t), s()><<<row_grid, kGroupThreads, 0, hs>>>(b); });
+    return launched();
+}
