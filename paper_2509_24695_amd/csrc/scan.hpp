@@ -53,7 +53,7 @@ struct ScanPlace {
         u = b * a.su.b + h * a.su.h + i;
         z = b * a.sz.b + h * a.sz.h + i;
         y = b * a.sy.b + h * a.sy.h + i;
-        length = held_length(a.lengths, b, a.N);
+        length = b < a.B ? held_length(a.lengths, b, a.N) : 0;
         first = segment * a.per_segment;
         const int64_t end = (int64_t)first + a.per_segment;
         last = end < length ? (int)end : length;
@@ -61,7 +61,8 @@ struct ScanPlace {
     __device__ __forceinline__ int64_t slot(const ScanArgs &a) const { return (int64_t)b * a.segments + segment; }
 };
 
-// n numbers that are the same for all lanes, out of the scalar cache.
+// n numbers that are the same for all lanes, out of the scalar cache.  Scalar loads come back in any order, so a wait for one waits for all:
+// arrive() makes it in front of the request for the next token's numbers, which then are on their way for a whole token.
 template <typename T, int n> struct Scalars;
 template <int n> struct Scalars<float, n> {
     uint32_t w[n];
@@ -72,6 +73,11 @@ template <int n> struct Scalars<float, n> {
         for (int i = 0; i < n; ++i) w[i] = p[i];
     }
     __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int i = 0; i < n; ++i) asm volatile("" : "+s"(w[i]));
+    }
 };
 template <int n> struct Scalars<uint16_t, n> {
     uint32_t w[n / 2];
@@ -82,6 +88,11 @@ template <int n> struct Scalars<uint16_t, n> {
         for (int i = 0; i < n / 2; ++i) w[i] = p[i];
     }
     __device__ __forceinline__ float operator[](int i) const { return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]); }
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) asm volatile("" : "+s"(w[i]));
+    }
 };
 
 // A channel's A, times log2(e): exp(D A) = 2^(D A2).
@@ -113,16 +124,17 @@ template <int n> __device__ __forceinline__ void store_state(float *p, int64_t r
 // nothing stays one.
 __device__ __forceinline__ float kept(float A2, float steps) { return fminf(__builtin_amdgcn_exp2f(A2 * steps), 3.40282347e38f); }
 
-// Numbers of kAhead tokens on their way.
+// Numbers of AHEAD tokens on their way, as they lie in memory (a conversion here would wait for them).  Past the last token the last one
+// is read again: no branch stands between the loads.
 template <typename T, int AHEAD> struct Ahead {
-    float x[AHEAD];
+    T raw[AHEAD];
     __device__ __forceinline__ void request(const void *base, int64_t at, int64_t stride, int t, int last)
     {
         const T *p = static_cast<const T *>(base) + at;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (t + i < last) x[i] = Elem<T>::load(p + (t + i) * stride);
+        for (int i = 0; i < AHEAD; ++i) raw[i] = p[(t + i < last ? t + i : last - 1) * stride];
     }
+    __device__ __forceinline__ float operator[](int i) const { return Elem<T>::load(&raw[i]); }
 };
 
 constexpr int kScanAhead = 4;
@@ -136,31 +148,43 @@ template <typename T, int n, bool MARKS> __device__ __forceinline__ void scan_su
 #pragma unroll
     for (int i = 0; i < n; ++i) h[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
-    Ahead<T, kScanAhead> u{}, dt{};
-    u.request(a.u, at.u, a.su.n, at.first, at.last);
-    dt.request(a.dt, at.u, a.su.n, at.first, at.last);
-    for (int t0 = at.first; t0 < at.last; t0 += kScanAhead) {
-        if (MARKS && t0 % kScanRun == 0 && t0 != at.first && at.mine) {
-            const int64_t mark = (int64_t)at.b * a.runs + t0 / kScanRun;
+    Ahead<T, kScanAhead> u, dt;
+    auto request = [&](int t) {
+        u.request(a.u, at.u, a.su.n, t, at.last);
+        dt.request(a.dt, at.u, a.su.n, t, at.last);
+    };
+    request(at.first);
+    Scalars<T, n> next;
+    next.load(a.bm, bc + at.first * a.sbc.n);
+    auto token = [&](int t, float ut, float dtt) {
+        Scalars<T, n> B = next;
+        B.arrive();
+        next.load(a.bm, bc + (t + 1 < at.last ? t + 1 : t) * a.sbc.n);
+        __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
+        const float D = softplus(dtt + bias), x = D * ut;
+        steps += D;
 #pragma unroll
-            for (int i = 0; i < n; ++i) a.marks[(mark * n + i) * a.channels + at.channel] = h[i];
-            a.mark_steps[mark * a.channels + at.channel] = steps;
-        }
+        for (int i = 0; i < n; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
+    };
+    auto mark = [&](int t) {
+        if (!MARKS || t % kScanRun || t == at.first || t >= at.last || !at.mine) return;
+        const int64_t mark = (int64_t)at.b * a.runs + t / kScanRun;
+#pragma unroll
+        for (int i = 0; i < n; ++i) a.marks[(mark * n + i) * a.channels + at.channel] = h[i];
+        a.mark_steps[mark * a.channels + at.channel] = steps;
+    };
+    int t = at.first;
+    for (; t + kScanAhead <= at.last; t += kScanAhead) {
+        mark(t);
         const Ahead<T, kScanAhead> u0 = u, dt0 = dt;
-        u.request(a.u, at.u, a.su.n, t0 + kScanAhead, at.last);
-        dt.request(a.dt, at.u, a.su.n, t0 + kScanAhead, at.last);
+        request(t + kScanAhead);
 #pragma unroll
-        for (int k = 0; k < kScanAhead; ++k) {
-            const int t = t0 + k;
-            if (t >= at.last) break;
-            Scalars<T, n> B;
-            B.load(a.bm, bc + t * a.sbc.n);
-            const float D = softplus(dt0.x[k] + bias), x = D * u0.x[k];
-            steps += D;
-#pragma unroll
-            for (int i = 0; i < n; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
-        }
+        for (int k = 0; k < kScanAhead; ++k) token(t + k, u0[k], dt0[k]);
     }
+    mark(t);
+#pragma unroll
+    for (int k = 0; k < kScanAhead; ++k)
+        if (t + k < at.last) token(t + k, u[k], dt[k]);
     if (!at.mine) return;
 #pragma unroll
     for (int i = 0; i < n; ++i) a.states[(at.slot(a) * n + i) * a.channels + at.channel] = h[i];
@@ -170,52 +194,53 @@ template <typename T, int n, bool MARKS> __device__ __forceinline__ void scan_su
 template <typename T, int n> __global__ __launch_bounds__(kScanWave) void scan_sums(ScanArgs a)
 {
     // (the last segment's sum is not needed)
-    const uint32_t per_b = (uint32_t)a.blocks * (a.segments - 1), b = blockIdx.x / per_b;
-    const ScanPlace at(a, b * (uint32_t)a.blocks * a.segments + (blockIdx.x - b * per_b));
+    const uint32_t per_b = (uint32_t)a.blocks * (a.segments - 1), task = scan_task(blockIdx.x, gridDim.x), b = task / per_b;
+    if ((int)b >= a.B) return;
+    const ScanPlace at(a, b * (uint32_t)a.blocks * a.segments + (task - b * per_b));
     if (at.first >= at.length) return;
     scan_sum_forward<T, n, false>(a, at);
 }
 
 // The states that the segments begin from, in place of what the segments before add; backwards (BACK) the gradients that arrive at their ends.
-template <int n, bool BACK> __device__ __forceinline__ void scan_state(const ScanArgs &a, int64_t id)
+// (a workgroup is 256 state numbers of one sequence: the segments' addresses are scalar)
+template <int n, bool BACK> __device__ __forceinline__ void scan_state(const ScanArgs &a, int block)
 {
-    const int c = (int)(id % a.channels), i = (int)(id / a.channels % n), b = (int)(id / a.channels / n);
+    const int tiles = (a.channels * n + 255) / 256, b = block / tiles, at = (block - b * tiles) * 256 + (int)threadIdx.x;
+    if (at >= a.channels * n) return;
+    const int i = at / a.channels, c = at - i * a.channels;
     const float A2 = a.A[(int64_t)c * n + i] * kLog2E;
     const float *from = BACK ? a.ds_out : a.s_in;
-    float *slots = (BACK ? a.grads : a.states) + ((int64_t)b * a.segments * n + i) * a.channels + c;
-    const float *steps = a.steps + (int64_t)b * a.segments * a.channels + c;
+    const int64_t stride = (int64_t)n * a.channels;
+    float *slots = (BACK ? a.grads : a.states) + (int64_t)b * a.segments * stride;
+    const float *steps = a.steps + (int64_t)b * a.segments * a.channels;
     float s = from ? from[((int64_t)b * a.channels + c) * n + i] : 0.f;
     const int length = held_length(a.lengths, b, a.N), used = length ? (length - 1) / a.per_segment + 1 : 1;
-    const int64_t stride = (int64_t)n * a.channels;
-    constexpr int kAhead = 8;
+    constexpr int kAhead = 32;
     for (int k0 = 0; k0 < used; k0 += kAhead) {
         float add[kAhead], sum[kAhead];
+        auto segment = [&](int k) { return BACK ? used - 1 - k0 - k : k0 + k; };
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int seg = BACK ? used - 1 - k0 - k : k0 + k;
-            const bool in = BACK ? seg > 0 : seg + 1 < used;          // the walk's last segment hands nothing on
-            add[k] = in ? slots[seg * stride] : 0.f;
-            sum[k] = in ? steps[(int64_t)seg * a.channels] : 0.f;
+            int seg = segment(k);                                     // the walk's last segment hands nothing on: any other is read in its place
+            if (BACK) seg = seg > 0 ? seg : used - 1;
+            else seg = seg + 1 < used ? seg : 0;
+            add[k] = (slots + seg * stride)[at];
+            sum[k] = (steps + (int64_t)seg * a.channels)[c];
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int seg = BACK ? used - 1 - k0 - k : k0 + k;
-            if (k0 + k >= used) break;
-            slots[seg * stride] = s;
-            s = __builtin_fmaf(kept(A2, sum[k]), s, add[k]);
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (k0 + k < used) {
+                (slots + segment(k) * stride)[at] = s;
+                s = __builtin_fmaf(kept(A2, sum[k]), s, add[k]);
+            }
     }
 }
-template <int n> __global__ __launch_bounds__(256) void scan_states(ScanArgs a)
-{
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id < (int64_t)a.B * a.channels * n) scan_state<n, false>(a, id);
-}
+template <int n> __global__ __launch_bounds__(256) void scan_states(ScanArgs a) { scan_state<n, false>(a, (int)blockIdx.x); }
 
 template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_walk(ScanArgs a)
 {
-    const ScanPlace at(a, blockIdx.x);
-    if (at.first >= at.length && at.segment > 0) return;
+    const ScanPlace at(a, scan_task(blockIdx.x, gridDim.x));
+    if (at.b >= a.B || (at.first >= at.length && at.segment > 0)) return;
     float A2[n], h[n];
     load_rates<n>(a, at.channel, A2);
     const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f, skip = a.skip ? a.skip[at.channel] : 0.f;
@@ -225,34 +250,47 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) 
         for (int i = 0; i < n; ++i) h[i] = a.states[(at.slot(a) * n + i) * a.channels + at.channel];
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
     T *y = static_cast<T *>(a.y) + at.y;
-    Ahead<T, kScanAhead> u{}, dt{}, z{};
+    Ahead<T, kScanAhead> u, dt, z;
     auto request = [&](int t) {
         u.request(a.u, at.u, a.su.n, t, at.last);
         dt.request(a.dt, at.u, a.su.n, t, at.last);
         if (GATE) z.request(a.z, at.z, a.sz.n, t, at.last);
     };
-    request(at.first);
-    for (int t0 = at.first; t0 < at.last; t0 += kScanAhead) {
-        const Ahead<T, kScanAhead> u0 = u, dt0 = dt, z0 = z;
-        request(t0 + kScanAhead);
-#pragma unroll
-        for (int k = 0; k < kScanAhead; ++k) {
-            const int t = t0 + k;
-            if (t >= at.last) break;
-            Scalars<T, n> B, C;
-            B.load(a.bm, bc + t * a.sbc.n);
-            C.load(a.cm, bc + t * a.sbc.n);
-            const float D = softplus(dt0.x[k] + bias), x = D * u0.x[k];
-            float out = skip * u0.x[k];
-#pragma unroll
-            for (int i = 0; i < n; ++i) {
-                h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
-                out = __builtin_fmaf(C[i], h[i], out);
-            }
-            if (GATE) out *= silu(z0.x[k]);
-            if (at.mine) Elem<T>::store(y + t * a.sy.n, out);
-        }
+    Scalars<T, n> nB, nC;
+    auto request_scalars = [&](int t) {
+        nB.load(a.bm, bc + t * a.sbc.n);
+        nC.load(a.cm, bc + t * a.sbc.n);
+        __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
+    };
+    if (at.first < at.last) {
+        request(at.first);
+        request_scalars(at.first);
     }
+    auto token = [&](int t, float ut, float dtt, float zt) {
+        Scalars<T, n> B = nB, C = nC;
+        B.arrive();
+        C.arrive();
+        request_scalars(t + 1 < at.last ? t + 1 : t);
+        const float D = softplus(dtt + bias), x = D * ut;
+        float out = skip * ut;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
+            out = __builtin_fmaf(C[i], h[i], out);
+        }
+        if (GATE) out *= silu(zt);
+        if (at.mine) Elem<T>::store(y + t * a.sy.n, out);
+    };
+    int t = at.first;
+    for (; t + kScanAhead <= at.last; t += kScanAhead) {
+        const Ahead<T, kScanAhead> u0 = u, dt0 = dt, z0 = z;
+        request(t + kScanAhead);
+#pragma unroll
+        for (int k = 0; k < kScanAhead; ++k) token(t + k, u0[k], dt0[k], GATE ? z0[k] : 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kScanAhead; ++k)
+        if (t + k < at.last) token(t + k, u[k], dt[k], GATE ? z[k] : 0.f);
     if (a.s_out && at.mine && at.last == at.length) store_state<n>(a.s_out, (int64_t)at.b * a.channels + at.channel, h);
 }
 

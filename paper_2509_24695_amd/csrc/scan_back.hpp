@@ -4,8 +4,8 @@
 //   ddt = dD sigmoid(dt + bias),  dz = dy (sum_i C h_t + skip u) silu'(z),  dA = sum_t D p,  dskip = sum_t y' u
 //
 // Cut into segments like the forward pass, with gradients handed on from segment to segment the same way from the end.  The states are
-// needed from the last to the first: scan_back_sums leaves the local state before every run of eight tokens, a wave adds what the
-// segment's first state has become by then, walks the run forwards with its eight states in registers, and then backwards.  The sums over channels (dB, dC)
+// needed from the last to the first: scan_back_sums leaves the local state before every run of four tokens, a wave adds what the
+// segment's first state has become by then, walks the run forwards with its states in registers, and then backwards.  The sums over channels (dB, dC)
 // go through the wave by exchanges that halve the number of values a lane holds with every step: 2 n values cost little more than 2 n additions.
 #pragma once
 
@@ -23,7 +23,7 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
     for (int i = 0; i < n; ++i) g[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
     // tokens from the last: token k of the walk is last - 1 - k
-    Ahead<T, kScanAhead> dy{}, dt{}, z{};
+    Ahead<T, kScanAhead> dy, dt, z;
     const int count = at.last - at.first;
     auto request = [&](int k) {
         const int64_t top = at.last - 1;
@@ -32,19 +32,28 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
         if (GATE) z.request(a.z, at.z + top * a.sz.n, -a.sz.n, k, count);
     };
     request(0);
-    for (int k0 = 0; k0 < count; k0 += kScanAhead) {
+    Scalars<T, n> next;
+    next.load(a.cm, bc + (at.last - 1) * a.sbc.n);
+    auto token = [&](int k, float v, float dtt, float zt) {
+        Scalars<T, n> C = next;
+        C.arrive();
+        next.load(a.cm, bc + (at.last - 1 - (k + 1 < count ? k + 1 : k)) * a.sbc.n);
+        __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
+        const float D = softplus(dtt + bias);
+        if (GATE) v *= silu(zt);
+#pragma unroll
+        for (int i = 0; i < n; ++i) g[i] = __builtin_amdgcn_exp2f(D * A2[i]) * __builtin_fmaf(C[i], v, g[i]);
+    };
+    int k0 = 0;
+    for (; k0 + kScanAhead <= count; k0 += kScanAhead) {
         const Ahead<T, kScanAhead> dy0 = dy, dt0 = dt, z0 = z;
         request(k0 + kScanAhead);
 #pragma unroll
-        for (int k = 0; k < kScanAhead; ++k) {
-            if (k0 + k >= count) break;
-            Scalars<T, n> C;
-            C.load(a.cm, bc + (at.last - 1 - k0 - k) * a.sbc.n);
-            const float D = softplus(dt0.x[k] + bias), v = GATE ? dy0.x[k] * silu(z0.x[k]) : dy0.x[k];
-#pragma unroll
-            for (int i = 0; i < n; ++i) g[i] = __builtin_amdgcn_exp2f(D * A2[i]) * __builtin_fmaf(C[i], v, g[i]);
-        }
+        for (int k = 0; k < kScanAhead; ++k) token(k0 + k, dy0[k], dt0[k], GATE ? z0[k] : 0.f);
     }
+#pragma unroll
+    for (int k = 0; k < kScanAhead; ++k)
+        if (k0 + k < count) token(k0 + k, dy[k], dt[k], GATE ? z[k] : 0.f);
     if (!at.mine) return;
 #pragma unroll
     for (int i = 0; i < n; ++i) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = g[i];
@@ -52,9 +61,9 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
 
 template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_back_sums(ScanArgs a)
 {
-    const uint32_t half = (uint32_t)a.blocks * a.segments * a.B;
+    const uint32_t half = gridDim.x / 2;
     const bool back = blockIdx.x >= half;
-    const ScanPlace at(a, back ? blockIdx.x - half : blockIdx.x);
+    const ScanPlace at(a, scan_task(back ? blockIdx.x - half : blockIdx.x, half));
     if (at.first >= at.length) return;
     if (!back) scan_sum_forward<T, n, true>(a, at);
     else if (at.segment > 0) scan_sum_back<T, n, GATE>(a, at);
@@ -62,50 +71,53 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) 
 
 template <int n> __global__ __launch_bounds__(256) void scan_back_states(ScanArgs a)
 {
-    const int64_t count = (int64_t)a.B * a.channels * n, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id < count) scan_state<n, false>(a, id);
-    else if (id < 2 * count) scan_state<n, true>(a, id - count);
+    const int half = (int)gridDim.x / 2;
+    if ((int)blockIdx.x < half) scan_state<n, false>(a, (int)blockIdx.x);
+    else scan_state<n, true>(a, (int)blockIdx.x - half);
 }
 
-// Sums of V values over the wave: a lane ends with that of value wave_value<V>(lane), in v[0].
-template <int V> __device__ __forceinline__ void wave_sums(float (&v)[V])
+// Sums over the wave of 2 n values, n of either kind, by exchanges: two lanes keep one of two values each and get the other's share of it.
+// both(): the first exchange, between the halves of the wave, of value i of either kind.
+__device__ __forceinline__ float wave_both(float first, float second)
 {
-    static_assert(V == 16 || V == 32, "two or one lane a value and four steps");
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(first), __float_as_uint(second), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+// The rest: v[i] as wave_both left value i.  A lane ends with the sum of value wave_value<n>(lane), in v[0].
+template <int n> __device__ __forceinline__ void wave_sums(float (&v)[n])
+{
+    static_assert(n == 8 || n == 16, "two or four lanes a value at the end");
     const int lane = threadIdx.x % kScanWave;
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + V / 2]), false, false);
+    for (int i = 0; i < n / 2; ++i) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + n / 2]), false, false);
         v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
     }
-#pragma unroll
-    for (int i = 0; i < V / 4; ++i) {
-        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + V / 4]), false, false);
-        v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-    }
-    // a lane keeps one of two values and gets its partner's of the same
     auto step = [&](auto ctrl, int bit, float keep_low, float keep_high) {
         const bool high = lane & bit;
         const float own = high ? keep_high : keep_low, other = high ? keep_low : keep_high;
         return own + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, other), ctrl(), 0xf, 0xf, true));
     };
 #pragma unroll
-    for (int i = 0; i < V / 8; ++i) v[i] = step(std::integral_constant<int, 0x128>{}, 8, v[i], v[i + V / 8]);      // row_ror 8
+    for (int i = 0; i < n / 4; ++i) v[i] = step(std::integral_constant<int, 0x128>{}, 8, v[i], v[i + n / 4]);      // row_ror 8
 #pragma unroll
-    for (int i = 0; i < V / 16; ++i) v[i] = step(std::integral_constant<int, 0x141>{}, 4, v[i], v[i + V / 16]);    // row_half_mirror
-    if constexpr (V == 32) v[0] = step(std::integral_constant<int, 0x4e>{}, 2, v[0], v[1]);                        // quad_perm 2,3,0,1
+    for (int i = 0; i < n / 8; ++i) v[i] = step(std::integral_constant<int, 0x141>{}, 4, v[i], v[i + n / 8]);      // row_half_mirror
+    if constexpr (n == 16) v[0] = step(std::integral_constant<int, 0x4e>{}, 2, v[0], v[1]);                        // quad_perm 2,3,0,1
     else v[0] = dpp_add<0x4e>(v[0]);
     v[0] = dpp_add<0xb1>(v[0]);
 }
-template <int V> __device__ __forceinline__ int wave_value(int lane)
+// (the kind is the wave's half: values of the second kind follow those of the first)
+template <int n> __device__ __forceinline__ int wave_value(int lane)
 {
-    int i = (lane >> 5 & 1) * (V / 2) + (lane >> 4 & 1) * (V / 4) + (lane >> 3 & 1) * (V / 8) + (lane >> 2 & 1) * (V / 16);
-    if (V == 32) i += lane >> 1 & 1;
+    int i = (lane >> 5 & 1) * n + (lane >> 4 & 1) * (n / 2) + (lane >> 3 & 1) * (n / 4) + (lane >> 2 & 1) * (n / 8);
+    if (n == 16) i += lane >> 1 & 1;
     return i;
 }
 
-template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_back_walk(ScanArgs a)
+template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 2) void scan_back_walk(ScanArgs a)
 {
-    const ScanPlace at(a, blockIdx.x);
+    const ScanPlace at(a, scan_task(blockIdx.x, gridDim.x));
+    if (at.b >= a.B) return;
     const int lane = threadIdx.x;
     float *params = a.params + at.slot(a) * (n + 2) * a.channels + at.channel;
     if (at.first >= at.length && at.segment > 0) {
@@ -131,86 +143,102 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) 
 #pragma unroll
     for (int i = 0; i < n; ++i) dA[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
-    float *shared = a.shared + ((int64_t)at.b * a.blocks + at.block) * a.N * 2 * n + wave_value<2 * n>(lane);
+    float *shared = a.shared + ((int64_t)at.b * a.blocks + at.block) * a.N * 2 * n + wave_value<n>(lane);
     const bool sums_mine = lane % (64 / (2 * n)) == 0;
     const int runs = (at.last - at.first + kScanRun - 1) / kScanRun;
-    Ahead<T, kScanRun> u{}, dt{}, z{}, dy{};
+    Ahead<T, kScanRun> u, dt, z, dy;
     auto request = [&](int t) {
         u.request(a.u, at.u, a.su.n, t, at.last);
         dt.request(a.dt, at.u, a.su.n, t, at.last);
         dy.request(a.dy, at.y, a.sy.n, t, at.last);
         if (GATE) z.request(a.z, at.z, a.sz.n, t, at.last);
     };
-    if (runs) request(at.first + (runs - 1) * kScanRun);
-    for (int r = runs - 1; r >= 0; --r) {
-        const int t0 = at.first + r * kScanRun, count = at.last - t0 < kScanRun ? at.last - t0 : kScanRun;
+    // B and C of the token that comes after the present one: a run's tokens forwards, then backwards, then those of the run before
+    Scalars<T, n> nB, nC;
+    auto request_scalars = [&](int t) {
+        nB.load(a.bm, bc + t * a.sbc.n);
+        nC.load(a.cm, bc + t * a.sbc.n);
+        __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
+    };
+    auto run = [&](int t0, int count, auto whole) {
         const Ahead<T, kScanRun> u0 = u, dt0 = dt, z0 = z, dy0 = dy;
-        if (r > 0) request(t0 - kScanRun);
-        float h[kScanRun + 1][n], D[kScanRun], raw[kScanRun];
-        if (r > 0) {
+        const bool more = t0 > at.first;
+        float h[kScanRun + 1][n], D[kScanRun], slope[kScanRun], raw[kScanRun];
+        if (more) {
             const int64_t mark = (int64_t)at.b * a.runs + t0 / kScanRun;
             const float steps = a.mark_steps[mark * a.channels + at.channel];
 #pragma unroll
-            for (int i = 0; i < n; ++i)
-                h[0][i] = __builtin_fmaf(kept(A2[i], steps), begin[i], a.marks[(mark * n + i) * a.channels + at.channel]);
+            for (int i = 0; i < n; ++i) h[0][i] = a.marks[(mark * n + i) * a.channels + at.channel];
+#pragma unroll
+            for (int i = 0; i < n; ++i) h[0][i] = __builtin_fmaf(kept(A2[i], steps), begin[i], h[0][i]);
         } else {
 #pragma unroll
             for (int i = 0; i < n; ++i) h[0][i] = begin[i];
         }
 #pragma unroll
         for (int k = 0; k < kScanRun; ++k) {
-            if (k < count) {
-                Scalars<T, n> B, C;
-                B.load(a.bm, bc + (t0 + k) * a.sbc.n);
-                if (GATE) C.load(a.cm, bc + (t0 + k) * a.sbc.n);
-                D[k] = softplus(dt0.x[k] + bias);
-                const float x = D[k] * u0.x[k];
-                raw[k] = skip * u0.x[k];
+            if (!whole() && k >= count) break;
+            Scalars<T, n> B = nB, C = nC;
+            B.arrive();
+            C.arrive();
+            request_scalars(t0 + (k + 1 < count ? k + 1 : k));
+            D[k] = softplus(dt0[k] + bias, slope[k]);
+            const float x = D[k] * u0[k];
+            raw[k] = skip * u0[k];
 #pragma unroll
-                for (int i = 0; i < n; ++i) {
-                    h[k + 1][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D[k] * A2[i]), h[k][i], x * B[i]);
-                    if (GATE) raw[k] = __builtin_fmaf(C[i], h[k + 1][i], raw[k]);
-                }
+            for (int i = 0; i < n; ++i) {
+                h[k + 1][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D[k] * A2[i]), h[k][i], x * B[i]);
+                if (GATE) raw[k] = __builtin_fmaf(C[i], h[k + 1][i], raw[k]);
             }
         }
 #pragma unroll
         for (int k = kScanRun - 1; k >= 0; --k) {
-            if (k >= count) continue;
+            if (k == kScanRun - 2 && more) request(t0 - kScanRun);    // (the last token's state is no longer needed: its registers do)
+            if (!whole() && k >= count) continue;
             const int t = t0 + k;
-            Scalars<T, n> B, C;
-            B.load(a.bm, bc + t * a.sbc.n);
-            C.load(a.cm, bc + t * a.sbc.n);
-            float v = dy0.x[k];
+            Scalars<T, n> B = nB, C = nC;
+            B.arrive();
+            C.arrive();
+            request_scalars(k > 0 ? t - 1 : more ? t - kScanRun : t);
+            float v = dy0[k];
             if (GATE) {
-                const float s = sigmoid(z0.x[k]);
-                if (at.mine) Elem<T>::store(static_cast<T *>(a.dz) + at.z + t * a.sz.n, v * raw[k] * silu_slope(z0.x[k], s));
-                v *= z0.x[k] * s;
+                const float s = sigmoid(z0[k]);
+                if (at.mine) Elem<T>::store(static_cast<T *>(a.dz) + at.z + t * a.sz.n, v * raw[k] * silu_slope(z0[k], s));
+                v *= z0[k] * s;
             }
-            const float x = D[k] * u0.x[k];
-            float sums[2 * n], e = 0.f, along = 0.f;
+            // the decays are worked out again: kept from the way forwards they would take registers from a second wave
+            asm volatile("" : "+v"(D[k]));
+            // lanes that double a channel add nothing to the sums over channels
+            v = at.mine ? v : 0.f;
+            const float x = at.mine ? D[k] * u0[k] : 0.f;
+            float sums[n], e = 0.f, along = 0.f;
 #pragma unroll
             for (int i = 0; i < n; ++i) {
                 g[i] = __builtin_fmaf(C[i], v, g[i]);
-                sums[i] = at.mine ? g[i] * x : 0.f;
-                sums[n + i] = at.mine ? v * h[k + 1][i] : 0.f;
+                sums[i] = wave_both(g[i] * x, v * h[k + 1][i]);
                 e = __builtin_fmaf(g[i], B[i], e);
                 g[i] *= __builtin_amdgcn_exp2f(D[k] * A2[i]);
                 const float p = g[i] * h[k][i];
                 dA[i] = __builtin_fmaf(D[k], p, dA[i]);
                 along = __builtin_fmaf(A2[i], p, along);
             }
-            float slope;
-            softplus(dt0.x[k] + bias, slope);
-            const float ddt = __builtin_fmaf(along, 1.f / kLog2E, u0.x[k] * e) * slope;
+            const float ddt = __builtin_fmaf(along, 1.f / kLog2E, u0[k] * e) * slope[k];
             dbias += ddt;
-            dskip = __builtin_fmaf(v, u0.x[k], dskip);
+            dskip = __builtin_fmaf(v, u0[k], dskip);
             if (at.mine) {
                 Elem<T>::store(static_cast<T *>(a.du) + at.u + t * a.su.n, __builtin_fmaf(D[k], e, skip * v));
                 Elem<T>::store(static_cast<T *>(a.ddt) + at.u + t * a.su.n, ddt);
             }
-            wave_sums<2 * n>(sums);
+            wave_sums<n>(sums);
             if (sums_mine) shared[(int64_t)t * 2 * n] = sums[0];
         }
+    };
+    if (runs) {
+        int t0 = at.first + (runs - 1) * kScanRun;
+        request(t0);
+        request_scalars(t0);
+        run(t0, at.last - t0, std::false_type{});
+        for (t0 -= kScanRun; t0 >= at.first; t0 -= kScanRun) run(t0, kScanRun, std::true_type{});
     }
     if (!at.mine) return;
 #pragma unroll

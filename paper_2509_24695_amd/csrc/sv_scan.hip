@@ -32,7 +32,7 @@ sv_status check_tensors(const sv_tensor_desc *u, const void *Z, const sv_tensor_
     rc = check_rows(bc, sbc);
     if (rc != SV_OK) return rc;
     if (sbc->B != su->B || sbc->N != su->N || sbc->bf16 != su->bf16 || su->H % sbc->H) return SV_ERR_SHAPE;
-    if ((int64_t)su->H * su->d >= (int64_t)1 << 28) return SV_ERR_SHAPE;
+    if ((int64_t)su->H * su->d >= (int64_t)1 << 27) return SV_ERR_SHAPE;
     return SV_OK;
 }
 
@@ -105,8 +105,8 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
     ScanArgs a = scan_args(su, sz, sbc, sy, plan);
     const int64_t states = (int64_t)a.B * a.segments * a.channels * n, waves = (int64_t)a.B * a.segments * a.blocks;
     if (a.segments > 1 && workspace_bytes < (size_t)(states + states / n) * sizeof(float)) return SV_ERR_WORKSPACE;
-    const int64_t scan = ((int64_t)a.B * a.channels * n + 255) / 256;
-    if (!grid_ok(waves, kScanWave) || !grid_ok(scan, 256)) return SV_ERR_SHAPE;
+    const int64_t scan = (int64_t)a.B * (((int64_t)a.channels * n + 255) / 256);
+    if (!grid_ok(scan_grid(waves), kScanWave) || !grid_ok(scan, 256)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.y = Y;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.s_out = S_out;
@@ -116,12 +116,12 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
     sv_status done = SV_OK;
     with_scan(su.bf16, n, Z != nullptr, [&](auto t, auto k, auto gate) {
         if (a.segments > 1) {
-            scan_sums<decltype(t), k()><<<(unsigned)(waves / a.segments * (a.segments - 1)), kScanWave, 0, hs>>>(a);
+            scan_sums<decltype(t), k()><<<(unsigned)scan_grid(waves / a.segments * (a.segments - 1)), kScanWave, 0, hs>>>(a);
             if ((done = launched()) != SV_OK) return;
             scan_states<k()><<<(unsigned)scan, 256, 0, hs>>>(a);
             if ((done = launched()) != SV_OK) return;
         }
-        scan_walk<decltype(t), k(), gate()><<<(unsigned)waves, kScanWave, 0, hs>>>(a);
+        scan_walk<decltype(t), k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);
         done = launched();
     });
     return done;
@@ -179,9 +179,9 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     ScanArgs a = scan_args(su, sz, sbc, sy, plan);
     const ScanBackwardSpace space = scan_backward_space(a.B, a.G, a.channels, a.N, n, (int64_t)a.B * a.segments);
     if (workspace_bytes < (size_t)space.total * sizeof(float)) return SV_ERR_WORKSPACE;
-    const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = (2 * (int64_t)a.B * a.channels * n + 255) / 256;
+    const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = 2 * (int64_t)a.B * (((int64_t)a.channels * n + 255) / 256);
     const int64_t shared = ((int64_t)a.B * a.G * a.N * 2 * n + 255) / 256, params = ((int64_t)a.channels * (n + 2) + 255) / 256;
-    if (!grid_ok(2 * waves, kScanWave) || !grid_ok(states, 256) || !grid_ok(shared, 256) || !grid_ok(params, 256)) return SV_ERR_SHAPE;
+    if (!grid_ok(2 * scan_grid(waves), kScanWave) || !grid_ok(states, 256) || !grid_ok(shared, 256) || !grid_ok(params, 256)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.dy = dY;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.ds_out = dS_out;
@@ -199,13 +199,13 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     sv_status done = SV_OK;
     with_scan(su.bf16, n, Z != nullptr, [&](auto t, auto k, auto gate) {
         using T = decltype(t);
-        scan_back_sums<T, k(), gate()><<<(unsigned)(2 * waves), kScanWave, 0, hs>>>(a);
+        scan_back_sums<T, k(), gate()><<<(unsigned)(2 * scan_grid(waves)), kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
         if (a.segments > 1) {
             scan_back_states<k()><<<(unsigned)states, 256, 0, hs>>>(a);
             if ((done = launched()) != SV_OK) return;
         }
-        scan_back_walk<T, k(), gate()><<<(unsigned)waves, kScanWave, 0, hs>>>(a);
+        scan_back_walk<T, k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
         scan_back_shared<T, k()><<<(unsigned)shared, 256, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
