@@ -18,6 +18,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Element strides of a [B][H][N][d] token tensor (d contiguous).
@@ -84,11 +85,11 @@ template <bool NT = true> __device__ __forceinline__ u32x4 load_stream16(rsrc_t 
 template <bool NT = true> __device__ __forceinline__ void store_stream16(rsrc_t r, uint32_t off, u32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, NT ? 2 : 0);
 }
-// 16 bytes to global memory, past the caches or not.  The empty statements keep the two stores apart: the compiler makes one of them otherwise,
+// 16 bytes (or 8) to global memory, past the caches or not.  The empty statements keep the two stores apart: the compiler makes one of them otherwise,
 // without the hint.
 template <typename V> __device__ __forceinline__ void store16(void *p, V v, bool past_caches)
 {
-    static_assert(sizeof(V) == 16, "a piece");
+    static_assert(sizeof(V) == 16 || sizeof(V) == 8, "a piece or half of one");
     if (past_caches) {
         asm volatile("");
         __builtin_nontemporal_store(v, static_cast<V *>(p));

@@ -30,13 +30,16 @@ struct ConvArgs {
     NormDivisor pieces, head_pieces, run_div;
 };
 
+template <typename T> using ConvForward = Piece<T>;
+template <typename T> using ConvBackward = Quad<T>;
+
 // A thread's channels: head, feature, and place among all channels.
-template <typename T> struct ConvPlace {
+template <typename P> struct ConvPlace {
     int h, i, c;
     __device__ __forceinline__ ConvPlace(const ConvArgs &a, uint32_t piece)
     {
         h = (int)a.head_pieces.quotient(piece);
-        i = (int)(piece - (uint32_t)h * a.head_pieces.extent) * Piece<T>::kN;
+        i = (int)(piece - (uint32_t)h * a.head_pieces.extent) * P::kN;
         c = h * a.d + i;
     }
 };
@@ -52,8 +55,8 @@ template <int N> __device__ __forceinline__ void load_floats(const float *p, flo
 }
 
 // Taps and bias of a piece.
-template <typename T, int K> struct ConvWeights {
-    static constexpr int kN = Piece<T>::kN;
+template <typename P, int K> struct ConvWeights {
+    static constexpr int kN = P::kN;
     float w[K][kN], b[kN];
     __device__ __forceinline__ ConvWeights(const ConvArgs &a, int c)
     {
@@ -76,13 +79,37 @@ template <typename T, int K> struct ConvWeights {
 };
 
 // Row m of the cache and the tokens one after the other (m = 0: the cache's first); nothing where there is neither.
-template <typename T, int K>
-__device__ __forceinline__ u32x4 conv_row(const ConvArgs &a, const T *x, const void *cache, int64_t cache_at, int64_t m, int length)
+template <typename T, typename P, int K>
+__device__ __forceinline__ typename P::V conv_row(const ConvArgs &a, const T *x, const void *cache, int64_t cache_at, int64_t m, int length)
 {
-    if (m < K - 1) return cache ? *reinterpret_cast<const u32x4 *>(static_cast<const T *>(cache) + cache_at + m * a.d) : u32x4{0u, 0u, 0u, 0u};
+    typedef typename P::V V;
+    if (m < K - 1) return cache ? *reinterpret_cast<const V *>(static_cast<const T *>(cache) + cache_at + m * a.d) : V{};
     const int64_t t = m - (K - 1);
-    return t < length ? *reinterpret_cast<const u32x4 *>(x + t * a.sx.n) : u32x4{0u, 0u, 0u, 0u};
+    return t < length ? *reinterpret_cast<const V *>(x + t * a.sx.n) : V{};
 }
+
+// The rows of a run that come next, AHEAD at a time.  Past the last the last one is read again: no branch stands between the loads.
+template <typename T, typename P, int AHEAD> struct ConvRows {
+    typedef typename P::V V;
+    const T *at, *end;
+    int64_t stride;
+    int left;
+    V next[AHEAD];
+    __device__ __forceinline__ ConvRows(const T *x, int64_t stride, int first, int last)
+        : at(x + first * stride), end(x + (last - 1) * stride), stride(stride), left(last - first) {}
+    __device__ __forceinline__ void request()
+    {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) next[i] = *reinterpret_cast<const V *>(i < left ? at + i * stride : end);
+        at += AHEAD * stride;
+        left -= AHEAD;
+    }
+    __device__ __forceinline__ void take(V (&v)[AHEAD]) const
+    {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) v[i] = next[i];
+    }
+};
 
 template <int K, int N> __device__ __forceinline__ void conv_shift(float (&w)[K][N], const float (&now)[N])
 {
@@ -96,100 +123,105 @@ template <int K, int N> __device__ __forceinline__ void conv_shift(float (&w)[K]
 
 template <typename T, int K, bool SILU> __global__ __launch_bounds__(kConvThreads) void conv_rows(ConvArgs a)
 {
-    constexpr int kN = Piece<T>::kN, kAhead = 4;
+    using P = ConvForward<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN, kAhead = 4;
     const uint32_t id = blockIdx.x * kConvThreads + threadIdx.x, all = a.pieces.quotient(id), piece = id - all * a.pieces.extent;
     const uint32_t b = a.run_div.quotient(all), run = all - b * a.run_div.extent;
     if ((int)b >= a.B) return;
     const int length = held_length(a.lengths, (int)b, a.N);
-    const int64_t first = (int64_t)run * a.run, last = first + a.run < length ? first + a.run : length;
+    const int first = (int)run * a.run, last = first + a.run < length ? first + a.run : length;
     if (first >= length && run > 0) return;
-    const ConvPlace<T> at(a, piece);
+    const ConvPlace<P> at(a, piece);
     const T *x = static_cast<const T *>(a.x) + b * a.sx.b + at.h * a.sx.h + at.i;
     T *y = static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i;
     const int64_t cache_at = ((int64_t)b * a.H + at.h) * (K - 1) * a.d + at.i;
-    u32x4 next[kAhead] = {};
-    auto request = [&](int64_t t) {
+    if (first < last) {
+        ConvRows<T, P, kAhead> rows(x, a.sx.n, first, last);
+        rows.request();
+        float before[K - 1][kN];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (t + i < last) next[i] = *reinterpret_cast<const u32x4 *>(x + (t + i) * a.sx.n);
-    };
-    request(first);
-    float before[K - 1][kN];
+        for (int j = 0; j < K - 1; ++j) P::open(conv_row<T, P, K>(a, x, a.cache_in, cache_at, first + j, length), before[j]);
+        const ConvWeights<P, K> w(a, at.c);
+        T *to = y + first * a.sy.n;
+        for (int t = first; t < last; t += kAhead) {
+            V v[kAhead];
+            rows.take(v);
+            rows.request();
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) Piece<T>::open(conv_row<T, K>(a, x, a.cache_in, cache_at, first + j, length), before[j]);
-    const ConvWeights<T, K> w(a, at.c);
-    for (int64_t t = first; t < last; t += kAhead) {
-        u32x4 v[kAhead];
+            for (int i = 0; i < kAhead; ++i) {
+                float now[kN], out[kN];
+                P::open(v[i], now);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) v[i] = next[i];
-        request(t + kAhead);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            float now[kN], out[kN];
-            Piece<T>::open(v[i], now);
-#pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                out[e] = w.mix(before, now, e);
-                if (SILU) out[e] = silu(out[e]);
+                for (int e = 0; e < kN; ++e) {
+                    out[e] = w.mix(before, now, e);
+                    if (SILU) out[e] = silu(out[e]);
+                }
+                if (t + i < last) store16(to + i * a.sy.n, P::close(out), a.whole_lines);
+                conv_shift(before, now);
             }
-            if (t + i < last) store16(y + (t + i) * a.sy.n, Piece<T>::close(out), a.whole_lines);
-            conv_shift(before, now);
+            to += kAhead * a.sy.n;
         }
     }
     // the run that read the old cache writes the new one, which may be the same memory
     if (run == 0 && a.cache_out) {
-        u32x4 rows[K - 1];
+        V rows[K - 1];
 #pragma unroll
-        for (int r = 0; r < K - 1; ++r) rows[r] = conv_row<T, K>(a, x, a.cache_in, cache_at, (int64_t)length + r, length);
+        for (int r = 0; r < K - 1; ++r) rows[r] = conv_row<T, P, K>(a, x, a.cache_in, cache_at, (int64_t)length + r, length);
 #pragma unroll
-        for (int r = 0; r < K - 1; ++r) *reinterpret_cast<u32x4 *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r];
+        for (int r = 0; r < K - 1; ++r) *reinterpret_cast<V *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r];
     }
 }
 
 // One token of each row of a batch: a workgroup has `across` pieces of one row.
 template <typename T, int K, bool SILU> __global__ __launch_bounds__(kConvThreads) void conv_token(ConvArgs a)
 {
-    constexpr int kN = Piece<T>::kN;
+    using P = ConvForward<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN;
     const int b = (int)(blockIdx.x / a.runs);
     const uint32_t piece = blockIdx.x % a.runs * a.across + threadIdx.x;
     const int slot = a.lengths ? a.lengths[b] : b;
     if (slot < 0 || slot >= a.n_slots) return;
     const bool mine = threadIdx.x < (unsigned)a.across && piece < a.pieces.extent;
-    const ConvPlace<T> at(a, mine ? piece : 0);
+    const ConvPlace<P> at(a, mine ? piece : 0);
     const int64_t cache_at = ((int64_t)slot * a.H + at.h) * (K - 1) * a.d + at.i;
     const T *x = static_cast<const T *>(a.x) + b * a.sx.b + at.h * a.sx.h + at.i;
-    u32x4 rows[K];
+    V rows[K];
 #pragma unroll
-    for (int j = 0; j < K; ++j) rows[j] = conv_row<T, K>(a, x, a.cache_in, cache_at, j, 1);
-    const ConvWeights<T, K> w(a, at.c);
+    for (int j = 0; j < K; ++j) rows[j] = conv_row<T, P, K>(a, x, a.cache_in, cache_at, j, 1);
+    const ConvWeights<P, K> w(a, at.c);
     if (slot_taken(a.lengths, b, slot) || !mine) return;
     float before[K - 1][kN], now[kN], out[kN];
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) Piece<T>::open(rows[j], before[j]);
-    Piece<T>::open(rows[K - 1], now);
+    for (int j = 0; j < K - 1; ++j) P::open(rows[j], before[j]);
+    P::open(rows[K - 1], now);
 #pragma unroll
     for (int e = 0; e < kN; ++e) {
         out[e] = w.mix(before, now, e);
         if (SILU) out[e] = silu(out[e]);
     }
-    *reinterpret_cast<u32x4 *>(static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i) = Piece<T>::close(out);
+    *reinterpret_cast<V *>(static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i) = P::close(out);
 #pragma unroll
-    for (int r = 0; r < K - 1; ++r) *reinterpret_cast<u32x4 *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r + 1];
+    for (int r = 0; r < K - 1; ++r) *reinterpret_cast<V *>(static_cast<T *>(a.cache_out) + cache_at + (int64_t)r * a.d) = rows[r + 1];
 }
 
 // dx of a run of tokens (of the cache too, for a sequence's first run), and the workgroup's part of dW and db.  With da_t known for the last
 // K tokens, row m of cache and tokens together gets sum_j W[j] da_{m-j}; so a run goes on for K - 1 tokens of the next.
 template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds__(kConvThreads) void conv_rows_backward(ConvArgs a)
 {
-    constexpr int kN = Piece<T>::kN, kAhead = 4;
+    using P = ConvBackward<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN, kAhead = 4;
     const uint32_t tiles = (a.pieces.extent + a.across - 1) / a.across, tile = blockIdx.x % tiles, rest = blockIdx.x / tiles;
     const int block = (int)(rest % a.runs), b = (int)(rest / a.runs), down = kConvThreads / a.across;
     const int col = (int)threadIdx.x % a.across, line = (int)threadIdx.x / a.across;
     const uint32_t piece = tile * a.across + col;
     const bool mine = piece < a.pieces.extent;
     const int length = held_length(a.lengths, b, a.N);
-    const int64_t run = (int64_t)block * down + line, first = run * a.run, last = first + a.run < length ? first + a.run : length;
-    const ConvPlace<T> at(a, mine ? piece : 0);
+    const int64_t begin = ((int64_t)block * down + line) * a.run;      // past the last token of a short sequence: nothing
+    const int first = begin < length ? (int)begin : length, last = first + a.run < length ? first + a.run : length;
+    const ConvPlace<P> at(a, mine ? piece : 0);
     float dw[K][kN], db[kN];
 #pragma unroll
     for (int e = 0; e < kN; ++e) {
@@ -197,55 +229,51 @@ template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds_
 #pragma unroll
         for (int j = 0; j < K; ++j) dw[j][e] = 0.f;
     }
-    if (mine && (first < length || run == 0)) {
+    const int64_t cache_at = ((int64_t)b * a.H + at.h) * (K - 1) * a.d + at.i;
+    const T *dcache_out = a.dcache_out ? static_cast<const T *>(a.dcache_out) + cache_at : nullptr;
+    T *dcache_in = a.cache_out ? static_cast<T *>(a.cache_out) + cache_at : nullptr;
+    if (mine && first < last) {
         const T *x = static_cast<const T *>(a.x) + b * a.sx.b + at.h * a.sx.h + at.i;
         const T *dy = static_cast<const T *>(a.dy) + b * a.sdy.b + at.h * a.sdy.h + at.i;
         T *dx = static_cast<T *>(a.y) + b * a.sy.b + at.h * a.sy.h + at.i;
-        const int64_t cache_at = ((int64_t)b * a.H + at.h) * (K - 1) * a.d + at.i;
-        const T *dcache_out = a.dcache_out ? static_cast<const T *>(a.dcache_out) + cache_at : nullptr;
-        T *dcache_in = a.cache_out ? static_cast<T *>(a.cache_out) + cache_at : nullptr;
-        const int64_t end = last + K - 1, live = end < length ? end : length;      // rows [first, end) of da, tokens up to `live`
-        u32x4 nx[kAhead], ndy[kAhead];
-        auto request = [&](int64_t t) {
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                nx[i] = ndy[i] = u32x4{0u, 0u, 0u, 0u};
-                if (t + i < live) {
-                    nx[i] = *reinterpret_cast<const u32x4 *>(x + (t + i) * a.sx.n);
-                    ndy[i] = *reinterpret_cast<const u32x4 *>(dy + (t + i) * a.sdy.n);
-                }
-            }
-        };
-        request(first);
+        const int end = last + K - 1, live = end < length ? end : length;      // rows [first, end) of da, tokens up to `live`
+        ConvRows<T, P, kAhead> xs(x, a.sx.n, first, live), dys(dy, a.sdy.n, first, live);
+        xs.request();
+        dys.request();
         float before[K - 1][kN], da[K][kN];
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j) Piece<T>::open(conv_row<T, K>(a, x, a.cache_in, cache_at, first + j, length), before[j]);
+        for (int j = 0; j < K - 1; ++j) P::open(conv_row<T, P, K>(a, x, a.cache_in, cache_at, first + j, length), before[j]);
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
             for (int e = 0; e < kN; ++e) da[j][e] = 0.f;
-        const ConvWeights<T, K> w(a, at.c);
-        for (int64_t t = first; t < end; t += kAhead) {
-            u32x4 vx[kAhead], vdy[kAhead];
+        const ConvWeights<P, K> w(a, at.c);
+        T *to = dx + (int64_t)(first - (K - 1)) * a.sy.n;              // of the row that da_t is the last to reach
+        // rows t .. t + kAhead - 1; `inside`: all of them are tokens of this run
+        auto group = [&](int t, auto inside) {
+            V vx[kAhead], vdy[kAhead];
+            xs.take(vx);
+            dys.take(vdy);
+            xs.request();
+            dys.request();
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                vx[i] = nx[i];
-                vdy[i] = ndy[i];
-            }
-            request(t + kAhead);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int64_t m = t + i;                              // da_m is the newest that row m gets
+                const int m = t + i;                                  // da_m is the newest that row m gets
                 float now[kN], g[kN], out[kN];
-                Piece<T>::open(vx[i], now);
-                Piece<T>::open(vdy[i], g);
+                P::open(vx[i], now);
+                P::open(vdy[i], g);
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
                     if (SILU) {
                         const float y = w.mix(before, now, e);
-                        g[e] = m < live ? g[e] * silu_slope(y, sigmoid(y)) : 0.f;
+                        g[e] *= silu_slope(y, sigmoid(y));
                     }
-                    if (PARAMS && m < last) {
+                    if (!inside()) g[e] = m < live ? g[e] : 0.f;
+                }
+                // (not with a factor of zero for the next run's tokens: they may be no numbers)
+                if (PARAMS && (inside() || m < last)) {
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) {
 #pragma unroll
                         for (int j = 0; j < K - 1; ++j) dw[j][e] = __builtin_fmaf(g[e], before[j][e], dw[j][e]);
                         dw[K - 1][e] = __builtin_fmaf(g[e], now[e], dw[K - 1][e]);
@@ -254,24 +282,33 @@ template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds_
                 }
                 conv_shift(da, g);
                 conv_shift(before, now);
-                const bool cached = m < K - 1, write = m < end && (cached ? run == 0 : m - (K - 1) >= first);
-                if (!write || (cached && !dcache_in)) continue;
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
                     out[e] = w.w[0][e] * da[K - 1][e];
 #pragma unroll
                     for (int j = 1; j < K; ++j) out[e] = __builtin_fmaf(w.w[j][e], da[K - 1 - j][e], out[e]);
                 }
-                if (dcache_out && m >= length) {
+                if (!inside() && dcache_out && m >= length && m < end) {
                     float more[kN];
-                    Piece<T>::open(*reinterpret_cast<const u32x4 *>(dcache_out + (m - length) * a.d), more);
+                    P::open(*reinterpret_cast<const V *>(dcache_out + (m - length) * a.d), more);
 #pragma unroll
                     for (int e = 0; e < kN; ++e) out[e] += more[e];
                 }
-                if (cached) *reinterpret_cast<u32x4 *>(dcache_in + m * a.d) = Piece<T>::close(out);
-                else store16(dx + (m - (K - 1)) * a.sy.n, Piece<T>::close(out), a.whole_lines);
+                if ((inside() || m < end) && (i >= K - 1 || m - first >= K - 1)) store16(to + i * a.sy.n, P::close(out), a.whole_lines);
+                else if (dcache_in && m < K - 1) *reinterpret_cast<V *>(dcache_in + m * a.d) = P::close(out);       // (m < end: K - 1 at least)
             }
-        }
+            to += kAhead * a.sy.n;
+        };
+        int t = first;
+        for (; t + kAhead <= last; t += kAhead) group(t, std::true_type{});
+        for (; t < end; t += kAhead) group(t, std::false_type{});
+    } else if (mine && length == 0 && begin == 0 && dcache_in) {
+        // no tokens: the cache was handed through
+        V rows[K - 1];
+#pragma unroll
+        for (int r = 0; r < K - 1; ++r) rows[r] = dcache_out ? *reinterpret_cast<const V *>(dcache_out + r * a.d) : V{};
+#pragma unroll
+        for (int r = 0; r < K - 1; ++r) *reinterpret_cast<V *>(dcache_in + r * a.d) = rows[r];
     }
     if constexpr (PARAMS) {
         // lanes with the same channels are added up in order of their runs
@@ -289,7 +326,7 @@ template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds_
                 float s = sums[q];
                 for (int r = 1; r < down; ++r) s += sums[r * width + q];
                 const uint32_t p = tile * a.across + q % a.across;
-                if (p < a.pieces.extent) partial[j * channels + ConvPlace<T>(a, p).c + q / a.across] = s;
+                if (p < a.pieces.extent) partial[j * channels + ConvPlace<P>(a, p).c + q / a.across] = s;
             }
         }
     }

@@ -20,14 +20,15 @@ sv_status check_two(const sv_tensor_desc *x, const sv_tensor_desc *y, Shape *a, 
     return same_shape(*a, *b) ? SV_OK : SV_ERR_SHAPE;
 }
 
-ConvArgs conv_args(const Shape &x, const float *weight, const float *bias, int silu)
+// `bytes`: of the channels that a thread has.
+ConvArgs conv_args(const Shape &x, const float *weight, const float *bias, int silu, int bytes)
 {
     ConvArgs a{};
     a.weight = weight; a.bias = bias;
     a.sx = x.st;
     a.B = x.B; a.H = x.H; a.N = x.N; a.d = x.d;
     a.silu = silu;
-    const int per_head = x.d * x.elem_bytes / 16;
+    const int per_head = x.d * x.elem_bytes / bytes;
     a.head_pieces = NormDivisor::of(per_head);
     a.pieces = NormDivisor::of(per_head * x.H);
     return a;
@@ -67,7 +68,7 @@ extern "C" sv_status sv_causal_conv(const void *X, const sv_tensor_desc *x, cons
     if (!all_aligned({X, weight, bias, cache_in, cache_out, Y}) || !aligned4(lengths)) return SV_ERR_ALIGN;
     if (Y == X || (cache_in != cache_out && overlaps(cache_in, cache_out, cache_bytes(in, in.B, taps))) || cache_out == X || cache_out == Y) return SV_ERR_SHAPE;
     if (!channels_ok(in)) return SV_ERR_SHAPE;
-    ConvArgs a = conv_args(in, weight, bias, silu);
+    ConvArgs a = conv_args(in, weight, bias, silu, 16);
     a.x = X; a.y = Y; a.sy = out.st;
     a.lengths = lengths; a.cache_in = cache_in; a.cache_out = cache_out;
     a.whole_lines = lines_whole(out);
@@ -96,7 +97,7 @@ extern "C" sv_status sv_causal_conv_token(const void *X, const sv_tensor_desc *x
     if (!all_aligned({X, weight, bias, cache_in, cache_out, Y}) || !aligned4(slots)) return SV_ERR_ALIGN;
     if (Y == X || (cache_in != cache_out && overlaps(cache_in, cache_out, cache_bytes(in, n_slots, taps))) || cache_out == X || cache_out == Y) return SV_ERR_SHAPE;
     if (!channels_ok(in)) return SV_ERR_SHAPE;
-    ConvArgs a = conv_args(in, weight, bias, silu);
+    ConvArgs a = conv_args(in, weight, bias, silu, 16);
     a.x = X; a.y = Y; a.sy = out.st;
     a.lengths = slots; a.n_slots = n_slots;
     a.cache_in = cache_in; a.cache_out = cache_out;
@@ -136,7 +137,7 @@ extern "C" sv_status sv_causal_conv_backward(const void *X, const sv_tensor_desc
         dcache_in == dX || (dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == bias))
         return SV_ERR_SHAPE;
     if (!channels_ok(in)) return SV_ERR_SHAPE;
-    ConvArgs a = conv_args(in, weight, bias, silu);
+    ConvArgs a = conv_args(in, weight, bias, silu, 4 * in.elem_bytes);
     const ConvCut cut = conv_cut(in.B, in.N, a.pieces.extent);
     const int64_t channels = (int64_t)in.H * in.d, floats = channels * (taps + 1);
     if (params && workspace_bytes < (size_t)conv_partial_floats(in.B, cut.blocks, channels, taps) * sizeof(float)) return SV_ERR_WORKSPACE;

@@ -169,6 +169,18 @@ def test_nonfinite_tokens_stay_where_the_formula_takes_them(value):
     assert (grads[0][1] != grads[1][1]).sum() == 4 and (grads[0][2] != grads[1][2]).sum() == 1
 
 
+def test_a_last_token_that_is_no_number_reaches_its_own_tap_only():
+    import torch
+    x, W, b, cache = _inputs((2, 1, 70, 16, 4, True, "f32", "bhnd", None, True))
+    x[0, 0, 69, 3], x[1, 0, 44, 3] = float("nan"), float("nan")
+    dy = draw(9, (2, 1, 70, 16), "f32")
+    dx, dW, db = like(x), torch.empty_like(W), torch.empty_like(b)
+    ws = space(sv.sv_causal_conv_backward_workspace_bytes(2, 1, 70, 16))
+    sv.sv_causal_conv_backward(x, sv.desc_of(x), dy, sv.desc_of(dy), W, b, 4, 0, ints([70, 45]), cache, None, dx, sv.desc_of(dx), None, dW, db, ws)
+    assert np.argwhere(np.isnan(f64(dW))).tolist() == [[3, 0, 3]] and not np.isnan(f64(db)).any()
+    assert not np.isnan(f64(dx)[0]).any() and not np.isnan(f64(dx)[1, :, :45]).any()
+
+
 def test_captured_and_replayed():
     import torch
     c = (3, 2, 90, 112, 4, True, "bf16", "bnhd", [90, 17, 0], True)
