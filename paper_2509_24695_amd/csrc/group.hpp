@@ -12,7 +12,9 @@
 #include "activation.hpp"
 #include "common.hpp"
 #include "group_plan.hpp"
+#include "norm_plan.hpp"
 #include "piece.hpp"
+#include "scan_plan.hpp"
 
 namespace sv {
 
@@ -27,15 +29,21 @@ struct GroupArgs {
     float *dw, *db;
     int H, N, d, G, width;                 // width: channels of a group
     int64_t BH;
-    int across, tiles, chunks;             // of this launch
+    int across, tiles, chunks, lines;      // of this launch
+    int64_t folds;                         // workgroups of group_back_fold for groups
     int64_t rows;
     int sum_chunks;                        // of the launch that wrote `sums`
     int whole_lines;
+    NormDivisor width_div;
     float eps;
 };
 
+template <typename T> using GroupSums = Piece<T>;
+template <typename T> using GroupApply = Piece<T>;
+template <typename T> using GroupBack = Quad<T>;
+
 // A workgroup's tile and chunk, and its threads' channels and first row.
-template <typename T> struct GroupPlace {
+template <typename T, typename P> struct GroupPlace {
     int bh, chunk, tile, col, line, down, c;
     int64_t first, last;
     bool mine;
@@ -49,7 +57,7 @@ template <typename T> struct GroupPlace {
         col = (int)threadIdx.x % a.across;
         line = (int)threadIdx.x / a.across;
         down = kGroupThreads / a.across;
-        c = (tile * a.across + col) * Piece<T>::kN;
+        c = (tile * a.across + col) * P::kN;
         mine = c < a.d;
         first = (int64_t)chunk * a.rows;
         last = first + a.rows < a.N ? first + a.rows : a.N;
@@ -73,37 +81,40 @@ template <int N> __device__ __forceinline__ void of_channel(const float *p, int 
 }
 
 // Walks a thread's rows, kGroupAhead at a time, the next ones on their way: f(row, pieces of x and (BOTH) dy).
-template <typename T, bool BOTH, typename F> __device__ __forceinline__ void group_walk(const GroupArgs &a, const GroupPlace<T> &at, F &&f)
+template <typename T, typename P, bool BOTH, typename F> __device__ __forceinline__ void group_walk(const GroupArgs &a, const GroupPlace<T, P> &at, F &&f)
 {
+    typedef typename P::V V;
     const T *x = at.at(a, a.x, a.sx), *dy = BOTH ? at.at(a, a.dy, a.sdy) : nullptr;
-    u32x4 nx[kGroupAhead] = {}, ndy[kGroupAhead] = {};
+    V nx[kGroupAhead], ndy[kGroupAhead];
+    // past the last row the last one is read again: no branch stands between the loads
     auto request = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < kGroupAhead; ++i) {
-            const int64_t r = row + i * at.down;
-            if (r < at.last) {
-                nx[i] = *reinterpret_cast<const u32x4 *>(x + r * a.sx.n);
-                if (BOTH) ndy[i] = *reinterpret_cast<const u32x4 *>(dy + r * a.sdy.n);
-            }
+            const int64_t r = row + i * at.down < at.last ? row + i * at.down : at.last - 1;
+            nx[i] = *reinterpret_cast<const V *>(x + r * a.sx.n);
+            if (BOTH) ndy[i] = *reinterpret_cast<const V *>(dy + r * a.sdy.n);
         }
     };
     request(at.first + at.line);
-    for (int64_t row = at.first + at.line; row < at.last; row += kGroupAhead * at.down) {
-        u32x4 vx[kGroupAhead], vdy[kGroupAhead];
+    int64_t row = at.first + at.line;
+    for (; row + (kGroupAhead - 1) * at.down < at.last; row += kGroupAhead * at.down) {
+        V vx[kGroupAhead], vdy[kGroupAhead];
 #pragma unroll
         for (int i = 0; i < kGroupAhead; ++i) {
             vx[i] = nx[i];
-            vdy[i] = ndy[i];
+            if (BOTH) vdy[i] = ndy[i];
         }
         request(row + kGroupAhead * at.down);
 #pragma unroll
-        for (int i = 0; i < kGroupAhead; ++i)
-            if (row + i * at.down < at.last) f(row + i * at.down, vx[i], vdy[i]);
+        for (int i = 0; i < kGroupAhead; ++i) f(row + i * at.down, vx[i], vdy[i]);
     }
+#pragma unroll
+    for (int i = 0; i < kGroupAhead; ++i)
+        if (row + i * at.down < at.last) f(row + i * at.down, nx[i], ndy[i]);
 }
 
 // Sums of a workgroup's lines, two numbers (of type S) a channel, into its place of `sums`.
-template <typename T, typename S, int N> __device__ __forceinline__ void group_store_sums(const GroupArgs &a, const GroupPlace<T> &at, const S (&p)[N], const S (&q)[N])
+template <typename T, typename P, typename S, int N> __device__ __forceinline__ void group_store_sums(const GroupArgs &a, const GroupPlace<T, P> &at, const S (&p)[N], const S (&q)[N])
 {
     __shared__ S lines[kGroupThreads * N];
     S *out = reinterpret_cast<S *>(a.sums) + ((int64_t)at.bh * a.chunks + at.chunk) * 2 * a.d;
@@ -125,15 +136,17 @@ template <typename T, typename S, int N> __device__ __forceinline__ void group_s
 
 template <typename T> __global__ __launch_bounds__(kGroupThreads) void group_sums(GroupArgs a)
 {
-    constexpr int kN = Piece<T>::kN;
-    const GroupPlace<T> at(a);
+    using P = GroupSums<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN;
+    const GroupPlace<T, P> at(a);
     double s[kN], q[kN];
 #pragma unroll
     for (int e = 0; e < kN; ++e) s[e] = q[e] = 0.;
     if (at.mine)
-        group_walk<T, false>(a, at, [&](int64_t, u32x4 vx, u32x4) {
+        group_walk<T, P, false>(a, at, [&](int64_t, V vx, V) {
             float x[kN];
-            Piece<T>::open(vx, x);
+            P::open(vx, x);
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
                 const double v = x[e];
@@ -141,38 +154,76 @@ template <typename T> __global__ __launch_bounds__(kGroupThreads) void group_sum
                 q[e] = __builtin_fma(v, v, q[e]);
             }
         });
-    group_store_sums<T, double, kN>(a, at, s, q);
+    group_store_sums<T, P, double, kN>(a, at, s, q);
 }
 
-// A wave's sums.
-__device__ __forceinline__ double wave_sum(double x)
+// A workgroup's sums of two numbers, for all of its threads (`lds`: two for each wave).
+template <int THREADS> __device__ __forceinline__ void group_total(double &s, double &q, double *lds)
 {
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m, 64);
-    return x;
+    for (int m = 1; m < 64; m *= 2) {
+        s += __shfl_xor(s, m, 64);
+        q += __shfl_xor(q, m, 64);
+    }
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) {
+        lds[threadIdx.x / 64 * 2] = s;
+        lds[threadIdx.x / 64 * 2 + 1] = q;
+    }
+    __syncthreads();
+    s = lds[0];
+    q = lds[1];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) {
+        s += lds[2 * w];
+        q += lds[2 * w + 1];
+    }
 }
 
-// mean and rstd of each group: a wave adds up the chunks and channels of one.
+// A group's two sums over its chunks and channels: f(channel, address of the first sum).
+template <typename S, typename F> __device__ __forceinline__ void group_gather(const GroupArgs &a, int64_t bh, int group, F &&f)
+{
+    const uint32_t count = (uint32_t)a.sum_chunks * a.width;
+    const S *p = reinterpret_cast<const S *>(a.sums) + bh * a.sum_chunks * 2 * a.d;
+    constexpr int kAt = 8;
+    for (uint32_t k0 = threadIdx.x; k0 < count; k0 += kAt * kGroupThreads) {
+        S s[kAt], q[kAt];
+        int c[kAt];
+#pragma unroll
+        for (int i = 0; i < kAt; ++i) {
+            const uint32_t k = k0 + i * kGroupThreads < count ? k0 + i * kGroupThreads : k0, chunk = a.width_div.quotient(k);
+            c[i] = group * a.width + (int)(k - chunk * a.width);
+            const S *at = p + (int64_t)chunk * 2 * a.d + c[i];
+            s[i] = at[0];
+            q[i] = at[a.d];
+        }
+#pragma unroll
+        for (int i = 0; i < kAt; ++i)
+            if (k0 + i * kGroupThreads < count) f(c[i], s[i], q[i]);
+    }
+}
+
+// mean and rstd from a group's sums of x and (x - from)^2
+__device__ __forceinline__ float group_scale(double squares, double over, float eps)
+{
+    const double var = squares * over;
+    return (float)(1. / __builtin_sqrt((var > 0. || var != var ? var : 0.) + eps));
+}
+
+// mean and rstd of each group: a workgroup adds up the chunks and channels of one.
 __global__ __launch_bounds__(kGroupThreads) void group_fold(GroupArgs a)
 {
-    const int64_t id = (int64_t)blockIdx.x * (kGroupThreads / 64) + threadIdx.x / 64;
-    if (id >= a.BH * a.G) return;
-    const int64_t bh = id / a.G;
-    const int group = (int)(id % a.G), lane = threadIdx.x % 64;
-    const double *p = a.sums + bh * a.sum_chunks * 2 * a.d + group * a.width;
+    __shared__ double lds[2 * kGroupThreads / 64];
+    const int64_t id = blockIdx.x, bh = id / a.G;
     double s = 0., q = 0.;
-    const int count = a.sum_chunks * a.width;
-#pragma unroll 4
-    for (int k = lane; k < count; k += 64) {
-        const double *at = p + (int64_t)(k / a.width) * 2 * a.d + k % a.width;
-        s += at[0];
-        q += at[a.d];
-    }
-    s = wave_sum(s);
-    q = wave_sum(q);
-    if (lane) return;
-    const double over = 1. / ((double)a.N * a.width), mean = s * over, var = __builtin_fma(-mean, mean, q * over);
-    const float m = (float)mean, r = (float)(1. / __builtin_sqrt((var > 0. || var != var ? var : 0.) + a.eps));
+    group_gather<double>(a, bh, (int)(id - bh * a.G), [&](int, double x, double xx) {
+        s += x;
+        q += xx;
+    });
+    group_total<kGroupThreads>(s, q, lds);
+    if (threadIdx.x) return;
+    const double over = 1. / ((double)a.N * a.width), mean = s * over;
+    const float m = (float)mean, r = group_scale(__builtin_fma(-mean, s, q), over, a.eps);
     a.level[id] = m;
     a.scale[id] = r;
     if (a.mean) {
@@ -183,8 +234,10 @@ __global__ __launch_bounds__(kGroupThreads) void group_fold(GroupArgs a)
 
 template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) void group_apply(GroupArgs a)
 {
-    constexpr int kN = Piece<T>::kN;
-    const GroupPlace<T> at(a);
+    using P = GroupApply<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN;
+    const GroupPlace<T, P> at(a);
     if (!at.mine) return;
     float mean[kN], rstd[kN], w[kN], b[kN];
     by_channel<kN>(a, a.level, at.bh, at.c, mean);
@@ -192,25 +245,25 @@ template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) voi
     of_channel<kN>(a.weight, at.c, 1.f, w);
     of_channel<kN>(a.bias, at.c, 0.f, b);
     T *y = const_cast<T *>(at.at(a, a.y, a.sy));
-    group_walk<T, false>(a, at, [&](int64_t row, u32x4 vx, u32x4) {
+    group_walk<T, P, false>(a, at, [&](int64_t row, V vx, V) {
         float x[kN];
-        Piece<T>::open(vx, x);
+        P::open(vx, x);
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
             x[e] = __builtin_fmaf((x[e] - mean[e]) * rstd[e], w[e], b[e]);
             if (SILU) x[e] = silu(x[e]);
         }
-        store16(y + row * a.sy.n, Piece<T>::close(x), a.whole_lines);
+        store16(y + row * a.sy.n, P::close(x), a.whole_lines);
     });
 }
 
 // xh and da of a thread's channels of one row.
-template <typename T, bool SILU, int N>
-__device__ __forceinline__ void group_terms(u32x4 vx, u32x4 vdy, const float (&mean)[N], const float (&rstd)[N], const float (&w)[N], const float (&b)[N], float (&xh)[N],
+template <typename P, bool SILU, int N>
+__device__ __forceinline__ void group_terms(typename P::V vx, typename P::V vdy, const float (&mean)[N], const float (&rstd)[N], const float (&w)[N], const float (&b)[N], float (&xh)[N],
                                             float (&da)[N])
 {
-    Piece<T>::open(vx, xh);
-    Piece<T>::open(vdy, da);
+    P::open(vx, xh);
+    P::open(vdy, da);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         xh[e] = (xh[e] - mean[e]) * rstd[e];
@@ -224,8 +277,10 @@ __device__ __forceinline__ void group_terms(u32x4 vx, u32x4 vdy, const float (&m
 // Sums of da and da xh by channel.
 template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) void group_back_sums(GroupArgs a)
 {
-    constexpr int kN = Piece<T>::kN;
-    const GroupPlace<T> at(a);
+    using P = GroupBack<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN;
+    const GroupPlace<T, P> at(a);
     float p[kN], q[kN];
 #pragma unroll
     for (int e = 0; e < kN; ++e) p[e] = q[e] = 0.f;
@@ -235,9 +290,9 @@ template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) voi
         by_channel<kN>(a, a.rstd, at.bh, at.c, rstd);
         of_channel<kN>(a.weight, at.c, 1.f, w);
         of_channel<kN>(a.bias, at.c, 0.f, b);
-        group_walk<T, true>(a, at, [&](int64_t, u32x4 vx, u32x4 vdy) {
+        group_walk<T, P, true>(a, at, [&](int64_t, V vx, V vdy) {
             float xh[kN], da[kN];
-            group_terms<T, SILU, kN>(vx, vdy, mean, rstd, w, b, xh, da);
+            group_terms<P, SILU, kN>(vx, vdy, mean, rstd, w, b, xh, da);
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
                 p[e] += da[e];
@@ -245,32 +300,26 @@ template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) voi
             }
         });
     }
-    group_store_sums<T, float, kN>(a, at, p, q);
+    group_store_sums<T, P, float, kN>(a, at, p, q);
 }
 
-// Of each group sum t / count and sum (t xh) / count (a wave each, in fp64); behind these db and dw of each channel.
+// Of each group sum t / count and sum (t xh) / count (a workgroup each, in fp64); behind these db and dw of each channel.
 __global__ __launch_bounds__(kGroupThreads) void group_back_fold(GroupArgs a)
 {
     const float *sums = reinterpret_cast<const float *>(a.sums);
-    const int64_t waves = a.BH * a.G, blocks = (waves + kGroupThreads / 64 - 1) / (kGroupThreads / 64);
+    const int64_t blocks = a.folds;
     if ((int64_t)blockIdx.x < blocks) {
-        const int64_t id = (int64_t)blockIdx.x * (kGroupThreads / 64) + threadIdx.x / 64;
-        if (id >= waves) return;
-        const int64_t bh = id / a.G;
-        const int group = (int)(id % a.G), lane = threadIdx.x % 64, count = a.sum_chunks * a.width;
+        __shared__ double lds[2 * kGroupThreads / 64];
+        const int64_t id = blockIdx.x, bh = id / a.G;
         double s = 0., q = 0.;
-#pragma unroll 4
-        for (int k = lane; k < count; k += 64) {
-            const int c = group * a.width + k % a.width;
-            const float *at = sums + (bh * a.sum_chunks + k / a.width) * 2 * a.d + c;
+        group_gather<float>(a, bh, (int)(id - bh * a.G), [&](int c, float p, float px) {
             const double w = a.weight ? a.weight[c] : 1.f;
-            s = __builtin_fma(w, (double)at[0], s);
-            q = __builtin_fma(w, (double)at[a.d], q);
-        }
-        s = wave_sum(s);
-        q = wave_sum(q);
+            s = __builtin_fma(w, (double)p, s);
+            q = __builtin_fma(w, (double)px, q);
+        });
+        group_total<kGroupThreads>(s, q, lds);
         const double over = 1. / ((double)a.N * a.width);
-        if (lane == 0) {
+        if (threadIdx.x == 0) {
             a.level[id] = (float)(s * over);
             a.scale[id] = (float)(q * over);
         }
@@ -295,8 +344,10 @@ __global__ __launch_bounds__(kGroupThreads) void group_back_fold(GroupArgs a)
 
 template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) void group_back_apply(GroupArgs a)
 {
-    constexpr int kN = Piece<T>::kN;
-    const GroupPlace<T> at(a);
+    using P = GroupBack<T>;
+    typedef typename P::V V;
+    constexpr int kN = P::kN;
+    const GroupPlace<T, P> at(a);
     if (!at.mine) return;
     float mean[kN], rstd[kN], w[kN], b[kN], level[kN], along[kN];
     by_channel<kN>(a, a.mean, at.bh, at.c, mean);
@@ -306,12 +357,12 @@ template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) voi
     of_channel<kN>(a.weight, at.c, 1.f, w);
     of_channel<kN>(a.bias, at.c, 0.f, b);
     T *dx = const_cast<T *>(at.at(a, a.y, a.sy));
-    group_walk<T, true>(a, at, [&](int64_t row, u32x4 vx, u32x4 vdy) {
+    group_walk<T, P, true>(a, at, [&](int64_t row, V vx, V vdy) {
         float xh[kN], da[kN];
-        group_terms<T, SILU, kN>(vx, vdy, mean, rstd, w, b, xh, da);
+        group_terms<P, SILU, kN>(vx, vdy, mean, rstd, w, b, xh, da);
 #pragma unroll
         for (int e = 0; e < kN; ++e) da[e] = rstd[e] * (w[e] * da[e] - level[e] - xh[e] * along[e]);
-        store16(dx + row * a.sy.n, Piece<T>::close(da), a.whole_lines);
+        store16(dx + row * a.sy.n, P::close(da), a.whole_lines);
     });
 }
 

@@ -37,4 +37,25 @@ inline int64_t group_slots(int64_t BH, int64_t N, int64_t d)
     return all < most ? all : most;
 }
 
+// A group whose rows fit the registers of one workgroup is read once, by one launch: units of 16, 4 or 2 bytes (the largest that a group's part of a
+// row is whole units of), a thread the same unit of every row that it has, `most` words of it at most.
+constexpr int kHeldThreads = 1024;
+struct HeldForm {
+    int unit, across, lines, rows;     // bytes; units of a row; rows side by side; rows of a thread; unit == 0: does not fit
+};
+inline HeldForm held_form(int64_t N, int64_t width_bytes, int most)
+{
+    HeldForm f{};
+    const int unit = width_bytes % 16 == 0 ? 16 : width_bytes % 4 == 0 ? 4 : 2, words = unit == 16 ? 4 : 1;
+    if (width_bytes / unit > kHeldThreads) return f;
+    f.across = (int)(width_bytes / unit);
+    f.lines = kHeldThreads / f.across;
+    const int64_t rows = (N + f.lines - 1) / f.lines;
+    if (rows * words > most) return f;
+    f.unit = unit;
+    f.rows = (int)rows;
+    return f;
+}
+constexpr int kHeldForwardWords = 32, kHeldBackwardWords = 16;      // (a thread of 1 024 has 128 registers)
+
 }  // namespace sv

@@ -5,6 +5,7 @@
 
 #include "desc_checks.hpp"
 #include "group.hpp"
+#include "group_held.hpp"
 
 namespace {
 
@@ -29,6 +30,7 @@ GroupArgs group_args(const Shape &x, int groups, void *workspace)
     GroupArgs a{};
     a.sx = x.st;
     a.H = x.H; a.N = x.N; a.d = x.d; a.G = groups; a.width = x.d / groups;
+    a.width_div = NormDivisor::of(a.width);
     a.BH = x.BH;
     a.level = static_cast<float *>(workspace);
     a.scale = a.level + a.BH * groups;
@@ -54,6 +56,33 @@ template <typename F> void with_group(bool bf16, int silu, F &&f)
     };
     if (bf16) act(uint16_t{});
     else act(float{});
+}
+
+// Calls f(element, unit, rows) with the constants of a form of at most `most` words a thread: the rows it has room for are a quarter of `most`, half
+// of it or all (in units of 16 bytes a quarter of that).
+template <int MOST, typename F> void with_held(bool bf16, const HeldForm &form, F &&f)
+{
+    auto sized = [&](auto t, auto unit) {
+        constexpr int kMost = unit() == 16 ? MOST / 4 : MOST;
+        if (form.unit != unit()) return;
+        if (form.rows <= kMost / 4) f(t, unit, std::integral_constant<int, kMost / 4>{});
+        else if (form.rows <= kMost / 2) f(t, unit, std::integral_constant<int, kMost / 2>{});
+        else f(t, unit, std::integral_constant<int, kMost>{});
+    };
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 16> sixteen;
+    if (bf16) sized(uint16_t{}, two), sized(uint16_t{}, four), sized(uint16_t{}, sixteen);
+    else sized(float{}, four), sized(float{}, sixteen);
+}
+// Gives a launch the form; its workgroups, 0: more than a launch has.
+unsigned held_args(GroupArgs &a, const HeldForm &form, int elem_bytes)
+{
+    a.across = form.across;
+    a.lines = form.lines;
+    a.whole_lines = a.whole_lines && a.width * elem_bytes % 128 == 0;
+    const int64_t grid = scan_grid(a.BH * a.G);
+    return grid_ok(grid, kHeldThreads) ? (unsigned)grid : 0;
 }
 
 size_t workspace_bytes_of(int32_t B, int32_t H, int32_t N, int32_t d, int32_t groups, size_t number)
@@ -96,12 +125,21 @@ extern "C" sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const 
     a.x = X; a.y = Y; a.sy = out.st;
     a.weight = weight; a.bias = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
     a.whole_lines = lines_whole(out);
+    const auto hs = static_cast<hipStream_t>(stream);
+    if (const HeldForm held = held_form(a.N, (int64_t)a.width * in.elem_bytes, kHeldForwardWords); held.unit) {
+        const unsigned grid = held_args(a, held, in.elem_bytes);
+        if (!grid) return SV_ERR_SHAPE;
+        with_held<kHeldForwardWords>(in.bf16, held, [&](auto t, auto unit, auto rows) {
+            if (silu) group_held<decltype(t), unit(), rows(), true><<<grid, kHeldThreads, 0, hs>>>(a);
+            else group_held<decltype(t), unit(), rows(), false><<<grid, kHeldThreads, 0, hs>>>(a);
+        });
+        return launched();
+    }
     GroupArgs b = a;
     const unsigned sum_grid = cut_args(a, sums), row_grid = cut_args(b, rows);
-    const int64_t fold = (a.BH * a.G + kGroupThreads / 64 - 1) / (kGroupThreads / 64);
+    const int64_t fold = a.BH * a.G;
     if (!sum_grid || !row_grid || !grid_ok(fold, kGroupThreads)) return SV_ERR_SHAPE;
     a.sum_chunks = b.sum_chunks = (int)sums.chunks;
-    const auto hs = static_cast<hipStream_t>(stream);
     if (in.bf16) group_sums<uint16_t><<<sum_grid, kGroupThreads, 0, hs>>>(a);
     else group_sums<float><<<sum_grid, kGroupThreads, 0, hs>>>(a);
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
@@ -128,7 +166,7 @@ extern "C" sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *
     if (silu < 0 || silu > 1) return SV_ERR_RANGE;
     if (dX == X || (dX == dY && !same_rows(grad, out)) || (dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == bias)) return SV_ERR_SHAPE;
     GroupArgs a = group_args(in, groups, workspace);
-    const int pieces = in.d * in.elem_bytes / 16;
+    const int pieces = in.d / 4;
     const GroupCut sums = group_cut(a.BH, a.N, pieces, kGroupSumWgs), rows = group_cut(a.BH, a.N, pieces, kGroupApplyWgs);
     if (workspace_bytes < (size_t)(reinterpret_cast<char *>(a.sums) - static_cast<char *>(workspace)) + (size_t)a.BH * sums.chunks * 2 * a.d * sizeof(float))
         return SV_ERR_WORKSPACE;
@@ -136,13 +174,33 @@ extern "C" sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *
     a.weight = weight; a.bias = bias; a.dw = dweight; a.db = dbias;
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.whole_lines = lines_whole(out);
+    const auto hs = static_cast<hipStream_t>(stream);
+    const bool params = dweight || dbias;
+    const int64_t param_folds = params ? (2 * a.d + 15) / 16 : 0;
+    if (const HeldForm held = held_form(a.N, (int64_t)a.width * in.elem_bytes, kHeldBackwardWords); held.unit) {
+        const unsigned grid = held_args(a, held, in.elem_bytes);
+        if (!grid) return SV_ERR_SHAPE;
+        with_held<kHeldBackwardWords>(in.bf16, held, [&](auto t, auto unit, auto rows) {
+            auto go = [&](auto act, auto p) { group_held_back<decltype(t), unit(), rows(), act(), p()><<<grid, kHeldThreads, 0, hs>>>(a); };
+            auto with = [&](auto act) {
+                if (params) go(act, std::true_type{});
+                else go(act, std::false_type{});
+            };
+            if (silu) with(std::true_type{});
+            else with(std::false_type{});
+        });
+        if (launched() != SV_OK) return SV_ERR_LAUNCH;
+        if (!params) return SV_OK;
+        a.sum_chunks = 1;
+        group_back_fold<<<(unsigned)param_folds, kGroupThreads, 0, hs>>>(a);
+        return launched();
+    }
+    a.folds = a.BH * a.G;
     GroupArgs b = a;
     const unsigned sum_grid = cut_args(a, sums), row_grid = cut_args(b, rows);
-    int64_t fold = (a.BH * a.G + kGroupThreads / 64 - 1) / (kGroupThreads / 64);
-    if (dweight || dbias) fold += (2 * a.d + 15) / 16;
+    const int64_t fold = a.folds + param_folds;
     if (!sum_grid || !row_grid || !grid_ok(fold, kGroupThreads)) return SV_ERR_SHAPE;
     a.sum_chunks = b.sum_chunks = (int)sums.chunks;
-    const auto hs = static_cast<hipStream_t>(stream);
     with_group(in.bf16, silu, [&](auto t, auto s) { group_back_sums<decltype(t), s()><<<sum_grid, kGroupThreads, 0, hs>>>(a); });
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
     group_back_fold<<<(unsigned)fold, kGroupThreads, 0, hs>>>(a);

@@ -30,6 +30,14 @@ int main()
                         if (most == kGroupSumWgs) CHECK(BH * c.chunks * d <= group_slots(BH, N, d));
                     }
                     CHECK(group_slots(BH, N, d) <= group_slots(BH + 1, N, d) && group_slots(BH, N, d) <= group_slots(BH, N + 1, d));
+                    for (int width : {1, 2, 3, 10, 70, 256, d})
+                        for (int most : {kHeldForwardWords, kHeldBackwardWords}) {
+                            const int bytes = width * (per == 8 ? 2 : 4);
+                            const HeldForm f = held_form(N, bytes, most);
+                            if (!f.unit) continue;
+                            CHECK((f.unit == 2 || f.unit == 4 || f.unit == 16) && f.across * f.unit == bytes && f.across * f.lines <= kHeldThreads && f.lines >= 1);
+                            CHECK((long)f.lines * f.rows >= N && f.rows * (f.unit == 16 ? 4 : 1) <= most && (per == 8 || f.unit != 2));
+                        }
                     for (long H : {1L, 3L, 20L}) {
                         const ConvCut c = conv_cut(BH, N, H * pieces);
                         CHECK(c.across * c.down == kConvThreads && c.tiles * c.across >= H * pieces);
