@@ -2,6 +2,7 @@
 // tests.
 #pragma once
 
+#include <math.h>
 #include <stdint.h>
 
 #include "tile_walk.hpp"
@@ -10,8 +11,7 @@ namespace sv {
 
 constexpr int kScanWave = 64;               // channels of a wave
 constexpr int kScanRun = 4;                 // tokens whose states the backward pass holds at once: segments are multiples of it
-constexpr int kScanShortest = 32;           // tokens of a segment, where there is more than one
-constexpr int kScanMostSegments = 128;      // what scan_states walks one after the other
+constexpr int kScanShortest = 8;            // tokens of a segment, where there is more than one
 
 // A sequence is walked by `segments` waves per channel block, `per_segment` tokens each (the last fewer).
 struct ScanPlan {
@@ -19,15 +19,22 @@ struct ScanPlan {
     int segments, per_segment;
 };
 
-constexpr int64_t kScanForwardWaves = 4096, kScanBackwardWaves = 4096;
+// As many waves as run at once (forwards four on a SIMD, backwards two), cut no further than pays where there are few channels: a segment more
+// costs scan_states a step of its chain, a token less per segment the walks one of theirs, and they weigh the same with about sqrt(10 N) segments.
+constexpr int64_t kScanForwardWaves = 4096, kScanBackwardWaves = 2048;
 
+inline int64_t scan_longest_chain(int64_t n_tokens)
+{
+    const int64_t shortest = (n_tokens + kScanShortest - 1) / kScanShortest;
+    const int64_t s = (int64_t)sqrt((double)(10 * n_tokens));
+    return s < shortest ? s : shortest;
+}
 inline int64_t scan_most_segments(int64_t B, int64_t n_tokens, int64_t blocks, int64_t waves)
 {
-    int64_t s = waves / (B * blocks);
-    const int64_t longest = (n_tokens + kScanShortest - 1) / kScanShortest;
-    if (s > longest) s = longest;
-    if (s > kScanMostSegments) s = kScanMostSegments;
-    return s < 1 ? 1 : s;
+    const int64_t s = waves / (B * blocks);
+    if (s <= 1) return 1;
+    const int64_t longest = scan_longest_chain(n_tokens < (1 << 20) ? n_tokens : 1 << 20);
+    return s < longest ? s : longest;
 }
 inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_tokens, int64_t waves)
 {
@@ -45,8 +52,8 @@ inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_token
 // Segments of all sequences together in the largest call with no more batches and tokens and the same channels.
 inline int64_t scan_slots(int64_t B, int64_t n_tokens, int64_t channels, int64_t waves)
 {
-    const int64_t blocks = (channels + kScanWave - 1) / kScanWave, longest = (n_tokens + kScanShortest - 1) / kScanShortest;
-    const int64_t most = B * (longest < kScanMostSegments ? longest : kScanMostSegments), full = waves / blocks > B ? waves / blocks : B;
+    const int64_t blocks = (channels + kScanWave - 1) / kScanWave;
+    const int64_t most = B * scan_longest_chain(n_tokens < (1 << 20) ? n_tokens : 1 << 20), full = waves / blocks > B ? waves / blocks : B;
     return most < full ? most : full;
 }
 
