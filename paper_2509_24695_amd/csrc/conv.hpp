@@ -88,7 +88,8 @@ __device__ __forceinline__ typename P::V conv_row(const ConvArgs &a, const T *x,
     return t < length ? *reinterpret_cast<const V *>(x + t * a.sx.n) : V{};
 }
 
-// The rows of a run that come next, AHEAD at a time.  Past the last the last one is read again: no branch stands between the loads.
+// The rows of a run that come next, AHEAD at a time.  Past the last the last one is read again: no branch stands between a group's
+// loads.
 template <typename T, typename P, int AHEAD> struct ConvRows {
     typedef typename P::V V;
     const T *at, *end;
@@ -99,8 +100,13 @@ template <typename T, typename P, int AHEAD> struct ConvRows {
         : at(x + first * stride), end(x + (last - 1) * stride), stride(stride), left(last - first) {}
     __device__ __forceinline__ void request()
     {
+        if (left >= AHEAD) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) next[i] = *reinterpret_cast<const V *>(i < left ? at + i * stride : end);
+            for (int i = 0; i < AHEAD; ++i) next[i] = *reinterpret_cast<const V *>(at + i * stride);
+        } else {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) next[i] = *reinterpret_cast<const V *>(i < left ? at + i * stride : end);
+        }
         at += AHEAD * stride;
         left -= AHEAD;
     }

@@ -11,7 +11,7 @@ namespace sv {
 constexpr int kConvThreads = 256;
 inline int conv_run(int64_t BN, int pieces)
 {
-    for (int run = 32; run > 4; run /= 2)
+    for (int run = 16; run > 4; run /= 2)
         if (BN * pieces / run >= (int64_t)256 * 1024) return run;
     return 4;
 }
@@ -23,6 +23,7 @@ struct ConvCut {
     int64_t tiles, blocks;             // workgroups across the channels; workgroups along one sequence
 };
 constexpr int kConvMostRun = 64;
+constexpr int64_t kConvBackwardWgs = 2048;
 inline ConvCut conv_cut(int64_t B, int64_t N, int64_t pieces)
 {
     ConvCut c{};
@@ -31,17 +32,17 @@ inline ConvCut conv_cut(int64_t B, int64_t N, int64_t pieces)
     c.down = kConvThreads / c.across;
     c.tiles = (pieces + c.across - 1) / c.across;
     c.run = 4;
-    while (c.run < kConvMostRun && B * ((N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run)) * c.tiles > 1024) c.run *= 2;
+    while (c.run < kConvMostRun && B * ((N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run)) * c.tiles > kConvBackwardWgs) c.run *= 2;
     c.blocks = (N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run);
     return c;
 }
-// Partial sums of a call; and of the largest call with no more batches, tokens and channels: with more than 1 024 workgroups runs are as long as they
-// get, with fewer these leave at most 1 024 sums of 256 channels.
+// Partial sums of a call; and of the largest call with no more batches, tokens and channels: with more than kConvBackwardWgs workgroups runs are as long as they
+// get, with fewer these leave at most as many sums of 256 channels.
 inline int64_t conv_partial_floats(int64_t B, int64_t blocks, int64_t channels, int taps) { return B * blocks * channels * (taps + 1); }
 inline int64_t conv_workspace_floats(int64_t B, int64_t N, int64_t channels)
 {
     const int64_t shortest = B * ((N + 31) / 32) * channels, longest = B * ((N + 511) / 512) * channels;
-    const int64_t most = longest > 1024 * 256 ? longest : 1024 * 256;
+    const int64_t most = longest > kConvBackwardWgs * 256 ? longest : kConvBackwardWgs * 256;
     return 5 * (shortest < most ? shortest : most);
 }
 
