@@ -223,7 +223,7 @@ template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds_
     const int block = (int)(rest % a.runs), b = (int)(rest / a.runs), down = kConvThreads / a.across;
     const int col = (int)threadIdx.x % a.across, line = (int)threadIdx.x / a.across;
     const uint32_t piece = tile * a.across + col;
-    const bool mine = piece < a.pieces.extent;
+    const bool mine = piece < a.pieces.extent && line < down;
     const int length = held_length(a.lengths, b, a.N);
     const int64_t begin = ((int64_t)block * down + line) * a.run;      // past the last token of a short sequence: nothing
     const int first = begin < length ? (int)begin : length, last = first + a.run < length ? first + a.run : length;
@@ -326,7 +326,8 @@ template <typename T, int K, bool SILU, bool PARAMS> __global__ __launch_bounds_
         for (int j = 0; j <= K; ++j) {
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < kN; ++e) sums[(line * kN + e) * a.across + col] = j < K ? dw[j < K ? j : 0][e] : db[e];
+            for (int e = 0; e < kN; ++e)
+                if (line < down) sums[(line * kN + e) * a.across + col] = j < K ? dw[j < K ? j : 0][e] : db[e];
             __syncthreads();
             for (int q = threadIdx.x; q < width; q += kConvThreads) {
                 float s = sums[q];

@@ -16,22 +16,21 @@ inline int conv_run(int64_t BN, int pieces)
     return 4;
 }
 
-// Backwards a workgroup is `across` pieces by `down` runs of tokens, so that one partial sum of the parameters' gradients is left for all
+// Backwards a workgroup is `across` pieces (at most 32, as many in every tile) by `down` runs of tokens, so that one partial sum of the parameters' gradients is left for all
 // of its runs.
 struct ConvCut {
     int across, down, run;             // run: tokens of a thread
     int64_t tiles, blocks;             // workgroups across the channels; workgroups along one sequence
 };
-constexpr int kConvMostRun = 64;
+constexpr int kConvLeastRun = 8, kConvMostRun = 64;
 constexpr int64_t kConvBackwardWgs = 2048;
 inline ConvCut conv_cut(int64_t B, int64_t N, int64_t pieces)
 {
     ConvCut c{};
-    c.across = 32;
-    while (c.across > 4 && c.across / 2 >= pieces) c.across /= 2;
+    c.tiles = (pieces + 31) / 32;
+    c.across = (int)((pieces + c.tiles - 1) / c.tiles);
     c.down = kConvThreads / c.across;
-    c.tiles = (pieces + c.across - 1) / c.across;
-    c.run = 4;
+    c.run = kConvLeastRun;
     while (c.run < kConvMostRun && B * ((N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run)) * c.tiles > kConvBackwardWgs) c.run *= 2;
     c.blocks = (N + (int64_t)c.down * c.run - 1) / ((int64_t)c.down * c.run);
     return c;

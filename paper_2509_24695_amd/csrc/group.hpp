@@ -24,6 +24,8 @@ struct GroupArgs {
     TokStrides sx, sdy, sy;
     const float *weight, *bias;            // [d] or NULL
     double *sums;                          // [BH][chunks][2][d]: of x and x^2 (backward fp32, of da and da xh)
+    double *pairs;                         // [BH][chunks][tiles][per_tile][2]: the same by group (backward of t and t xh); NULL: groups are narrow
+    int per_tile, sum_tiles, tile_width;   // groups and channels of a tile of the launch that writes them
     float *level, *scale;                  // [BH][G]: mean and rstd; backward: sum t / count and sum (t xh) / count
     float *mean, *rstd;                    // [BH][G]: outputs, or backward inputs
     float *dw, *db;
@@ -58,7 +60,7 @@ template <typename T, typename P> struct GroupPlace {
         line = (int)threadIdx.x / a.across;
         down = kGroupThreads / a.across;
         c = (tile * a.across + col) * P::kN;
-        mine = c < a.d;
+        mine = c < a.d && line < down;
         first = (int64_t)chunk * a.rows;
         last = first + a.rows < a.N ? first + a.rows : a.N;
     }
@@ -113,28 +115,56 @@ template <typename T, typename P, bool BOTH, typename F> __device__ __forceinlin
         if (row + i * at.down < at.last) f(row + i * at.down, nx[i], ndy[i]);
 }
 
-// Sums of a workgroup's lines, two numbers (of type S) a channel, into its place of `sums`.
-template <typename T, typename P, typename S, int N> __device__ __forceinline__ void group_store_sums(const GroupArgs &a, const GroupPlace<T, P> &at, const S (&p)[N], const S (&q)[N])
+// Sums over a workgroup's lines of two numbers (of type S) a channel: into its place of `sums`, and (PAIRS) by group into its place of `pairs`, there
+// times the channel's weight if `weigh`.
+template <bool SUMS, bool PAIRS, typename T, typename P, typename S, int N>
+__device__ __forceinline__ void group_store_sums(const GroupArgs &a, const GroupPlace<T, P> &at, const S (&p)[N], const S (&q)[N], bool weigh)
 {
     __shared__ S lines[kGroupThreads * N];
-    S *out = reinterpret_cast<S *>(a.sums) + ((int64_t)at.bh * a.chunks + at.chunk) * 2 * a.d;
-    const int width = a.across * N;
+    __shared__ double channels[2][32 * N];
+    const int64_t part = (int64_t)at.bh * a.chunks + at.chunk;
+    S *out = reinterpret_cast<S *>(a.sums) + part * 2 * a.d;
+    const int width = a.across * N, c0 = at.tile * width;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < N; ++e) lines[at.line * width + at.col * N + e] = which ? q[e] : p[e];
+        for (int e = 0; e < N; ++e)
+            if (at.line < at.down) lines[at.line * width + at.col * N + e] = which ? q[e] : p[e];
         __syncthreads();
         for (int k = threadIdx.x; k < width; k += kGroupThreads) {
             S s = lines[k];
             for (int r = 1; r < at.down; ++r) s += lines[r * width + k];
-            const int c = at.tile * width + k;
-            if (c < a.d) out[which * a.d + c] = s;
+            const int c = c0 + k;
+            if (SUMS && c < a.d) out[which * a.d + c] = s;
+            if (PAIRS) channels[which][k] = c < a.d ? (weigh ? (double)a.weight[c] : 1.) * (double)s : 0.;
+        }
+    }
+    if constexpr (PAIRS) {
+        __syncthreads();
+        const int lane = threadIdx.x % 64, first = c0 / a.width, end = c0 + width < a.d ? c0 + width : a.d;
+        for (int g = first + (int)threadIdx.x / 64; g * a.width < end; g += kGroupThreads / 64) {
+            const int from = g * a.width > c0 ? g * a.width - c0 : 0, to = (g + 1) * a.width < end ? (g + 1) * a.width - c0 : end - c0;
+            double s = 0., t = 0.;
+            for (int k = from + lane; k < to; k += 64) {
+                s += channels[0][k];
+                t += channels[1][k];
+            }
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) {
+                s += __shfl_xor(s, m, 64);
+                t += __shfl_xor(t, m, 64);
+            }
+            double *pair = a.pairs + ((part * a.tiles + at.tile) * a.per_tile + g - first) * 2;
+            if (lane == 0) {
+                pair[0] = s;
+                pair[1] = t;
+            }
         }
     }
 }
 
-template <typename T> __global__ __launch_bounds__(kGroupThreads) void group_sums(GroupArgs a)
+template <typename T, bool WIDE> __global__ __launch_bounds__(kGroupThreads) void group_sums(GroupArgs a)
 {
     using P = GroupSums<T>;
     typedef typename P::V V;
@@ -154,7 +184,7 @@ template <typename T> __global__ __launch_bounds__(kGroupThreads) void group_sum
                 q[e] = __builtin_fma(v, v, q[e]);
             }
         });
-    group_store_sums<T, P, double, kN>(a, at, s, q);
+    group_store_sums<!WIDE, WIDE>(a, at, s, q, false);
 }
 
 // A workgroup's sums of two numbers, for all of its threads (`lds`: two for each wave).
@@ -203,6 +233,20 @@ template <typename S, typename F> __device__ __forceinline__ void group_gather(c
     }
 }
 
+// A group's two sums out of the pairs of its chunks and tiles.
+__device__ __forceinline__ void group_gather_pairs(const GroupArgs &a, int64_t bh, int group, double &s, double &q)
+{
+    const int t0 = group * a.width / a.tile_width, t1 = ((group + 1) * a.width - 1) / a.tile_width, n = t1 - t0 + 1, count = a.sum_chunks * n;
+    const double *p = a.pairs + bh * a.sum_chunks * a.sum_tiles * a.per_tile * 2;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < count; k += kGroupThreads) {
+        const int chunk = k / n, t = t0 + k - chunk * n;
+        const double *pair = p + (((int64_t)chunk * a.sum_tiles + t) * a.per_tile + group - t * a.tile_width / a.width) * 2;
+        s += pair[0];
+        q += pair[1];
+    }
+}
+
 // mean and rstd from a group's sums of x and (x - from)^2
 __device__ __forceinline__ float group_scale(double squares, double over, float eps)
 {
@@ -216,10 +260,12 @@ __global__ __launch_bounds__(kGroupThreads) void group_fold(GroupArgs a)
     __shared__ double lds[2 * kGroupThreads / 64];
     const int64_t id = blockIdx.x, bh = id / a.G;
     double s = 0., q = 0.;
-    group_gather<double>(a, bh, (int)(id - bh * a.G), [&](int, double x, double xx) {
-        s += x;
-        q += xx;
-    });
+    if (a.pairs) group_gather_pairs(a, bh, (int)(id - bh * a.G), s, q);
+    else
+        group_gather<double>(a, bh, (int)(id - bh * a.G), [&](int, double x, double xx) {
+            s += x;
+            q += xx;
+        });
     group_total<kGroupThreads>(s, q, lds);
     if (threadIdx.x) return;
     const double over = 1. / ((double)a.N * a.width), mean = s * over;
@@ -274,8 +320,8 @@ __device__ __forceinline__ void group_terms(typename P::V vx, typename P::V vdy,
     }
 }
 
-// Sums of da and da xh by channel.
-template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) void group_back_sums(GroupArgs a)
+// Sums of da and da xh, by channel (SUMS) and, for wide groups, by group.
+template <typename T, bool SILU, bool SUMS, bool WIDE> __global__ __launch_bounds__(kGroupThreads) void group_back_sums(GroupArgs a)
 {
     using P = GroupBack<T>;
     typedef typename P::V V;
@@ -300,7 +346,7 @@ template <typename T, bool SILU> __global__ __launch_bounds__(kGroupThreads) voi
             }
         });
     }
-    group_store_sums<T, P, float, kN>(a, at, p, q);
+    group_store_sums<SUMS, WIDE>(a, at, p, q, a.weight != nullptr);
 }
 
 // Of each group sum t / count and sum (t xh) / count (a workgroup each, in fp64); behind these db and dw of each channel.
@@ -312,11 +358,13 @@ __global__ __launch_bounds__(kGroupThreads) void group_back_fold(GroupArgs a)
         __shared__ double lds[2 * kGroupThreads / 64];
         const int64_t id = blockIdx.x, bh = id / a.G;
         double s = 0., q = 0.;
-        group_gather<float>(a, bh, (int)(id - bh * a.G), [&](int c, float p, float px) {
-            const double w = a.weight ? a.weight[c] : 1.f;
-            s = __builtin_fma(w, (double)p, s);
-            q = __builtin_fma(w, (double)px, q);
-        });
+        if (a.pairs) group_gather_pairs(a, bh, (int)(id - bh * a.G), s, q);
+        else
+            group_gather<float>(a, bh, (int)(id - bh * a.G), [&](int c, float p, float px) {
+                const double w = a.weight ? a.weight[c] : 1.f;
+                s = __builtin_fma(w, (double)p, s);
+                q = __builtin_fma(w, (double)px, q);
+            });
         group_total<kGroupThreads>(s, q, lds);
         const double over = 1. / ((double)a.N * a.width);
         if (threadIdx.x == 0) {

@@ -5,7 +5,7 @@
 
 namespace sv {
 
-// A workgroup is `across` 16-byte pieces by `down` rows, and walks a chunk of the rows of one (b, h).
+// A workgroup is `across` pieces (at most 32, as many in every tile) by `down` rows, and walks a chunk of the rows of one (b, h).
 constexpr int kGroupThreads = 256, kGroupAhead = 4;
 struct GroupCut {
     int across, down;
@@ -16,10 +16,9 @@ struct GroupCut {
 inline GroupCut group_cut(int64_t BH, int64_t N, int64_t pieces, int64_t most)
 {
     GroupCut c{};
-    c.across = 32;
-    while (c.across > 4 && c.across / 2 >= pieces) c.across /= 2;
+    c.tiles = (pieces + 31) / 32;
+    c.across = (int)((pieces + c.tiles - 1) / c.tiles);
     c.down = kGroupThreads / c.across;
-    c.tiles = (pieces + c.across - 1) / c.across;
     const int64_t step = (int64_t)c.down * kGroupAhead, steps = (N + step - 1) / step;
     int64_t chunks = most / (BH * c.tiles);
     chunks = chunks > steps ? steps : chunks < 1 ? 1 : chunks;
@@ -28,6 +27,11 @@ inline GroupCut group_cut(int64_t BH, int64_t N, int64_t pieces, int64_t most)
     return c;
 }
 constexpr int64_t kGroupSumWgs = 1024, kGroupApplyWgs = 4096;
+
+// Sums of wide groups are kept by group: a chunk and tile leave two numbers for each group that the tile touches, at most this many groups.
+// Those of narrow ones are kept by channel, and so are those that become the parameters' gradients.
+constexpr int kWideGroup = 32;
+inline int group_pairs(int64_t tile_channels, int64_t width) { return (int)((tile_channels - 1) / width) + 2; }
 
 // Chunks times channels of all (b, h) together in the largest call with no more batches, heads and rows and the same d: with one chunk each
 // these are BH d, with more there are at most kGroupSumWgs workgroups of 32 pieces of at most eight channels; and a chunk has at least 32 rows.

@@ -69,11 +69,11 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) 
     else if (at.segment > 0) scan_sum_back<T, n, GATE>(a, at);
 }
 
-template <int n> __global__ __launch_bounds__(256) void scan_back_states(ScanArgs a)
+template <int n, int RUNS, int SPAN> __global__ __launch_bounds__(64 * RUNS) void scan_back_states(ScanArgs a)
 {
     const int half = (int)gridDim.x / 2;
-    if ((int)blockIdx.x < half) scan_state<n, false>(a, (int)blockIdx.x);
-    else scan_state<n, true>(a, (int)blockIdx.x - half);
+    if ((int)blockIdx.x < half) scan_state<n, RUNS, SPAN, false>(a, (int)blockIdx.x);
+    else scan_state<n, RUNS, SPAN, true>(a, (int)blockIdx.x - half);
 }
 
 // Sums over the wave of 2 n values, n of either kind, by exchanges: two lanes keep one of two values each and get the other's share of it.

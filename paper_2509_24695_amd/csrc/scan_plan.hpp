@@ -2,7 +2,6 @@
 // tests.
 #pragma once
 
-#include <math.h>
 #include <stdint.h>
 
 #include "tile_walk.hpp"
@@ -19,22 +18,19 @@ struct ScanPlan {
     int segments, per_segment;
 };
 
-// As many waves as run at once (forwards four on a SIMD, backwards two), cut no further than pays where there are few channels: a segment more
-// costs scan_states a step of its chain, a token less per segment the walks one of theirs, and they weigh the same with about sqrt(10 N) segments.
+// As many waves as run at once: forwards four on a SIMD, backwards two.
+constexpr int kScanMostSegments = 512;
 constexpr int64_t kScanForwardWaves = 4096, kScanBackwardWaves = 2048;
 
 inline int64_t scan_longest_chain(int64_t n_tokens)
 {
     const int64_t shortest = (n_tokens + kScanShortest - 1) / kScanShortest;
-    const int64_t s = (int64_t)sqrt((double)(10 * n_tokens));
-    return s < shortest ? s : shortest;
+    return shortest < kScanMostSegments ? shortest : kScanMostSegments;
 }
 inline int64_t scan_most_segments(int64_t B, int64_t n_tokens, int64_t blocks, int64_t waves)
 {
-    const int64_t s = waves / (B * blocks);
-    if (s <= 1) return 1;
-    const int64_t longest = scan_longest_chain(n_tokens < (1 << 20) ? n_tokens : 1 << 20);
-    return s < longest ? s : longest;
+    const int64_t s = waves / (B * blocks), longest = scan_longest_chain(n_tokens);
+    return s < 1 ? 1 : s < longest ? s : longest;
 }
 inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_tokens, int64_t waves)
 {
@@ -53,7 +49,7 @@ inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_token
 inline int64_t scan_slots(int64_t B, int64_t n_tokens, int64_t channels, int64_t waves)
 {
     const int64_t blocks = (channels + kScanWave - 1) / kScanWave;
-    const int64_t most = B * scan_longest_chain(n_tokens < (1 << 20) ? n_tokens : 1 << 20), full = waves / blocks > B ? waves / blocks : B;
+    const int64_t most = B * scan_longest_chain(n_tokens), full = waves / blocks > B ? waves / blocks : B;
     return most < full ? most : full;
 }
 

@@ -37,6 +37,14 @@ GroupArgs group_args(const Shape &x, int groups, void *workspace)
     a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + lines(2 * a.BH * groups * (int64_t)sizeof(float)));
     return a;
 }
+// Where the sums of wide groups go: `pairs`, as many as group_slots has channels for.
+void pair_args(GroupArgs &a, const GroupCut &c, int channels, double *pairs)
+{
+    a.tile_width = c.across * channels;
+    a.sum_tiles = (int)c.tiles;
+    a.per_tile = group_pairs(a.tile_width, a.width);
+    a.pairs = a.width >= kWideGroup ? pairs : nullptr;
+}
 // The workgroups of a launch; 0: more than a launch has.
 unsigned cut_args(GroupArgs &a, const GroupCut &c)
 {
@@ -101,7 +109,7 @@ extern "C" size_t sv_groupnorm_workspace_bytes(int32_t B, int32_t H, int32_t n_t
 
 extern "C" size_t sv_groupnorm_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t groups)
 {
-    return workspace_bytes_of(B, H, n_tokens, d, groups, sizeof(float));
+    return workspace_bytes_of(B, H, n_tokens, d, groups, 2 * sizeof(float));
 }
 
 extern "C" sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const float *weight, const float *bias, int32_t groups, float eps, int32_t silu,
@@ -135,13 +143,19 @@ extern "C" sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const 
         });
         return launched();
     }
+    pair_args(a, sums, 16 / in.elem_bytes, a.sums);
     GroupArgs b = a;
     const unsigned sum_grid = cut_args(a, sums), row_grid = cut_args(b, rows);
     const int64_t fold = a.BH * a.G;
     if (!sum_grid || !row_grid || !grid_ok(fold, kGroupThreads)) return SV_ERR_SHAPE;
     a.sum_chunks = b.sum_chunks = (int)sums.chunks;
-    if (in.bf16) group_sums<uint16_t><<<sum_grid, kGroupThreads, 0, hs>>>(a);
-    else group_sums<float><<<sum_grid, kGroupThreads, 0, hs>>>(a);
+    auto sum = [&](auto t, auto wide) { group_sums<decltype(t), wide()><<<sum_grid, kGroupThreads, 0, hs>>>(a); };
+    auto sum_of = [&](auto t) {
+        if (a.pairs) sum(t, std::true_type{});
+        else sum(t, std::false_type{});
+    };
+    if (in.bf16) sum_of(uint16_t{});
+    else sum_of(float{});
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
     group_fold<<<(unsigned)fold, kGroupThreads, 0, hs>>>(a);
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
@@ -168,7 +182,7 @@ extern "C" sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *
     GroupArgs a = group_args(in, groups, workspace);
     const int pieces = in.d / 4;
     const GroupCut sums = group_cut(a.BH, a.N, pieces, kGroupSumWgs), rows = group_cut(a.BH, a.N, pieces, kGroupApplyWgs);
-    if (workspace_bytes < (size_t)(reinterpret_cast<char *>(a.sums) - static_cast<char *>(workspace)) + (size_t)a.BH * sums.chunks * 2 * a.d * sizeof(float))
+    if (workspace_bytes < (size_t)(reinterpret_cast<char *>(a.sums) - static_cast<char *>(workspace)) + (size_t)a.BH * sums.chunks * 2 * a.d * 2 * sizeof(float))
         return SV_ERR_WORKSPACE;
     a.x = X; a.dy = dY; a.y = dX; a.sdy = grad.st; a.sy = out.st;
     a.weight = weight; a.bias = bias; a.dw = dweight; a.db = dbias;
@@ -196,12 +210,19 @@ extern "C" sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *
         return launched();
     }
     a.folds = a.BH * a.G;
+    // (the first half of the sums' place is the channels', the second the groups')
+    pair_args(a, sums, 4, a.sums + a.BH * sums.chunks * a.d);
     GroupArgs b = a;
     const unsigned sum_grid = cut_args(a, sums), row_grid = cut_args(b, rows);
     const int64_t fold = a.folds + param_folds;
     if (!sum_grid || !row_grid || !grid_ok(fold, kGroupThreads)) return SV_ERR_SHAPE;
     a.sum_chunks = b.sum_chunks = (int)sums.chunks;
-    with_group(in.bf16, silu, [&](auto t, auto s) { group_back_sums<decltype(t), s()><<<sum_grid, kGroupThreads, 0, hs>>>(a); });
+    with_group(in.bf16, silu, [&](auto t, auto s) {
+        auto go = [&](auto by_channel, auto wide) { group_back_sums<decltype(t), s(), by_channel(), wide()><<<sum_grid, kGroupThreads, 0, hs>>>(a); };
+        if (!a.pairs) go(std::true_type{}, std::false_type{});
+        else if (params) go(std::true_type{}, std::true_type{});
+        else go(std::false_type{}, std::true_type{});
+    });
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
     group_back_fold<<<(unsigned)fold, kGroupThreads, 0, hs>>>(a);
     if (launched() != SV_OK) return SV_ERR_LAUNCH;

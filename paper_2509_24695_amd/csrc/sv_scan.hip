@@ -68,6 +68,19 @@ template <typename F> void with_scan(bool bf16, int n, bool gate, F &&f)
     else sized(float{});
 }
 
+// Calls f(runs, span) with the form of scan_states for this many segments.
+template <typename F> void with_span(int segments, F &&f)
+{
+    const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 16> sixteen;
+    if (segments <= 16) f(four, four);
+    else if (segments <= 32) f(four, std::integral_constant<int, 8>{});
+    else if (segments <= 64) f(sixteen, four);
+    else if (segments <= 128) f(sixteen, std::integral_constant<int, 8>{});
+    else f(sixteen, std::integral_constant<int, 32>{});
+}
+static_assert(kScanMostSegments <= 16 * 32, "segments of a sequence");
+
 bool sizes_ok(int32_t B, int32_t H, int32_t N, int32_t d, int32_t n)
 {
     return B > 0 && H > 0 && N > 0 && d > 0 && d % 4 == 0 && d <= kMostRowWidth && state_ok(n) && (int64_t)B * H <= kMostHeads;
@@ -105,8 +118,8 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
     ScanArgs a = scan_args(su, sz, sbc, sy, plan);
     const int64_t states = (int64_t)a.B * a.segments * a.channels * n, waves = (int64_t)a.B * a.segments * a.blocks;
     if (a.segments > 1 && workspace_bytes < (size_t)(states + states / n) * sizeof(float)) return SV_ERR_WORKSPACE;
-    const int64_t scan = (int64_t)a.B * (((int64_t)a.channels * n + 255) / 256);
-    if (!grid_ok(scan_grid(waves), kScanWave) || !grid_ok(scan, 256)) return SV_ERR_SHAPE;
+    const int64_t scan = (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
+    if (!grid_ok(scan_grid(waves), kScanWave) || !grid_ok(scan, 1024)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.y = Y;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.s_out = S_out;
@@ -118,7 +131,7 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
         if (a.segments > 1) {
             scan_sums<decltype(t), k()><<<(unsigned)scan_grid(waves / a.segments * (a.segments - 1)), kScanWave, 0, hs>>>(a);
             if ((done = launched()) != SV_OK) return;
-            scan_states<k()><<<(unsigned)scan, 256, 0, hs>>>(a);
+            with_span(a.segments, [&](auto runs, auto span) { scan_states<k(), runs(), span()><<<(unsigned)scan, 64 * runs(), 0, hs>>>(a); });
             if ((done = launched()) != SV_OK) return;
         }
         scan_walk<decltype(t), k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);
@@ -179,9 +192,9 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     ScanArgs a = scan_args(su, sz, sbc, sy, plan);
     const ScanBackwardSpace space = scan_backward_space(a.B, a.G, a.channels, a.N, n, (int64_t)a.B * a.segments);
     if (workspace_bytes < (size_t)space.total * sizeof(float)) return SV_ERR_WORKSPACE;
-    const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = 2 * (int64_t)a.B * (((int64_t)a.channels * n + 255) / 256);
+    const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = 2 * (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
     const int64_t shared = ((int64_t)a.B * a.G * a.N * 2 * n + 255) / 256, params = ((int64_t)a.channels * (n + 2) + 255) / 256;
-    if (!grid_ok(2 * scan_grid(waves), kScanWave) || !grid_ok(states, 256) || !grid_ok(shared, 256) || !grid_ok(params, 256)) return SV_ERR_SHAPE;
+    if (!grid_ok(2 * scan_grid(waves), kScanWave) || !grid_ok(states, 1024) || !grid_ok(shared, 256) || !grid_ok(params, 256)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.dy = dY;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.ds_out = dS_out;
@@ -202,7 +215,7 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
         scan_back_sums<T, k(), gate()><<<(unsigned)(2 * scan_grid(waves)), kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
         if (a.segments > 1) {
-            scan_back_states<k()><<<(unsigned)states, 256, 0, hs>>>(a);
+            with_span(a.segments, [&](auto runs, auto span) { scan_back_states<k(), runs(), span()><<<(unsigned)states, 64 * runs(), 0, hs>>>(a); });
             if ((done = launched()) != SV_OK) return;
         }
         scan_back_walk<T, k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);

@@ -24,9 +24,11 @@ int main()
                     const long pieces = d / per;
                     for (long most : {kGroupSumWgs, kGroupApplyWgs}) {
                         const GroupCut c = group_cut(BH, N, pieces, most);
-                        CHECK(c.across * c.down == kGroupThreads && c.tiles * c.across >= pieces && (c.tiles - 1) * c.across < pieces);
+                        CHECK(c.across <= 32 && c.across * c.down <= kGroupThreads && c.across * (c.down + 1) > kGroupThreads && c.tiles * c.across >= pieces && (c.tiles - 1) * c.across < pieces);
                         CHECK(c.chunks >= 1 && c.chunks * c.rows >= N && (c.chunks - 1) * c.rows < N && c.rows % c.down == 0);
                         CHECK(c.chunks == 1 || BH * c.tiles * c.chunks <= most);
+                        for (int width : {32, 40, 70, 256, d})
+                            if (width >= kWideGroup && width <= d) CHECK(2 * c.tiles * group_pairs(c.across * per, width) <= d);
                         if (most == kGroupSumWgs) CHECK(BH * c.chunks * d <= group_slots(BH, N, d));
                     }
                     CHECK(group_slots(BH, N, d) <= group_slots(BH + 1, N, d) && group_slots(BH, N, d) <= group_slots(BH, N + 1, d));
@@ -40,8 +42,8 @@ int main()
                         }
                     for (long H : {1L, 3L, 20L}) {
                         const ConvCut c = conv_cut(BH, N, H * pieces);
-                        CHECK(c.across * c.down == kConvThreads && c.tiles * c.across >= H * pieces);
-                        CHECK(c.blocks * c.down * c.run >= N && (c.blocks - 1) * c.down * c.run < N && c.run >= 4 && c.run <= kConvMostRun);
+                        CHECK(c.across <= 32 && c.across * c.down <= kConvThreads && c.across * (c.down + 1) > kConvThreads && c.tiles * c.across >= H * pieces);
+                        CHECK(c.blocks * c.down * c.run >= N && (c.blocks - 1) * c.down * c.run < N && c.run >= kConvLeastRun && c.run <= kConvMostRun);
                         CHECK(conv_partial_floats(BH, c.blocks, H * d, 4) <= conv_workspace_floats(BH, N, H * d));
                         CHECK(conv_workspace_floats(BH, N, H * d) <= conv_workspace_floats(BH + 1, N, H * d));
                         CHECK(conv_workspace_floats(BH, N, H * d) <= conv_workspace_floats(BH, N + 1, H * d));

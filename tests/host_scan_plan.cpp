@@ -23,7 +23,7 @@ int main()
                         if (B * N > (1L << 31)) continue;
                         const ScanPlan p = scan_plan(B, G, K, N, waves);
                         CHECK(p.blocks == G * ((K + 63) / 64));
-                        CHECK(p.segments >= 1 && (p.segments == 1 || (long)p.segments * p.segments <= 10L * N));
+                        CHECK(p.segments >= 1 && p.segments <= kScanMostSegments);
                         CHECK(p.per_segment % kScanRun == 0);
                         CHECK((int64_t)p.per_segment * p.segments >= N && (int64_t)p.per_segment * (p.segments - 1) < N);
                         CHECK(p.segments == 1 || p.per_segment >= kScanShortest);
