@@ -33,6 +33,9 @@ constexpr int64_t kGroupSumWgs = 1024, kGroupApplyWgs = 4096;
 constexpr int kWideGroup = 32;
 inline int group_pairs(int64_t tile_channels, int64_t width) { return (int)((tile_channels - 1) / width) + 2; }
 
+// With this many pairs a group at most the workgroups of the next launch add them up themselves.
+constexpr int64_t kFoldedPairs = 128;
+
 // Chunks times channels of all (b, h) together in the largest call with no more batches, heads and rows and the same d: with one chunk each
 // these are BH d, with more there are at most kGroupSumWgs workgroups of 32 pieces of at most eight channels; and a chunk has at least 32 rows.
 inline int64_t group_slots(int64_t BH, int64_t N, int64_t d)

@@ -157,9 +157,13 @@ extern "C" sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const 
     if (in.bf16) sum_of(uint16_t{});
     else sum_of(float{});
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
+    if (a.pairs && sums.chunks * ((a.width - 1) / a.tile_width + 2) <= kFoldedPairs) {
+        with_group(in.bf16, silu, [&](auto t, auto s) { group_apply<decltype(t), s(), true><<<row_grid, kGroupThreads, 0, hs>>>(b); });
+        return launched();
+    }
     group_fold<<<(unsigned)fold, kGroupThreads, 0, hs>>>(a);
     if (launched() != SV_OK) return SV_ERR_LAUNCH;
-    with_group(in.bf16, silu, [&](auto t, auto s) { group_apply<decltype(t), s()><<<row_grid, kGroupThreads, 0, hs>>>(b); });
+    with_group(in.bf16, silu, [&](auto t, auto s) { group_apply<decltype(t), s(), false><<<row_grid, kGroupThreads, 0, hs>>>(b); });
     return launched();
 }
 

@@ -18,6 +18,10 @@ CASES = [
     (1, 1, 20, 8192, 64, True, "bf16", "bhnd", True, 0.3), (1, 1, 9, 8192, 8192, False, "f32", "bhnd", True, 0.3), (1, 1, 333, 64, 4, True, "f32", "bhnd", True, 300.0),
     (1, 3, 1560, 140, 2, True, "f32", "bhnd", True, 0.3), (2, 2, 700, 40, 8, True, "bf16", "bnhd", True, 2.0), (1, 2, 3000, 24, 8, False, "bf16", "apart", True, 0.3),
     (1, 1, 2000, 512, 4, True, "bf16", "bhnd", True, 0.3), (1, 1, 130, 2048, 1, True, "bf16", "bhnd", True, 0.3), (3, 7, 100, 256, 1, False, "f32", "bhnd", True, 0.3),
+    # streamed: wide groups whose sums go by group (added up by the next launch's workgroups, or by one of their own), groups across tiles, narrow ones
+    (2, 1, 5000, 384, 4, True, "bf16", "bhnd", True, 0.3), (2, 3, 2000, 384, 4, True, "bf16", "bnhd", True, 2.0), (1, 2, 1500, 520, 1, False, "bf16", "apart", False, 0.3),
+    (1, 3, 1100, 660, 5, True, "f32", "bhnd", True, 0.3), (3, 1, 2500, 296, 8, True, "bf16", "bhnd", True, 0.3), (1, 1, 7000, 72, 1, True, "f32", "apart", True, 0.3),
+    (2, 1, 9000, 320, 32, True, "bf16", "bhnd", True, 0.3),
     (5, 40, 3, 48, 6, True, "bf16", "bnhd", True, 0.3), (2, 700, 2, 32, 8, True, "bf16", "bhnd", True, 0.3), (1, 1, 9000, 264, 11, True, "bf16", "bhnd", True, 0.3),
 ]
 
@@ -85,6 +89,9 @@ def test_backward(c):
     _backward(c, x, inside, w, b, mean, rstd, inside, only, None)     # in place of dy, one of the parameters' gradients
     same_bits(dx, inside)
     same_bits(dw, only)
+    alone = like(x)
+    _backward(c, x, dy, w, b, mean, rstd, alone, None, None)
+    same_bits(dx, alone)
 
 
 @pytest.mark.parametrize("rows", [64, 70000])                         # held by one workgroup, and streamed
