@@ -23,7 +23,7 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
     for (int i = 0; i < n; ++i) g[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
     // tokens from the last: token k of the walk is last - 1 - k
-    Ahead<T, kScanAhead> dy, dt, z;
+    Ahead<T, kScanBackAhead> dy, dt, z;
     const int count = at.last - at.first;
     auto request = [&](int k) {
         const int64_t top = at.last - 1;
@@ -45,14 +45,14 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
         for (int i = 0; i < n; ++i) g[i] = __builtin_amdgcn_exp2f(D * A2[i]) * __builtin_fmaf(C[i], v, g[i]);
     };
     int k0 = 0;
-    for (; k0 + kScanAhead <= count; k0 += kScanAhead) {
-        const Ahead<T, kScanAhead> dy0 = dy, dt0 = dt, z0 = z;
-        request(k0 + kScanAhead);
+    for (; k0 + kScanBackAhead <= count; k0 += kScanBackAhead) {
+        const Ahead<T, kScanBackAhead> dy0 = dy, dt0 = dt, z0 = z;
+        request(k0 + kScanBackAhead);
 #pragma unroll
-        for (int k = 0; k < kScanAhead; ++k) token(k0 + k, dy0[k], dt0[k], GATE ? z0[k] : 0.f);
+        for (int k = 0; k < kScanBackAhead; ++k) token(k0 + k, dy0[k], dt0[k], GATE ? z0[k] : 0.f);
     }
 #pragma unroll
-    for (int k = 0; k < kScanAhead; ++k)
+    for (int k = 0; k < kScanBackAhead; ++k)
         if (k0 + k < count) token(k0 + k, dy[k], dt[k], GATE ? z[k] : 0.f);
     if (!at.mine) return;
 #pragma unroll

@@ -18,8 +18,9 @@ struct ScanPlan {
     int segments, per_segment;
 };
 
-// As many waves as run at once: forwards four on a SIMD, backwards two.
-constexpr int kScanMostSegments = 512;
+// As many waves as run at once, forwards four on a SIMD, backwards two; forwards twice as many where segments are long enough for it (a state
+// that is handed on costs 16 bytes of traffic a number): 32 760 tokens of 2 240 channels without a gate 490 us, with four 545; 8 190 tokens 181 and 168.
+constexpr int kScanMostSegments = 512, kScanLongSegment = 128;
 constexpr int64_t kScanForwardWaves = 4096, kScanBackwardWaves = 2048;
 
 inline int64_t scan_longest_chain(int64_t n_tokens)
@@ -29,7 +30,10 @@ inline int64_t scan_longest_chain(int64_t n_tokens)
 }
 inline int64_t scan_most_segments(int64_t B, int64_t n_tokens, int64_t blocks, int64_t waves)
 {
-    const int64_t s = waves / (B * blocks), longest = scan_longest_chain(n_tokens);
+    int64_t s = waves / (B * blocks), more = waves == kScanForwardWaves ? 2 * waves / (B * blocks) : 0;
+    if (more > n_tokens / kScanLongSegment) more = n_tokens / kScanLongSegment;
+    if (s < more) s = more;
+    const int64_t longest = scan_longest_chain(n_tokens);
     return s < 1 ? 1 : s < longest ? s : longest;
 }
 inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_tokens, int64_t waves)
@@ -49,7 +53,7 @@ inline ScanPlan scan_plan(int64_t B, int groups, int group_channels, int n_token
 inline int64_t scan_slots(int64_t B, int64_t n_tokens, int64_t channels, int64_t waves)
 {
     const int64_t blocks = (channels + kScanWave - 1) / kScanWave;
-    const int64_t most = B * scan_longest_chain(n_tokens), full = waves / blocks > B ? waves / blocks : B;
+    const int64_t most = B * scan_longest_chain(n_tokens), full = 2 * waves / blocks > B ? 2 * waves / blocks : B;
     return most < full ? most : full;
 }
 

@@ -30,7 +30,7 @@ int main()
                         CHECK(B * p.segments <= scan_slots(B, N, (int64_t)G * K, waves));
                         CHECK(scan_slots(B, N, (int64_t)G * K, waves) <= scan_slots(B + 1, N, (int64_t)G * K, waves));
                         CHECK(scan_slots(B, N, (int64_t)G * K, waves) <= scan_slots(B, N + 1, (int64_t)G * K, waves));
-                        CHECK(p.segments == 1 || B * p.segments * p.blocks <= waves);
+                        CHECK(p.segments == 1 || B * p.segments * p.blocks <= waves || (B * p.segments * p.blocks <= 2 * waves && p.per_segment >= kScanLongSegment));
                     }
     return 0;
 }
