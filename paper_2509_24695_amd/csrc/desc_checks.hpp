@@ -73,6 +73,7 @@ inline sv_status check_desc(const sv_tensor_desc *t, Shape *s, bool any_width = 
 
 constexpr int64_t kMostHeads = 1 << 24;        // batches times heads of the operators that deal rows, not heads, to the grid
 constexpr int kMostRowWidth = 8192;            // features of their widest row
+constexpr int kMostTokens = INT32_MAX - 4096;  // of the operators that count a little past the last token
 
 // A tensor of rows of any width that is whole 16-byte pieces.
 inline sv_status check_rows(const sv_tensor_desc *t, Shape *s)

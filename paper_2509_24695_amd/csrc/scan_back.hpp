@@ -248,26 +248,25 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
     if (a.ds_in && at.segment == 0) store_state<n>(a.ds_in, row, g);
 }
 
-// dB and dC: the blocks' sums over their channels, added up in order and rounded.
-template <typename T, int n> __global__ __launch_bounds__(256) void scan_back_shared(ScanArgs a)
+// dB and dC: the blocks' sums over their channels, added up in order and rounded.  Behind these workgroups (`shared` of them) dA, ddt_bias and dskip:
+// the segments' sums, added up in order.
+template <typename T, int n> __global__ __launch_bounds__(256) void scan_back_fold(ScanArgs a, uint32_t shared)
 {
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.N * 2 * n;
-    const int64_t bg = id / per, at = id - bg * per;
-    if (bg >= (int64_t)a.B * a.G) return;
-    const int b = (int)(bg / a.G), group = (int)(bg % a.G), t = (int)(at / (2 * n)), i = (int)(at % (2 * n));
-    if (t >= held_length(a.lengths, b, a.N)) return;
-    const float *p = a.shared + ((int64_t)b * a.blocks + group * a.group_blocks) * per + at;
-    float s = 0.f;
+    if (blockIdx.x < shared) {
+        const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.N * 2 * n;
+        const int64_t bg = id / per, at = id - bg * per;
+        if (bg >= (int64_t)a.B * a.G) return;
+        const int b = (int)(bg / a.G), group = (int)(bg % a.G), t = (int)(at / (2 * n)), i = (int)(at % (2 * n));
+        if (t >= held_length(a.lengths, b, a.N)) return;
+        const float *p = a.shared + ((int64_t)b * a.blocks + group * a.group_blocks) * per + at;
+        float s = 0.f;
 #pragma unroll 8
-    for (int k = 0; k < a.group_blocks; ++k) s += p[k * per];
-    T *out = static_cast<T *>(i < n ? a.db : a.dc) + b * a.sbc.b + group * a.sbc.h + t * a.sbc.n;
-    Elem<T>::store(out + i % n, s);
-}
-
-// dA, ddt_bias and dskip: the segments' sums, added up in order.
-template <int n> __global__ __launch_bounds__(256) void scan_back_params(ScanArgs a)
-{
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.channels * (n + 2);
+        for (int k = 0; k < a.group_blocks; ++k) s += p[k * per];
+        T *out = static_cast<T *>(i < n ? a.db : a.dc) + b * a.sbc.b + group * a.sbc.h + t * a.sbc.n;
+        Elem<T>::store(out + i % n, s);
+        return;
+    }
+    const int64_t id = (int64_t)(blockIdx.x - shared) * 256 + threadIdx.x, per = (int64_t)a.channels * (n + 2);
     if (id >= per) return;
     const int i = (int)(id / a.channels), c = (int)(id % a.channels);
     float s = 0.f;

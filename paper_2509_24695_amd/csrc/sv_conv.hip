@@ -34,7 +34,8 @@ ConvArgs conv_args(const Shape &x, const float *weight, const float *bias, int s
     return a;
 }
 
-bool channels_ok(const Shape &x) { return (int64_t)x.H * x.d < (int64_t)1 << 28; }
+// What the kernels count in 32 bits: channels, and tokens a little past the last.
+bool counts_ok(const Shape &x) { return (int64_t)x.H * x.d < (int64_t)1 << 28 && x.N <= kMostTokens; }
 
 size_t cache_bytes(const Shape &x, int64_t entries, int taps) { return (size_t)entries * x.H * (taps - 1) * x.d * x.elem_bytes; }
 
@@ -67,7 +68,7 @@ extern "C" sv_status sv_causal_conv(const void *X, const sv_tensor_desc *x, cons
     if (silu < 0 || silu > 1) return SV_ERR_RANGE;
     if (!all_aligned({X, weight, bias, cache_in, cache_out, Y}) || !aligned4(lengths)) return SV_ERR_ALIGN;
     if (Y == X || (cache_in != cache_out && overlaps(cache_in, cache_out, cache_bytes(in, in.B, taps))) || cache_out == X || cache_out == Y) return SV_ERR_SHAPE;
-    if (!channels_ok(in)) return SV_ERR_SHAPE;
+    if (!counts_ok(in)) return SV_ERR_SHAPE;
     ConvArgs a = conv_args(in, weight, bias, silu, 16);
     a.x = X; a.y = Y; a.sy = out.st;
     a.lengths = lengths; a.cache_in = cache_in; a.cache_out = cache_out;
@@ -96,7 +97,7 @@ extern "C" sv_status sv_causal_conv_token(const void *X, const sv_tensor_desc *x
     if (in.N != 1 || n_slots <= 0 || (!slots && n_slots < in.B)) return SV_ERR_SHAPE;
     if (!all_aligned({X, weight, bias, cache_in, cache_out, Y}) || !aligned4(slots)) return SV_ERR_ALIGN;
     if (Y == X || (cache_in != cache_out && overlaps(cache_in, cache_out, cache_bytes(in, n_slots, taps))) || cache_out == X || cache_out == Y) return SV_ERR_SHAPE;
-    if (!channels_ok(in)) return SV_ERR_SHAPE;
+    if (!counts_ok(in)) return SV_ERR_SHAPE;
     ConvArgs a = conv_args(in, weight, bias, silu, 16);
     a.x = X; a.y = Y; a.sy = out.st;
     a.lengths = slots; a.n_slots = n_slots;
@@ -136,7 +137,7 @@ extern "C" sv_status sv_causal_conv_backward(const void *X, const sv_tensor_desc
     if (dX == X || dX == dY || overlaps(dcache_in, dcache_out, caches) || overlaps(dcache_in, cache_in, caches) || dcache_in == X || dcache_in == dY ||
         dcache_in == dX || (dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == bias))
         return SV_ERR_SHAPE;
-    if (!channels_ok(in)) return SV_ERR_SHAPE;
+    if (!counts_ok(in)) return SV_ERR_SHAPE;
     ConvArgs a = conv_args(in, weight, bias, silu, 4 * in.elem_bytes);
     const ConvCut cut = conv_cut(in.B, in.N, a.pieces.extent);
     const int64_t channels = (int64_t)in.H * in.d, floats = channels * (taps + 1);

@@ -30,7 +30,7 @@ namespace {
 
 using namespace sv;
 
-constexpr int kVersion = 500;   // 0.5.0
+constexpr int kVersion = 600;   // 0.6.0
 
 // Tuned launch shapes of the bf16 MFMA kernels (one workgroup per compute unit).
 // DP = 64 serves d = 64; DP = 128 serves d = 112 and 128.  Depths are tiles in

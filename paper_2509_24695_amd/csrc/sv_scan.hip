@@ -32,7 +32,7 @@ sv_status check_tensors(const sv_tensor_desc *u, const void *Z, const sv_tensor_
     rc = check_rows(bc, sbc);
     if (rc != SV_OK) return rc;
     if (sbc->B != su->B || sbc->N != su->N || sbc->bf16 != su->bf16 || su->H % sbc->H) return SV_ERR_SHAPE;
-    if ((int64_t)su->H * su->d >= (int64_t)1 << 27) return SV_ERR_SHAPE;
+    if ((int64_t)su->H * su->d >= (int64_t)1 << 27 || su->N > kMostTokens) return SV_ERR_SHAPE;
     return SV_OK;
 }
 
@@ -155,12 +155,16 @@ extern "C" sv_status sv_selective_scan_token(const void *U, const void *DT, cons
     if (Y == U || Y == DT || Y == Z || Y == Bm || Y == Cm || (S_in != S_out && overlaps(S_in, S_out, state_bytes(su, n_slots, n)))) return SV_ERR_SHAPE;
     ScanTokenArgs a{U, DT, Z, Bm, Cm, Y, su.st, sz.st, sbc.st, sy.st, A, dt_bias, skip, slots, S_in, S_out, n_slots, su.d, su.H * su.d,
                     su.H / sbc.H * su.d, 0};
-    constexpr int kTokenThreads = 256;
+    constexpr int kTokenThreads = 256, kFewTokens = 2048;             // workgroups of one unit
     const int per = kTokenThreads / (n / 4);
-    a.tiles = (a.channels + per - 1) / per;
+    const bool few = (int64_t)su.B * ((a.channels + per - 1) / per) <= kFewTokens;
+    a.tiles = few ? (a.channels + per - 1) / per : (a.channels + 2 * per - 1) / (2 * per);
     if (!grid_ok((int64_t)su.B * a.tiles, kTokenThreads)) return SV_ERR_SHAPE;
+    const unsigned grid = (unsigned)((int64_t)su.B * a.tiles);
+    const auto hs = static_cast<hipStream_t>(stream);
     with_scan(su.bf16, n, Z != nullptr, [&](auto t, auto k, auto gate) {
-        scan_token<decltype(t), k(), gate()><<<(unsigned)((int64_t)su.B * a.tiles), kTokenThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+        if (few) scan_token<decltype(t), k(), gate(), 1><<<grid, kTokenThreads, 0, hs>>>(a);
+        else scan_token<decltype(t), k(), gate(), 2><<<grid, kTokenThreads, 0, hs>>>(a);
     });
     return launched();
 }
@@ -193,8 +197,8 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     const ScanBackwardSpace space = scan_backward_space(a.B, a.G, a.channels, a.N, n, (int64_t)a.B * a.segments);
     if (workspace_bytes < (size_t)space.total * sizeof(float)) return SV_ERR_WORKSPACE;
     const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = 2 * (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
-    const int64_t shared = ((int64_t)a.B * a.G * a.N * 2 * n + 255) / 256, params = ((int64_t)a.channels * (n + 2) + 255) / 256;
-    if (!grid_ok(2 * scan_grid(waves), kScanWave) || !grid_ok(states, 1024) || !grid_ok(shared, 256) || !grid_ok(params, 256)) return SV_ERR_SHAPE;
+    const int64_t shared = ((int64_t)a.B * a.G * a.N * 2 * n + 255) / 256, params = dA || ddt_bias || dskip ? ((int64_t)a.channels * (n + 2) + 255) / 256 : 0;
+    if (!grid_ok(2 * scan_grid(waves), kScanWave) || !grid_ok(states, 1024) || !grid_ok(shared + params, 256)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.dy = dY;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.ds_out = dS_out;
@@ -220,9 +224,7 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
         }
         scan_back_walk<T, k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
-        scan_back_shared<T, k()><<<(unsigned)shared, 256, 0, hs>>>(a);
-        if ((done = launched()) != SV_OK) return;
-        if (a.dA || a.ddt_bias || a.dskip) scan_back_params<k()><<<(unsigned)params, 256, 0, hs>>>(a);
+        scan_back_fold<T, k()><<<(unsigned)(shared + params), 256, 0, hs>>>(a, (uint32_t)shared);
         done = launched();
     });
     return done;

@@ -142,7 +142,8 @@ def test_backward_of_the_state_in_place():
 
 @pytest.mark.parametrize("rows,pool,H,d,G,n,gate,dtype,elsewhere", [
     (1, 1, 1, 8, 1, 16, True, "bf16", False), (5, 9, 4, 36, 2, 8, False, "f32", True), (12, 12, 2, 112, 2, 16, True, "bf16", True),
-    (6, 8, 1, 2240, 1, 16, True, "bf16", False), (3, 5, 1, 8192, 1, 8, False, "f32", True), (5, 6, 5, 64, 5, 16, True, "f32", False)])
+    (6, 8, 1, 2240, 1, 16, True, "bf16", False), (3, 5, 1, 8192, 1, 8, False, "f32", True), (5, 6, 5, 64, 5, 16, True, "f32", False),
+    (70, 80, 1, 2240, 1, 16, True, "bf16", True), (130, 140, 2, 1100, 2, 8, False, "f32", False)])
 def test_token(rows, pool, H, d, G, n, gate, dtype, elsewhere):
     import torch
     say(f"scan token {rows} of {pool} {H}x{d} G{G} n{n} {dtype}")

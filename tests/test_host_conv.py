@@ -69,7 +69,8 @@ def test_forward():
         assert _forward(Y=A[9], silu=act) == 5
     assert _forward(Y=A[0]) == 2                                      # in place
     assert _forward(Y=A[9], co=A[3] + 16) == 2 and _forward(Y=A[9], co=A[9]) == 2 and _forward(Y=A[9], co=A[0]) == 2
-    n = (1 << 31) - 1
+    n = (1 << 31) - 1                                                 # tokens are counted a little past the last
+    assert _forward(Y=A[9], **{k: _desc(H=1, N=n, d=8, stride_n=8, stride_h=8 * n, stride_b=8 * n) for k in ("x", "y")}) == 2
     assert _forward(Y=A[9], **{k: _desc(H=1, N=n, d=2048, stride_n=2048, stride_h=n * 2048, stride_b=n * 2048) for k in ("x", "y")}) == 2
     assert _forward(Y=A[9], **{k: _desc(H=1 << 20, N=1, d=4096, stride_n=4096, stride_h=4096, stride_b=1 << 40) for k in ("x", "y")}) == 2
 

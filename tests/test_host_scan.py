@@ -87,6 +87,11 @@ def test_forward(route):
         assert _forward(Y=A[same]) == 2
     assert _forward(Y=A[30], so=A[8] + 16) == 2
     assert _forward(Y=A[30], wb=64) == 6
+    n = (1 << 31) - 1                                                 # tokens are counted a little past the last
+    long = {k: _desc(H=1, N=n, d=8, stride_n=8, stride_h=8 * n, stride_b=8 * n) for k in ("u", "z", "y")}
+    assert _forward(Y=A[30], bc=_bc(N=n, stride_h=16 * n, stride_b=16 * n), **long) == 2
+    wide = {k: _desc(H=1 << 16, d=4096, stride_n=4096, stride_h=128 * 4096, stride_b=1 << 40) for k in ("u", "z", "y")}
+    assert _forward(Y=A[30], **wide) == 2
 
 
 def test_token(route):
