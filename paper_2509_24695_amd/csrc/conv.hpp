@@ -3,8 +3,11 @@
 //   a_t = bias + sum_j W[j] x_{t-(K-1)+j},  y = a or silu(a);   da = dy or dy silu'(a)
 //   dx_t = sum_j W[j] da_{t+(K-1)-j},  dW[j] = sum da_t x_{t-(K-1)+j},  db = sum da_t
 //
-// Bound by memory: a thread owns one 16-byte piece of the channels, whose taps it keeps in registers, and walks a run of tokens with the last
-// K-1 of them in registers too, so that a token is read once (and K-1 more times at the runs' edges, out of the caches).
+// A thread owns a piece of the channels, whose taps it keeps in registers, and walks a run of tokens with the last K-1 of them in registers too, so
+// that a token is read once (and K-1 more times at the runs' edges, out of the caches).  Forwards bound by memory: 32 760 tokens of 2 240 channels bf16
+// 58 us (294 MB, 5.0 TB/s; a copy 56).  Backwards a thread has four channels of either type (with eight, 256 registers and one wave on a SIMD, the call
+// below took 174 us), and the vector unit is as busy as the memory: some 30 instructions a value, 62 of the kernel's 80 us for 2 x 20 heads of
+// 14 040 and 9 360 tokens of 112 (315 MB, 3.9 TB/s), and 5 us for the fold of the partial sums.
 #pragma once
 
 #include "activation.hpp"

@@ -7,7 +7,8 @@
 
 namespace sv {
 
-// Forwards a thread owns one 16-byte piece of the channels and walks a run of tokens; threads are numbered pieces first, then runs.
+// Forwards a thread owns one 16-byte piece of the channels and walks a run of tokens; threads are numbered pieces first, then runs.  Sixteen tokens where that
+// makes 1 024 threads a compute unit (32 760 tokens of 2 240 channels bf16 58.6 us, runs of 8 60.2, of 32 62.5), fewer in smaller calls.
 constexpr int kConvThreads = 256;
 inline int conv_run(int64_t BN, int pieces)
 {
@@ -17,7 +18,8 @@ inline int conv_run(int64_t BN, int pieces)
 }
 
 // Backwards a workgroup is `across` pieces (at most 32, as many in every tile) by `down` runs of tokens, so that one partial sum of the parameters' gradients is left for all
-// of its runs.
+// of its runs.  Runs as long as 2 048 workgroups allow (2 x 20 heads of up to 14 040 tokens of 112 80 us, with 1 024 88, with 4 096 86), of eight tokens at least (2 799 x 3
+// tokens of 672 channels fp32 17 us, with four 26).
 struct ConvCut {
     int across, down, run;             // run: tokens of a thread
     int64_t tiles, blocks;             // workgroups across the channels; workgroups along one sequence

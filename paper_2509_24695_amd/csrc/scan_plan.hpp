@@ -4,13 +4,11 @@
 
 #include <stdint.h>
 
-#include "tile_walk.hpp"
-
 namespace sv {
 
 constexpr int kScanWave = 64;               // channels of a wave
 constexpr int kScanRun = 4;                 // tokens whose states the backward pass holds at once: segments are multiples of it
-constexpr int kScanShortest = 8;            // tokens of a segment, where there is more than one
+constexpr int kScanShortest = 8;            // tokens of a segment, where there is more than one (64 tokens of 2 240 channels 16 us, with 32 33; backwards 33 and 70)
 
 // A sequence is walked by `segments` waves per channel block, `per_segment` tokens each (the last fewer).
 struct ScanPlan {
@@ -56,12 +54,6 @@ inline int64_t scan_slots(int64_t B, int64_t n_tokens, int64_t channels, int64_t
     const int64_t most = B * scan_longest_chain(n_tokens), full = 2 * waves / blocks > B ? 2 * waves / blocks : B;
     return most < full ? most : full;
 }
-
-// Workgroup ids go round the dies (one L2 each); a die takes a run of neighbouring tasks, so that the waves of a segment, which read the same B and C,
-// find them in one L2.  For ids below 8 ceil(tasks / 8); a task of `tasks` or more is none.
-constexpr int kScanDies = 8;
-inline int64_t scan_grid(int64_t tasks) { return (tasks + kScanDies - 1) / kScanDies * kScanDies; }
-SV_HOST_DEVICE inline uint32_t scan_task(uint32_t id, uint32_t grid) { return id % kScanDies * (grid / kScanDies) + id / kScanDies; }
 
 // Floats of the backward pass's workspace, part by part.
 struct ScanBackwardSpace {

@@ -89,7 +89,7 @@ unsigned held_args(GroupArgs &a, const HeldForm &form, int elem_bytes)
     a.across = form.across;
     a.lines = form.lines;
     a.whole_lines = a.whole_lines && a.width * elem_bytes % 128 == 0;
-    const int64_t grid = scan_grid(a.BH * a.G);
+    const int64_t grid = held_grid(a.BH * a.G);
     return grid_ok(grid, kHeldThreads) ? (unsigned)grid : 0;
 }
 

@@ -77,6 +77,7 @@ template <typename F> void with_span(int segments, F &&f)
     else if (segments <= 32) f(four, std::integral_constant<int, 8>{});
     else if (segments <= 64) f(sixteen, four);
     else if (segments <= 128) f(sixteen, std::integral_constant<int, 8>{});
+    else if (segments <= 256) f(sixteen, sixteen);
     else f(sixteen, std::integral_constant<int, 32>{});
 }
 static_assert(kScanMostSegments <= 16 * 32, "segments of a sequence");
@@ -119,7 +120,7 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
     const int64_t states = (int64_t)a.B * a.segments * a.channels * n, waves = (int64_t)a.B * a.segments * a.blocks;
     if (a.segments > 1 && workspace_bytes < (size_t)(states + states / n) * sizeof(float)) return SV_ERR_WORKSPACE;
     const int64_t scan = (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
-    if (!grid_ok(scan_grid(waves), kScanWave) || !grid_ok(scan, 1024)) return SV_ERR_SHAPE;
+    if (!grid_ok(waves, kScanWave) || !grid_ok(scan, 1024)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.y = Y;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.s_out = S_out;
@@ -129,12 +130,12 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
     sv_status done = SV_OK;
     with_scan(su.bf16, n, Z != nullptr, [&](auto t, auto k, auto gate) {
         if (a.segments > 1) {
-            scan_sums<decltype(t), k()><<<(unsigned)scan_grid(waves / a.segments * (a.segments - 1)), kScanWave, 0, hs>>>(a);
+            scan_sums<decltype(t), k()><<<(unsigned)(waves / a.segments * (a.segments - 1)), kScanWave, 0, hs>>>(a);
             if ((done = launched()) != SV_OK) return;
             with_span(a.segments, [&](auto runs, auto span) { scan_states<k(), runs(), span()><<<(unsigned)scan, 64 * runs(), 0, hs>>>(a); });
             if ((done = launched()) != SV_OK) return;
         }
-        scan_walk<decltype(t), k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);
+        scan_walk<decltype(t), k(), gate()><<<(unsigned)waves, kScanWave, 0, hs>>>(a);
         done = launched();
     });
     return done;
@@ -198,7 +199,7 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     if (workspace_bytes < (size_t)space.total * sizeof(float)) return SV_ERR_WORKSPACE;
     const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = 2 * (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
     const int64_t shared = ((int64_t)a.B * a.G * a.N * 2 * n + 255) / 256, params = dA || ddt_bias || dskip ? ((int64_t)a.channels * (n + 2) + 255) / 256 : 0;
-    if (!grid_ok(2 * scan_grid(waves), kScanWave) || !grid_ok(states, 1024) || !grid_ok(shared + params, 256)) return SV_ERR_SHAPE;
+    if (!grid_ok(2 * waves, kScanWave) || !grid_ok(states, 1024) || !grid_ok(shared + params, 256)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.dy = dY;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.ds_out = dS_out;
@@ -216,13 +217,13 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     sv_status done = SV_OK;
     with_scan(su.bf16, n, Z != nullptr, [&](auto t, auto k, auto gate) {
         using T = decltype(t);
-        scan_back_sums<T, k(), gate()><<<(unsigned)(2 * scan_grid(waves)), kScanWave, 0, hs>>>(a);
+        scan_back_sums<T, k(), gate()><<<(unsigned)(2 * waves), kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
         if (a.segments > 1) {
             with_span(a.segments, [&](auto runs, auto span) { scan_back_states<k(), runs(), span()><<<(unsigned)states, 64 * runs(), 0, hs>>>(a); });
             if ((done = launched()) != SV_OK) return;
         }
-        scan_back_walk<T, k(), gate()><<<(unsigned)scan_grid(waves), kScanWave, 0, hs>>>(a);
+        scan_back_walk<T, k(), gate()><<<(unsigned)waves, kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
         scan_back_fold<T, k()><<<(unsigned)(shared + params), 256, 0, hs>>>(a, (uint32_t)shared);
         done = launched();
