@@ -8,9 +8,10 @@
 // segment's first state has become by then, walks the run forwards with its states in registers, and then backwards.  The sums over channels (dB, dC)
 // go through the wave by exchanges that halve the number of values a lane holds with every step: 2 n values cost little more than 2 n additions.
 //
-// Bound by the vector unit: some 430 instructions a token and channel in scan_back_walk.  Runs of four tokens and decays worked out again keep a wave below 256
-// registers, so that two run on a SIMD (one alone reaches half of its rate): 2 x 4 680 tokens of 2 240 channels, n = 16, bf16 497 us, sums 160, states 11, walk 350, fold 11;
-// with runs of eight the walk took 545.
+// Bound by the vector unit: some 390 instructions a token and channel in scan_back_walk.  Runs of four tokens, with their decays (and what the segment begins
+// from) in LDS, 20 KB a wave, keep a wave below 256 registers, so that two run on a SIMD (one alone reaches half of its rate).  The next run's numbers and mark
+// are on their way during a run's first token, which comes last.  2 x 4 680 tokens of 2 240 channels, n = 16, bf16: 495 us, sums 173, states 12, walk 323, fold 12;
+// with decays worked out again and marks fetched when they were needed the walk took 358 (520 in all), with runs of eight tokens and one wave 545.
 #pragma once
 
 #include "scan.hpp"
@@ -120,22 +121,29 @@ template <int n> __device__ __forceinline__ int wave_value(int lane)
 
 template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 2) void scan_back_walk(ScanArgs a)
 {
+    __shared__ f32x4 decays[kScanRun][n / 4][kScanWave], begins[n / 4][kScanWave];
     const ScanPlace at(a, blockIdx.x);
     const int lane = threadIdx.x;
-    float *params = a.params + at.slot(a) * (n + 2) * a.channels + at.channel;
-    if (at.first >= at.length && at.segment > 0) {
-        if (at.mine)
+    auto store_params = [&](const float (&dA)[n], float dbias, float dskip) {
+        int channel = at.channel;                                     // (the address is worked out here: kept since the start it would take registers)
+        asm volatile("" : "+v"(channel));
+        float *params = a.params + at.slot(a) * (n + 2) * a.channels + channel;
 #pragma unroll
-            for (int i = 0; i < n + 2; ++i) params[(int64_t)i * a.channels] = 0.f;
+        for (int i = 0; i < n; ++i) params[(int64_t)i * a.channels] = dA[i];
+        params[(int64_t)n * a.channels] = dbias;
+        params[(int64_t)(n + 1) * a.channels] = dskip;
+    };
+    if (at.first >= at.length && at.segment > 0) {
+        const float none[n] = {};
+        if (at.mine) store_params(none, 0.f, 0.f);
         return;
     }
     float A2[n], begin[n], g[n], dA[n], dbias = 0.f, dskip = 0.f;
     load_rates<n>(a, at.channel, A2);
     const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f, skip = a.skip ? a.skip[at.channel] : 0.f;
-    const int64_t row = (int64_t)at.b * a.channels + at.channel;
     if (a.segments == 1) {
-        load_state<n>(a.s_in, row, begin);
-        load_state<n>(a.ds_out, row, g);
+        load_state<n>(a.s_in, (int64_t)at.b * a.channels + at.channel, begin);
+        load_state<n>(a.ds_out, (int64_t)at.b * a.channels + at.channel, g);
     } else {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
@@ -143,6 +151,8 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
             g[i] = a.grads[(at.slot(a) * n + i) * a.channels + at.channel];
         }
     }
+#pragma unroll
+    for (int q = 0; q < n / 4; ++q) begins[q][lane] = f32x4{begin[4 * q], begin[4 * q + 1], begin[4 * q + 2], begin[4 * q + 3]};
 #pragma unroll
     for (int i = 0; i < n; ++i) dA[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
@@ -163,20 +173,23 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
         nC.load(a.cm, bc + t * a.sbc.n);
         __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
     };
+    float mark[n], mark_steps;
+    auto request_mark = [&](int t0) {
+        const int64_t m = (int64_t)at.b * a.runs + t0 / kScanRun;
+        mark_steps = a.mark_steps[m * a.channels + at.channel];
+#pragma unroll
+        for (int i = 0; i < n; ++i) mark[i] = a.marks[(m * n + i) * a.channels + at.channel];
+    };
     auto run = [&](int t0, int count, auto whole) {
         const Ahead<T, kScanRun> u0 = u, dt0 = dt, z0 = z, dy0 = dy;
         const bool more = t0 > at.first;
         float h[kScanRun + 1][n], D[kScanRun], slope[kScanRun], raw[kScanRun];
         if (more) {
-            const int64_t mark = (int64_t)at.b * a.runs + t0 / kScanRun;
-            const float steps = a.mark_steps[mark * a.channels + at.channel];
 #pragma unroll
-            for (int i = 0; i < n; ++i) h[0][i] = a.marks[(mark * n + i) * a.channels + at.channel];
-#pragma unroll
-            for (int i = 0; i < n; ++i) h[0][i] = __builtin_fmaf(kept(A2[i], steps), begin[i], h[0][i]);
+            for (int i = 0; i < n; ++i) h[0][i] = __builtin_fmaf(kept(A2[i], mark_steps), begins[i / 4][lane][i % 4], mark[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < n; ++i) h[0][i] = begin[i];
+            for (int i = 0; i < n; ++i) h[0][i] = begins[i / 4][lane][i % 4];
         }
 #pragma unroll
         for (int k = 0; k < kScanRun; ++k) {
@@ -189,14 +202,24 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
             const float x = D[k] * u0[k];
             raw[k] = skip * u0[k];
 #pragma unroll
-            for (int i = 0; i < n; ++i) {
-                h[k + 1][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D[k] * A2[i]), h[k][i], x * B[i]);
-                if (GATE) raw[k] = __builtin_fmaf(C[i], h[k + 1][i], raw[k]);
+            for (int q = 0; q < n / 4; ++q) {
+                f32x4 decay;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 4 * q + e;
+                    decay[e] = __builtin_amdgcn_exp2f(D[k] * A2[i]);
+                    h[k + 1][i] = __builtin_fmaf(decay[e], h[k][i], x * B[i]);
+                    if (GATE) raw[k] = __builtin_fmaf(C[i], h[k + 1][i], raw[k]);
+                }
+                decays[k][q][lane] = decay;
             }
         }
 #pragma unroll
         for (int k = kScanRun - 1; k >= 0; --k) {
-            if (k == kScanRun - 2 && more) request(t0 - kScanRun);    // (the last token's state is no longer needed: its registers do)
+            if (k == 0 && more) {                                     // (the later tokens' states are no longer needed: their registers do)
+                request(t0 - kScanRun);
+                if (t0 - kScanRun > at.first) request_mark(t0 - kScanRun);
+            }
             if (!whole() && k >= count) continue;
             const int t = t0 + k;
             Scalars<T, n> B = nB, C = nC;
@@ -209,18 +232,19 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
                 if (at.mine) Elem<T>::store(static_cast<T *>(a.dz) + at.z + t * a.sz.n, v * raw[k] * silu_slope(z0[k], s));
                 v *= z0[k] * s;
             }
-            // the decays are worked out again: kept from the way forwards they would take registers from a second wave
-            asm volatile("" : "+v"(D[k]));
             // lanes that double a channel add nothing to the sums over channels
             v = at.mine ? v : 0.f;
             const float x = at.mine ? D[k] * u0[k] : 0.f;
             float sums[n], e = 0.f, along = 0.f;
+            f32x4 decay[n / 4];
+#pragma unroll
+            for (int q = 0; q < n / 4; ++q) decay[q] = decays[k][q][lane];
 #pragma unroll
             for (int i = 0; i < n; ++i) {
                 g[i] = __builtin_fmaf(C[i], v, g[i]);
                 sums[i] = wave_both(g[i] * x, v * h[k + 1][i]);
                 e = __builtin_fmaf(g[i], B[i], e);
-                g[i] *= __builtin_amdgcn_exp2f(D[k] * A2[i]);
+                g[i] *= decay[i / 4][i % 4];
                 const float p = g[i] * h[k][i];
                 dA[i] = __builtin_fmaf(D[k], p, dA[i]);
                 along = __builtin_fmaf(A2[i], p, along);
@@ -238,17 +262,19 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
     };
     if (runs) {
         int t0 = at.first + (runs - 1) * kScanRun;
+        if (t0 > at.first) request_mark(t0);
         request(t0);
         request_scalars(t0);
         run(t0, at.last - t0, std::false_type{});
         for (t0 -= kScanRun; t0 >= at.first; t0 -= kScanRun) run(t0, kScanRun, std::true_type{});
     }
     if (!at.mine) return;
-#pragma unroll
-    for (int i = 0; i < n; ++i) params[(int64_t)i * a.channels] = dA[i];
-    params[(int64_t)n * a.channels] = dbias;
-    params[(int64_t)(n + 1) * a.channels] = dskip;
-    if (a.ds_in && at.segment == 0) store_state<n>(a.ds_in, row, g);
+    store_params(dA, dbias, dskip);
+    if (a.ds_in && at.segment == 0) {
+        int channel = at.channel;
+        asm volatile("" : "+v"(channel));
+        store_state<n>(a.ds_in, (int64_t)at.b * a.channels + channel, g);
+    }
 }
 
 // dB and dC: the blocks' sums over their channels, added up in order and rounded.  Behind these workgroups (`shared` of them) dA, ddt_bias and dskip:
