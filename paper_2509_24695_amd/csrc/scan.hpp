@@ -6,7 +6,7 @@
 // by the vector unit: an exponential and four other instructions for each state, with softplus and the gate beside them.  A long sequence
 // is cut into segments that are walked side by side: scan_sums finds what each segment adds to a state of nothing and its sum of steps,
 // scan_states turns these into the states the segments begin from (what a segment keeps of its state is exp(A sum D)), and scan_walk
-// walks from there.  32 760 tokens of 2 240 channels, n = 16, with a gate, bf16: 513 us, the sums 250, the states 13, the walk 310 under the profiler's clock (590 MB;
+// walks from there.  32 760 tokens of 2 240 channels, n = 16, with a gate, bf16: 491 us, the sums 223, the states 26, the walk 302 under the profiler's clock (590 MB;
 // an exponential costs 2.2 instructions, the walk 117 instructions a value and token: at the rate that the vector unit reaches, 36 T a second, 182 and 280 us).  Decays that are
 // kept instead of worked out twice would be 64 bytes a value.
 #pragma once
@@ -124,7 +124,8 @@ template <int n> __device__ __forceinline__ void store_state(float *p, int64_t r
 }
 // What a run of tokens with steps that sum to `steps` keeps of a state number: past the largest fp32 number that number, so that a state of
 // nothing stays one.
-__device__ __forceinline__ float kept(float A2, float steps) { return fminf(__builtin_amdgcn_exp2f(A2 * steps), 3.40282347e38f); }
+constexpr float kMostKept = 3.40282347e38f;
+__device__ __forceinline__ float kept(float A2, float steps) { return fminf(__builtin_amdgcn_exp2f(A2 * steps), kMostKept); }
 
 // Numbers of AHEAD tokens on their way, as they lie in memory (a conversion here would wait for them).  Past the last token the last one
 // is read again: no branch stands between the loads.
@@ -139,37 +140,56 @@ template <typename T, int AHEAD> struct Ahead {
     __device__ __forceinline__ float operator[](int i) const { return Elem<T>::load(&raw[i]); }
 };
 
-// Tokens whose numbers are on their way: eight where a pass has little else in registers (backward sums of 2 x 4 680 tokens of 2 240 channels: the whole call
-// 508 us, with four 518; without a gate 437 and 466; the forward walk gains nothing).
+// Tokens whose numbers are on their way: eight in the backward sums, of which two waves run on a SIMD (2 x 4 680 tokens of 2 240 channels 151 us, with four 186; the
+// forward walk gains nothing).
 constexpr int kScanAhead = 4, kScanBackAhead = 8;
 
-// What the tokens of a segment add to a state of nothing, and the sum of their steps.  MARKS: the local state before each run too.
-template <typename T, int n, bool MARKS> __device__ __forceinline__ void scan_sum_forward(const ScanArgs &a, const ScanPlace &at)
+// What the tokens of a segment add to a state of nothing, and the sum of their steps.  MARKS: the local state before each run too.  GRADS: and what
+// they add to the gradient of the state that the segment begins from, sum_t C_t y'_t times the decays up to t.
+template <typename T, int n, bool MARKS, bool GRADS, bool GATE> __device__ __forceinline__ void scan_sum(const ScanArgs &a, const ScanPlace &at)
 {
     constexpr int kAhead = MARKS ? kScanBackAhead : kScanAhead;
-    float A2[n], h[n], steps = 0.f;
+    float A2[n], h[n], along[n], g[n], steps = 0.f;
     load_rates<n>(a, at.channel, A2);
     const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f;
 #pragma unroll
-    for (int i = 0; i < n; ++i) h[i] = 0.f;
+    for (int i = 0; i < n; ++i) {
+        h[i] = g[i] = 0.f;
+        along[i] = 1.f;
+    }
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
-    Ahead<T, kAhead> u, dt;
+    Ahead<T, kAhead> u, dt, dy, z;
     auto request = [&](int t) {
         u.request(a.u, at.u, a.su.n, t, at.last);
         dt.request(a.dt, at.u, a.su.n, t, at.last);
+        if (GRADS) dy.request(a.dy, at.y, a.sy.n, t, at.last);
+        if (GRADS && GATE) z.request(a.z, at.z, a.sz.n, t, at.last);
     };
     request(at.first);
-    Scalars<T, n> next;
-    next.load(a.bm, bc + at.first * a.sbc.n);
-    auto token = [&](int t, float ut, float dtt) {
-        Scalars<T, n> B = next;
+    Scalars<T, n> nB, nC;
+    auto request_scalars = [&](int t) {
+        nB.load(a.bm, bc + t * a.sbc.n);
+        if (GRADS) nC.load(a.cm, bc + t * a.sbc.n);
+    };
+    request_scalars(at.first);
+    auto token = [&](int t, float ut, float dtt, float v, float zt) {
+        Scalars<T, n> B = nB, C = nC;
         B.arrive();
-        next.load(a.bm, bc + (t + 1 < at.last ? t + 1 : t) * a.sbc.n);
+        if (GRADS) C.arrive();
+        request_scalars(t + 1 < at.last ? t + 1 : t);
         __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
         const float D = softplus(dtt + bias), x = D * ut;
         steps += D;
+        if (GRADS && GATE) v *= silu(zt);
 #pragma unroll
-        for (int i = 0; i < n; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(D * A2[i]), h[i], x * B[i]);
+        for (int i = 0; i < n; ++i) {
+            const float decay = __builtin_amdgcn_exp2f(D * A2[i]);
+            h[i] = __builtin_fmaf(decay, h[i], x * B[i]);
+            if (GRADS) {
+                along[i] = fminf(along[i] * decay, kMostKept);
+                g[i] = __builtin_fmaf(along[i], C[i] * v, g[i]);
+            }
+        }
     };
     auto mark = [&](int t) {
         if (!MARKS || t == at.first || t >= at.last || !at.mine) return;
@@ -180,22 +200,27 @@ template <typename T, int n, bool MARKS> __device__ __forceinline__ void scan_su
     };
     int t = at.first;
     for (; t + kAhead <= at.last; t += kAhead) {
-        const Ahead<T, kAhead> u0 = u, dt0 = dt;
+        const Ahead<T, kAhead> u0 = u, dt0 = dt, dy0 = dy, z0 = z;
         request(t + kAhead);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (k % kScanRun == 0) mark(t + k);
-            token(t + k, u0[k], dt0[k]);
+            token(t + k, u0[k], dt0[k], GRADS ? dy0[k] : 0.f, GRADS && GATE ? z0[k] : 0.f);
         }
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
         if (k % kScanRun == 0) mark(t + k);
-        if (t + k < at.last) token(t + k, u[k], dt[k]);
+        if (t + k < at.last) token(t + k, u[k], dt[k], GRADS ? dy[k] : 0.f, GRADS && GATE ? z[k] : 0.f);
     }
     if (!at.mine) return;
 #pragma unroll
-    for (int i = 0; i < n; ++i) a.states[(at.slot(a) * n + i) * a.channels + at.channel] = h[i];
+    for (int i = 0; i < n; ++i) {
+        a.states[(at.slot(a) * n + i) * a.channels + at.channel] = h[i];
+        // (where the decays were no numbers: the limit above has taken them for its own)
+        const float all = A2[i] * steps;
+        if (GRADS) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = all != all ? all : g[i];
+    }
     a.steps[at.slot(a) * a.channels + at.channel] = steps;
 }
 
@@ -205,7 +230,7 @@ template <typename T, int n> __global__ __launch_bounds__(kScanWave) void scan_s
     const uint32_t per_b = (uint32_t)a.blocks * (a.segments - 1), b = blockIdx.x / per_b;
     const ScanPlace at(a, b * (uint32_t)a.blocks * a.segments + (blockIdx.x - b * per_b));
     if (at.first >= at.length) return;
-    scan_sum_forward<T, n, false>(a, at);
+    scan_sum<T, n, false, false, false>(a, at);
 }
 
 // The states that the segments begin from, in place of what the segments before add; backwards (BACK) the gradients that arrive at their ends.

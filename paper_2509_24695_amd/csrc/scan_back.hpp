@@ -10,16 +10,21 @@
 //
 // Bound by the vector unit: some 390 instructions a token and channel in scan_back_walk.  Runs of four tokens, with their decays (and what the segment begins
 // from) in LDS, 20 KB a wave, keep a wave below 256 registers, so that two run on a SIMD (one alone reaches half of its rate).  The next run's numbers and mark
-// are on their way during a run's first token, which comes last.  2 x 4 680 tokens of 2 240 channels, n = 16, bf16: 495 us, sums 173, states 12, walk 323, fold 12;
-// with decays worked out again and marks fetched when they were needed the walk took 358 (520 in all), with runs of eight tokens and one wave 545.
+// are on their way during a run's first token, which comes last.  2 x 4 680 tokens of 2 240 channels, n = 16, bf16: 475 us, sums 151, states 12, walk 323, fold 12;
+// with decays worked out again and marks fetched when they were needed the walk took 358, with runs of eight tokens and one wave 545.
 #pragma once
 
 #include "scan.hpp"
 
 namespace sv {
 
-// g = C y' of a segment's tokens from its last on, carried to before its first: what the segment adds to the gradient of the state it began from.
-template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum_back(const ScanArgs &a, const ScanPlace &at)
+// A segment's two sums can be had in one walk forwards, with the decays and the softplus of both worked out once; the gradients' is then of the decays multiplied up.
+// It pays with a gate (2 x 4 680 tokens of 2 240 channels bf16 146 us, in a walk each 170; fp32 170 and 181) and at n = 8 (83 and 91 without a gate);
+// without one, n = 16, a walk each is as fast or faster (bf16 145 and 141, fp32, whose B and C take all scalar registers, 176 and 146).
+template <int n, bool GATE> constexpr bool kSumsTogether = GATE || n == 8;
+
+// g = C dy of a segment's tokens from its last on, carried to before its first: what the segment adds to the gradient of the state it began from.
+template <typename T, int n> __device__ __forceinline__ void scan_sum_back(const ScanArgs &a, const ScanPlace &at)
 {
     float A2[n], g[n];
     load_rates<n>(a, at.channel, A2);
@@ -28,37 +33,35 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
     for (int i = 0; i < n; ++i) g[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
     // tokens from the last: token k of the walk is last - 1 - k
-    Ahead<T, kScanBackAhead> dy, dt, z;
+    Ahead<T, kScanBackAhead> dy, dt;
     const int count = at.last - at.first;
     auto request = [&](int k) {
         const int64_t top = at.last - 1;
         dy.request(a.dy, at.y + top * a.sy.n, -a.sy.n, k, count);
         dt.request(a.dt, at.u + top * a.su.n, -a.su.n, k, count);
-        if (GATE) z.request(a.z, at.z + top * a.sz.n, -a.sz.n, k, count);
     };
     request(0);
     Scalars<T, n> next;
     next.load(a.cm, bc + (at.last - 1) * a.sbc.n);
-    auto token = [&](int k, float v, float dtt, float zt) {
+    auto token = [&](int k, float v, float dtt) {
         Scalars<T, n> C = next;
         C.arrive();
         next.load(a.cm, bc + (at.last - 1 - (k + 1 < count ? k + 1 : k)) * a.sbc.n);
         __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
         const float D = softplus(dtt + bias);
-        if (GATE) v *= silu(zt);
 #pragma unroll
         for (int i = 0; i < n; ++i) g[i] = __builtin_amdgcn_exp2f(D * A2[i]) * __builtin_fmaf(C[i], v, g[i]);
     };
     int k0 = 0;
     for (; k0 + kScanBackAhead <= count; k0 += kScanBackAhead) {
-        const Ahead<T, kScanBackAhead> dy0 = dy, dt0 = dt, z0 = z;
+        const Ahead<T, kScanBackAhead> dy0 = dy, dt0 = dt;
         request(k0 + kScanBackAhead);
 #pragma unroll
-        for (int k = 0; k < kScanBackAhead; ++k) token(k0 + k, dy0[k], dt0[k], GATE ? z0[k] : 0.f);
+        for (int k = 0; k < kScanBackAhead; ++k) token(k0 + k, dy0[k], dt0[k]);
     }
 #pragma unroll
     for (int k = 0; k < kScanBackAhead; ++k)
-        if (k0 + k < count) token(k0 + k, dy[k], dt[k], GATE ? z[k] : 0.f);
+        if (k0 + k < count) token(k0 + k, dy[k], dt[k]);
     if (!at.mine) return;
 #pragma unroll
     for (int i = 0; i < n; ++i) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = g[i];
@@ -66,12 +69,23 @@ template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum
 
 template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) void scan_back_sums(ScanArgs a)
 {
-    const uint32_t half = gridDim.x / 2;
-    const bool back = blockIdx.x >= half;
-    const ScanPlace at(a, back ? blockIdx.x - half : blockIdx.x);
-    if (at.first >= at.length) return;
-    if (!back) scan_sum_forward<T, n, true>(a, at);
-    else if (at.segment > 0) scan_sum_back<T, n, GATE>(a, at);
+    if constexpr (kSumsTogether<n, GATE>) {
+        const ScanPlace at(a, blockIdx.x);
+        if (at.first < at.length) scan_sum<T, n, true, true, GATE>(a, at);
+    } else {
+        const uint32_t half = gridDim.x / 2;
+        const bool back = blockIdx.x >= half;
+        const ScanPlace at(a, back ? blockIdx.x - half : blockIdx.x);
+        if (at.first >= at.length) return;
+        if (!back) scan_sum<T, n, true, false, false>(a, at);
+        else if (at.segment > 0) scan_sum_back<T, n>(a, at);
+    }
+}
+// A sequence of one segment: the marks alone.
+template <typename T, int n> __global__ __launch_bounds__(kScanWave) void scan_back_marks(ScanArgs a)
+{
+    const ScanPlace at(a, blockIdx.x);
+    if (at.first < at.length) scan_sum<T, n, true, false, false>(a, at);
 }
 
 template <int n, int RUNS, int SPAN> __global__ __launch_bounds__(64 * RUNS) void scan_back_states(ScanArgs a)

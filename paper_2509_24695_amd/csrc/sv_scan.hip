@@ -217,7 +217,8 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     sv_status done = SV_OK;
     with_scan(su.bf16, n, Z != nullptr, [&](auto t, auto k, auto gate) {
         using T = decltype(t);
-        scan_back_sums<T, k(), gate()><<<(unsigned)(2 * waves), kScanWave, 0, hs>>>(a);
+        if (a.segments > 1) scan_back_sums<T, k(), gate()><<<(unsigned)(kSumsTogether<k(), gate()> ? waves : 2 * waves), kScanWave, 0, hs>>>(a);
+        else scan_back_marks<T, k()><<<(unsigned)waves, kScanWave, 0, hs>>>(a);
         if ((done = launched()) != SV_OK) return;
         if (a.segments > 1) {
             with_span(a.segments, [&](auto runs, auto span) { scan_back_states<k(), runs(), span()><<<(unsigned)states, 64 * runs(), 0, hs>>>(a); });

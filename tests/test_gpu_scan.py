@@ -243,6 +243,30 @@ def test_nonfinite_tokens_leave_earlier_outputs_alone(value):
     same_bits(g.all["dC"][:, :, 151:], bad.all["dC"][:, :, 151:])
 
 
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("behind", [True, False])
+def test_a_step_that_is_no_number(gate, behind):
+    """Token 150 of one channel: no gradient comes back through it, also none of zero, and the later ones are what they were."""
+    c = (1, 1, 300, 64, 1, 16, gate, "f32", "bhnd", None, True)
+    x = _inputs(c)
+    dy = draw(20, (1, 1, 300, 64), "f32")
+    if not behind:
+        dy[:, :, 150:] = 0
+    good, bad = _Grads(x, 1, 1, 64, 16), _Grads(x, 1, 1, 64, 16)
+    _backward(c, x, dy, None, good.args())
+    x[1][0, 0, 150, 5] = float("nan")
+    _backward(c, x, dy, None, bad.args())
+    others = [i for i in range(64) if i != 5]
+    for k in ("du", "ddt"):
+        assert np.isnan(f64(bad.all[k])[0, 0, :150, 5]).all()
+        same_bits(good.all[k][..., others], bad.all[k][..., others])
+    same_bits(good.all["du"][:, :, 151:], bad.all["du"][:, :, 151:])
+    if gate:
+        same_bits(good.all["dz"][:, :, :150], bad.all["dz"][:, :, :150])
+    assert np.isnan(f64(bad.all["ds_in"])[0, 0, 5]).all()
+    same_bits(good.all["ds_in"][:, :, others], bad.all["ds_in"][:, :, others])
+
+
 def test_captured_and_replayed():
     import torch
     c = (3, 2, 290, 48, 1, 16, True, "bf16", "bnhd", [290, 17, 0], True)
