@@ -5,7 +5,7 @@
 //
 // Bound by memory, twice over: a pass for the sums and one for the rows (a copy is as slow out of the cache behind the L2s as out of memory).  21 frames of
 // 1 560 rows of 2 240 channels in 32 groups bf16 85 us, 31 for the sums (4.8 TB/s) and 50 for the rows (5.9 TB/s; a reading and a copying pass 80); backwards 14 040 rows
-// 64 us, 28 for the sums (4.5 TB/s), 5 for the fold and 32 (5.9 TB/s).  A thread keeps the same eight (fp32: four)
+// 62 us, 26 for the sums (4.8 TB/s), 5 for the fold and 32 (5.9 TB/s).  A thread keeps the same eight (fp32: four)
 // channels for all of its rows, so groups need not be whole pieces: sums are kept by channel, and group_fold adds up a group's channels and chunks.
 // Forwards the sums of x and x^2 are fp64, in which products of tensor values are exact: no cancellation shows for any mean that
 // fp32 rows can have.
@@ -83,16 +83,18 @@ template <int N> __device__ __forceinline__ void of_channel(const float *p, int 
     for (int e = 0; e < N; ++e) x[e] = p ? p[c + e] : otherwise;
 }
 
-// Walks a thread's rows, kGroupAhead at a time, the next ones on their way: f(row, pieces of x and (BOTH) dy).
+// Walks a thread's rows, kAhead at a time, the next ones on their way: f(row, pieces of x and (BOTH) dy).  Two of both, which leave room for more waves (backwards, 14 040
+// rows of 2 240 channels 68.1 us on buffers in turn; four 71, one 72; 21 frames of 1 560 rows 134, 136 and 160).
 template <typename T, typename P, bool BOTH, typename F> __device__ __forceinline__ void group_walk(const GroupArgs &a, const GroupPlace<T, P> &at, F &&f)
 {
     typedef typename P::V V;
+    constexpr int kAhead = BOTH ? kGroupAhead / 2 : kGroupAhead;
     const T *x = at.at(a, a.x, a.sx), *dy = BOTH ? at.at(a, a.dy, a.sdy) : nullptr;
-    V nx[kGroupAhead], ndy[kGroupAhead];
+    V nx[kAhead], ndy[kAhead];
     // past the last row the last one is read again: no branch stands between the loads
     auto request = [&](int64_t row) {
 #pragma unroll
-        for (int i = 0; i < kGroupAhead; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
             const int64_t r = row + i * at.down < at.last ? row + i * at.down : at.last - 1;
             nx[i] = *reinterpret_cast<const V *>(x + r * a.sx.n);
             if (BOTH) ndy[i] = *reinterpret_cast<const V *>(dy + r * a.sdy.n);
@@ -100,19 +102,19 @@ template <typename T, typename P, bool BOTH, typename F> __device__ __forceinlin
     };
     request(at.first + at.line);
     int64_t row = at.first + at.line;
-    for (; row + (kGroupAhead - 1) * at.down < at.last; row += kGroupAhead * at.down) {
-        V vx[kGroupAhead], vdy[kGroupAhead];
+    for (; row + (kAhead - 1) * at.down < at.last; row += kAhead * at.down) {
+        V vx[kAhead], vdy[kAhead];
 #pragma unroll
-        for (int i = 0; i < kGroupAhead; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
             vx[i] = nx[i];
             if (BOTH) vdy[i] = ndy[i];
         }
-        request(row + kGroupAhead * at.down);
+        request(row + kAhead * at.down);
 #pragma unroll
-        for (int i = 0; i < kGroupAhead; ++i) f(row + i * at.down, vx[i], vdy[i]);
+        for (int i = 0; i < kAhead; ++i) f(row + i * at.down, vx[i], vdy[i]);
     }
 #pragma unroll
-    for (int i = 0; i < kGroupAhead; ++i)
+    for (int i = 0; i < kAhead; ++i)
         if (row + i * at.down < at.last) f(row + i * at.down, nx[i], ndy[i]);
 }
 
