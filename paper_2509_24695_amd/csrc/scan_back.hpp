@@ -10,7 +10,7 @@
 //
 // Bound by the vector unit: some 390 instructions a token and channel in scan_back_walk.  Runs of four tokens, with their decays (and what the segment begins
 // from) in LDS, 20 KB a wave, keep a wave below 256 registers, so that two run on a SIMD (one alone reaches half of its rate).  The next run's numbers and mark
-// are on their way during a run's first token, which comes last.  2 x 4 680 tokens of 2 240 channels, n = 16, bf16: 475 us, sums 151, states 12, walk 323, fold 12;
+// are on their way during a run's first token, which comes last.  2 x 4 680 tokens of 2 240 channels, n = 16, bf16: 467 to 475 us, sums 151, states 12, walk 323 to 334, fold 12;
 // with decays worked out again and marks fetched when they were needed the walk took 358, with runs of eight tokens and one wave 545.
 #pragma once
 
