@@ -26,7 +26,8 @@
  *    and dtype, strides of their own.  d is any multiple of 8 (SV_BF16) or 4 (SV_F32) up to 8192.
  *  - `bc` describes Bm and Cm (and dB, dC) as [B][G][N][n] of the same dtype: its H is G, a divisor of u's H, its d is n.
  *  - A is fp32 [H][d][n], dt_bias and skip fp32 [H][d], each of the two or NULL (zeros).  A must be numbers and is meant negative (decays); where it is
- *    positive D A of a token must stay below 88 (the range of fp32's exp).
+ *    positive D A of a token must stay below 88 (the range of fp32's exp).  Over a run of tokens a state may grow or decay by any factor, as long as the states, and
+ *    what the tokens of any run add to a state of nothing, are in fp32's range themselves; and so for gradients, from the end.
  *  - lengths is int32 [B] or NULL: sequence b has the tokens [0, lengths[b]) of its row (values are held to [0, N]); NULL: N each.  Rows
  *    behind a sequence's last token are neither read nor written.  A sequence of length zero has S_out = S_in.
  *  - States are dense fp32 [B][H][d][n] (in the pool of sv_selective_scan_token [n_slots][H][d][n]).

@@ -122,10 +122,22 @@ template <int n> __device__ __forceinline__ void store_state(float *p, int64_t r
 #pragma unroll
     for (int q = 0; q < n / 4; ++q) *reinterpret_cast<f32x4 *>(p + row * n + 4 * q) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
 }
-// What a run of tokens with steps that sum to `steps` keeps of a state number: past the largest fp32 number that number, so that a state of
-// nothing stays one.
-constexpr float kMostKept = 3.40282347e38f;
-__device__ __forceinline__ float kept(float A2, float steps) { return fminf(__builtin_amdgcn_exp2f(A2 * steps), kMostKept); }
+// What a run of tokens whose steps sum to `steps` makes of a state number s, with what the run adds: exp(A steps) s + add.  The exponential may be far outside of
+// fp32's range where its product with s is not (a state of 1e-30 that grows, one of 1e30 that decays, one of nothing that stays so): what its exponent has
+// past 125 goes into that of s.
+__device__ __forceinline__ float carried(float A2, float steps, float s, float add)
+{
+    const float x = __builtin_amdgcn_fmed3f(A2 * steps, -1000.f, 1000.f), past = __builtin_rintf(x - __builtin_amdgcn_fmed3f(x, -125.f, 125.f));
+    return __builtin_fmaf(__builtin_amdgcn_exp2f(x - past), __builtin_amdgcn_ldexpf(s, (int)past), add);
+}
+// Has a lane of the wave a state number that grows (A > 0)?
+template <int n> __device__ __forceinline__ bool wave_grows(const float (&A2)[n])
+{
+    bool grows = false;
+#pragma unroll
+    for (int i = 0; i < n; ++i) grows |= A2[i] > 0.f;
+    return __any(grows);
+}
 
 // Numbers of AHEAD tokens on their way, as they lie in memory (a conversion here would wait for them).  Past the last token the last one
 // is read again: no branch stands between the loads.
@@ -145,7 +157,8 @@ template <typename T, int AHEAD> struct Ahead {
 constexpr int kScanAhead = 4, kScanBackAhead = 8;
 
 // What the tokens of a segment add to a state of nothing, and the sum of their steps.  MARKS: the local state before each run too.  GRADS: and what
-// they add to the gradient of the state that the segment begins from, sum_t C_t y'_t times the decays up to t.
+// they add to the gradient of the state that the segment begins from, sum_t C_t y'_t times the decays up to t (for A <= 0: the product of the decays then stays in
+// range but for what is less than 2^-126 of C_t y'_t).
 template <typename T, int n, bool MARKS, bool GRADS, bool GATE> __device__ __forceinline__ void scan_sum(const ScanArgs &a, const ScanPlace &at)
 {
     constexpr int kAhead = MARKS ? kScanBackAhead : kScanAhead;
@@ -186,7 +199,7 @@ template <typename T, int n, bool MARKS, bool GRADS, bool GATE> __device__ __for
             const float decay = __builtin_amdgcn_exp2f(D * A2[i]);
             h[i] = __builtin_fmaf(decay, h[i], x * B[i]);
             if (GRADS) {
-                along[i] = fminf(along[i] * decay, kMostKept);
+                along[i] *= decay;
                 g[i] = __builtin_fmaf(along[i], C[i] * v, g[i]);
             }
         }
@@ -217,9 +230,7 @@ template <typename T, int n, bool MARKS, bool GRADS, bool GATE> __device__ __for
 #pragma unroll
     for (int i = 0; i < n; ++i) {
         a.states[(at.slot(a) * n + i) * a.channels + at.channel] = h[i];
-        // (where the decays were no numbers: the limit above has taken them for its own)
-        const float all = A2[i] * steps;
-        if (GRADS) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = all != all ? all : g[i];
+        if (GRADS) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = g[i];
     }
     a.steps[at.slot(a) * a.channels + at.channel] = steps;
 }
@@ -262,19 +273,19 @@ template <int n, int RUNS, int SPAN, bool BACK> __device__ __forceinline__ void 
 #pragma unroll
     for (int k = 0; k < SPAN; ++k)
         if (run * SPAN + k + 1 < used) {
-            s = __builtin_fmaf(kept(A2, sum[k]), s, add[k]);
+            s = carried(A2, sum[k], s, add[k]);
             total += sum[k];
         }
     sums[run][lane] = total;
     ends[run][lane] = s;
     __syncthreads();
     s = from ? from[((int64_t)b * a.channels + c) * n + i] : 0.f;
-    for (int r = 0; r < run; ++r) s = __builtin_fmaf(kept(A2, sums[r][lane]), s, ends[r][lane]);
+    for (int r = 0; r < run; ++r) s = carried(A2, sums[r][lane], s, ends[r][lane]);
 #pragma unroll
     for (int k = 0; k < SPAN; ++k)
         if (run * SPAN + k < used) {
             if (mine <= last) (slots + segment(k) * stride)[at] = s;
-            s = __builtin_fmaf(kept(A2, sum[k]), s, add[k]);
+            s = carried(A2, sum[k], s, add[k]);
         }
 }
 template <int n, int RUNS, int SPAN> __global__ __launch_bounds__(64 * RUNS) void scan_states(ScanArgs a)

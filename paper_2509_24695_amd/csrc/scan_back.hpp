@@ -20,11 +20,12 @@ namespace sv {
 
 // A segment's two sums can be had in one walk forwards, with the decays and the softplus of both worked out once; the gradients' is then of the decays multiplied up.
 // It pays with a gate (2 x 4 680 tokens of 2 240 channels bf16 146 us, in a walk each 170; fp32 170 and 181) and at n = 8 (83 and 91 without a gate);
-// without one, n = 16, a walk each is as fast or faster (bf16 145 and 141, fp32, whose B and C take all scalar registers, 176 and 146).
+// without one, n = 16, a walk each is as fast or faster (bf16 145 and 141, fp32, whose B and C take all scalar registers, 176 and 146).  Where a state grows the
+// product would leave fp32's range before the sum does: a wave with an A > 0 takes a walk each.
 template <int n, bool GATE> constexpr bool kSumsTogether = GATE || n == 8;
 
 // g = C dy of a segment's tokens from its last on, carried to before its first: what the segment adds to the gradient of the state it began from.
-template <typename T, int n> __device__ __forceinline__ void scan_sum_back(const ScanArgs &a, const ScanPlace &at)
+template <typename T, int n, bool GATE> __device__ __forceinline__ void scan_sum_back(const ScanArgs &a, const ScanPlace &at)
 {
     float A2[n], g[n];
     load_rates<n>(a, at.channel, A2);
@@ -33,35 +34,37 @@ template <typename T, int n> __device__ __forceinline__ void scan_sum_back(const
     for (int i = 0; i < n; ++i) g[i] = 0.f;
     const int64_t bc = at.b * a.sbc.b + at.group * a.sbc.h;
     // tokens from the last: token k of the walk is last - 1 - k
-    Ahead<T, kScanBackAhead> dy, dt;
+    Ahead<T, kScanBackAhead> dy, dt, z;
     const int count = at.last - at.first;
     auto request = [&](int k) {
         const int64_t top = at.last - 1;
         dy.request(a.dy, at.y + top * a.sy.n, -a.sy.n, k, count);
         dt.request(a.dt, at.u + top * a.su.n, -a.su.n, k, count);
+        if (GATE) z.request(a.z, at.z + top * a.sz.n, -a.sz.n, k, count);
     };
     request(0);
     Scalars<T, n> next;
     next.load(a.cm, bc + (at.last - 1) * a.sbc.n);
-    auto token = [&](int k, float v, float dtt) {
+    auto token = [&](int k, float v, float dtt, float zt) {
         Scalars<T, n> C = next;
         C.arrive();
         next.load(a.cm, bc + (at.last - 1 - (k + 1 < count ? k + 1 : k)) * a.sbc.n);
         __builtin_amdgcn_sched_barrier(0);                            // not behind the arithmetic
         const float D = softplus(dtt + bias);
+        if (GATE) v *= silu(zt);
 #pragma unroll
         for (int i = 0; i < n; ++i) g[i] = __builtin_amdgcn_exp2f(D * A2[i]) * __builtin_fmaf(C[i], v, g[i]);
     };
     int k0 = 0;
     for (; k0 + kScanBackAhead <= count; k0 += kScanBackAhead) {
-        const Ahead<T, kScanBackAhead> dy0 = dy, dt0 = dt;
+        const Ahead<T, kScanBackAhead> dy0 = dy, dt0 = dt, z0 = z;
         request(k0 + kScanBackAhead);
 #pragma unroll
-        for (int k = 0; k < kScanBackAhead; ++k) token(k0 + k, dy0[k], dt0[k]);
+        for (int k = 0; k < kScanBackAhead; ++k) token(k0 + k, dy0[k], dt0[k], GATE ? z0[k] : 0.f);
     }
 #pragma unroll
     for (int k = 0; k < kScanBackAhead; ++k)
-        if (k0 + k < count) token(k0 + k, dy[k], dt[k]);
+        if (k0 + k < count) token(k0 + k, dy[k], dt[k], GATE ? z[k] : 0.f);
     if (!at.mine) return;
 #pragma unroll
     for (int i = 0; i < n; ++i) a.grads[(at.slot(a) * n + i) * a.channels + at.channel] = g[i];
@@ -71,14 +74,22 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave) 
 {
     if constexpr (kSumsTogether<n, GATE>) {
         const ScanPlace at(a, blockIdx.x);
-        if (at.first < at.length) scan_sum<T, n, true, true, GATE>(a, at);
+        if (at.first >= at.length) return;
+        float A2[n];
+        load_rates<n>(a, at.channel, A2);
+        if (!wave_grows(A2)) {
+            scan_sum<T, n, true, true, GATE>(a, at);
+        } else {
+            scan_sum<T, n, true, false, false>(a, at);
+            if (at.segment > 0) scan_sum_back<T, n, GATE>(a, at);
+        }
     } else {
         const uint32_t half = gridDim.x / 2;
         const bool back = blockIdx.x >= half;
         const ScanPlace at(a, back ? blockIdx.x - half : blockIdx.x);
         if (at.first >= at.length) return;
         if (!back) scan_sum<T, n, true, false, false>(a, at);
-        else if (at.segment > 0) scan_sum_back<T, n>(a, at);
+        else if (at.segment > 0) scan_sum_back<T, n, GATE>(a, at);
     }
 }
 // A sequence of one segment: the marks alone.
@@ -154,6 +165,7 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
     }
     float A2[n], begin[n], g[n], dA[n], dbias = 0.f, dskip = 0.f;
     load_rates<n>(a, at.channel, A2);
+    const bool grows = wave_grows(A2);
     const float bias = a.dt_bias ? a.dt_bias[at.channel] : 0.f, skip = a.skip ? a.skip[at.channel] : 0.f;
     if (a.segments == 1) {
         load_state<n>(a.s_in, (int64_t)at.b * a.channels + at.channel, begin);
@@ -198,9 +210,17 @@ template <typename T, int n, bool GATE> __global__ __launch_bounds__(kScanWave, 
         const Ahead<T, kScanRun> u0 = u, dt0 = dt, z0 = z, dy0 = dy;
         const bool more = t0 > at.first;
         float h[kScanRun + 1][n], D[kScanRun], slope[kScanRun], raw[kScanRun];
-        if (more) {
+        if (more && !grows) {
+            // carried() for exponents below zero, in two halves: each has what fp32 can have beside the largest state
+            const float half = 0.5f * mark_steps;
 #pragma unroll
-            for (int i = 0; i < n; ++i) h[0][i] = __builtin_fmaf(kept(A2[i], mark_steps), begins[i / 4][lane][i % 4], mark[i]);
+            for (int i = 0; i < n; ++i) {
+                const float part = __builtin_amdgcn_exp2f(A2[i] * half);
+                h[0][i] = __builtin_fmaf(part, part * begins[i / 4][lane][i % 4], mark[i]);
+            }
+        } else if (more) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) h[0][i] = carried(A2[i], mark_steps, begins[i / 4][lane][i % 4], mark[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < n; ++i) h[0][i] = begins[i / 4][lane][i % 4];
