@@ -70,8 +70,7 @@ size_t sv_groupnorm_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tok
  *  silu           0 or 1
  *  mean, rstd     fp32 [B][H][groups] device, or both NULL: kept for the backward pass
  *  eps            >= 0 and finite (0 with a group of equal values gives infinities or NaN)
- * Sums are fp64 (of eight numbers at a time fp32 where a workgroup holds a group).  Conventions and errors as in sv_linattn.h; plain kernels, which may be captured into a HIP graph from the first call
- * on; two calls that overlap in time need a workspace each; results are bit-reproducible. */
+ * Sums are fp64.  Conventions and errors as in sv_linattn.h; plain kernels, which may be captured into a HIP graph from the first call on; two calls that overlap in time need a workspace each; results are bit-reproducible. */
 sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const float *weight, const float *bias, int32_t groups, float eps,
                        int32_t silu, void *Y, const sv_tensor_desc *y, float *mean, float *rstd, void *workspace,
                        size_t workspace_bytes, void *stream);

@@ -190,27 +190,20 @@ template <typename T, bool WIDE> __global__ __launch_bounds__(kGroupThreads) voi
     group_store_sums<!WIDE, WIDE>(a, at, s, q, false);
 }
 
-// A workgroup's sums of two numbers, for all of its threads (`lds`: two for each wave).
-template <int THREADS> __device__ __forceinline__ void group_total(double &s, double &q, double *lds)
+// A workgroup's sums of one number or two, for all of its threads (`lds`: as many for each wave).
+template <int THREADS, typename... Q> __device__ __forceinline__ void group_total(double *lds, Q &...q)
 {
+    constexpr int kNumbers = sizeof...(q);
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        s += __shfl_xor(s, m, 64);
-        q += __shfl_xor(q, m, 64);
-    }
+    for (int m = 1; m < 64; m *= 2) ((q += __shfl_xor(q, m, 64)), ...);
     __syncthreads();
-    if (threadIdx.x % 64 == 0) {
-        lds[threadIdx.x / 64 * 2] = s;
-        lds[threadIdx.x / 64 * 2 + 1] = q;
-    }
+    double *own = lds + threadIdx.x / 64 * kNumbers;
+    if (threadIdx.x % 64 == 0) ((*own++ = q), ...);
     __syncthreads();
-    s = lds[0];
-    q = lds[1];
+    const double *at = lds;
+    ((q = *at++), ...);
 #pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) {
-        s += lds[2 * w];
-        q += lds[2 * w + 1];
-    }
+    for (int w = 1; w < THREADS / 64; ++w) ((q += *at++), ...);
 }
 
 // A group's two sums over its chunks and channels: f(channel, address of the first sum).
@@ -269,7 +262,7 @@ __global__ __launch_bounds__(kGroupThreads) void group_fold(GroupArgs a)
             s += x;
             q += xx;
         });
-    group_total<kGroupThreads>(s, q, lds);
+    group_total<kGroupThreads>(lds, s, q);
     if (threadIdx.x) return;
     const double over = 1. / ((double)a.N * a.width), mean = s * over;
     const float m = (float)mean, r = group_scale(__builtin_fma(-mean, s, q), over, a.eps);
@@ -401,7 +394,7 @@ __global__ __launch_bounds__(kGroupThreads) void group_back_fold(GroupArgs a)
                 s = __builtin_fma(w, (double)p, s);
                 q = __builtin_fma(w, (double)px, q);
             });
-        group_total<kGroupThreads>(s, q, lds);
+        group_total<kGroupThreads>(lds, s, q);
         const double over = 1. / ((double)a.N * a.width);
         if (threadIdx.x == 0) {
             a.level[id] = (float)(s * over);

@@ -1,6 +1,6 @@
 // Group norm of groups that one workgroup holds in registers: read once, one launch (a second one backwards, for the
-// parameters' gradients).  A thread has the same channels in all of its rows.  Three batches of 901 rows of 320 channels in 32 groups fp32: 9 us, in three launches
-// 12.6.  Bound by its own run through a launch: loads, two joins of 1 024 threads, stores.  Groups of twice the size (64 words a thread) lose: 21 frames of
+// parameters' gradients).  A thread has the same channels in all of its rows.  Three batches of 901 rows of 320 channels in 32 groups fp32: 8.7 us, in three launches
+// 12.6; 84 frames of 64 rows of 320 channels 30.  Bound by its own run through a launch: loads, two joins of 1 024 threads, stores.  Groups of twice the size (64 words a thread) lose: 21 frames of
 // 1 560 x 2 240 took 100 us, as nothing overlaps the arithmetic of the one workgroup on a compute unit.
 #pragma once
 
@@ -72,6 +72,12 @@ template <typename V, int ROWS> __device__ __forceinline__ void held_again(V (&v
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) asm volatile("" : "+v"(v[i]));
 }
+// The same for a row of a pass that ends before the next.  (Without it the compiler gathers all rows' numbers into one long vector, which spills.)
+template <typename P, int N> __device__ __forceinline__ void held_open(typename P::V v, float (&x)[N])
+{
+    asm volatile("" : "+v"(v));
+    P::open(v, x);
+}
 template <typename V> __device__ __forceinline__ void held_store(void *p, V v, bool past_caches)
 {
     if constexpr (sizeof(V) == 16) store16(p, v, past_caches);
@@ -90,59 +96,44 @@ template <typename T, int UNIT, int ROWS, bool SILU> __global__ __launch_bounds_
     float w[kN], b[kN];
     of_channel<kN>(a.weight, at.c, 1.f, w);
     of_channel<kN>(a.bias, at.c, 0.f, b);
-    // Sums of eight numbers at a time in fp32, of these in fp64: off by at most eight roundings of the numbers' magnitudes.  The squares are of what
-    // is left of the mean, so nothing cancels.
-    constexpr int kBlock = 8 / kN < ROWS ? 8 / kN : ROWS;
-    double s = 0., q = 0., none = 0.;
+    // Every number is added up in fp64, and so is the square of what is left of the fp64 mean: neither overflows for any fp32 rows, and constant groups
+    // have a variance of zero.
+    double s = 0., q = 0.;
 #pragma unroll
-    for (int i0 = 0; i0 < ROWS; i0 += kBlock)
-        if (i0 <= at.all) {
-            float part = 0.f;
+    for (int i = 0; i < ROWS; ++i)
+        if (i < at.rows) {
+            float x[kN];
+            held_open<P>(v[i], x);
 #pragma unroll
-            for (int i = i0; i < i0 + kBlock; ++i)
-                if (i < ROWS && i <= at.all) {
-                    float x[kN];
-                    P::open(v[i], x);
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) part += i < at.rows ? x[e] : 0.f;
-                }
-            s += part;
+            for (int e = 0; e < kN; ++e) s += x[e];
         }
-    group_total<kHeldThreads>(s, none, lds);
-    const double over = 1. / ((double)a.N * a.width);
-    const float mean = (float)(s * over);
-    held_again(v);
+    group_total<kHeldThreads>(lds, s);
+    const double over = 1. / ((double)a.N * a.width), exact = s * over;
+    const float mean = (float)exact;
 #pragma unroll
-    for (int i0 = 0; i0 < ROWS; i0 += kBlock)
-        if (i0 <= at.all) {
-            float part = 0.f;
+    for (int i = 0; i < ROWS; ++i)
+        if (i < at.rows) {
+            float x[kN];
+            held_open<P>(v[i], x);
 #pragma unroll
-            for (int i = i0; i < i0 + kBlock; ++i)
-                if (i < ROWS && i <= at.all) {
-                    float x[kN];
-                    P::open(v[i], x);
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) {
-                        const float left = i < at.rows ? x[e] - mean : 0.f;
-                        part = __builtin_fmaf(left, left, part);
-                    }
-                }
-            q += part;
+            for (int e = 0; e < kN; ++e) {
+                const double left = x[e] - exact;
+                q = __builtin_fma(left, left, q);
+            }
         }
-    group_total<kHeldThreads>(q, none, lds);
+    group_total<kHeldThreads>(lds, q);
     const float rstd = group_scale(q, over, a.eps);
     if (a.mean && threadIdx.x == 0) {
         a.mean[at.id] = mean;
         a.rstd[at.id] = rstd;
     }
     if (!at.mine) return;
-    held_again(v);
     T *y = const_cast<T *>(at.at(a, a.y, a.sy)) + at.line * a.sy.n;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
         if (i <= at.all) {
             float x[kN];
-            P::open(v[i], x);
+            held_open<P>(v[i], x);
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
                 x[e] = __builtin_fmaf((x[e] - mean) * rstd, w[e], b[e]);
@@ -191,7 +182,7 @@ template <typename T, int UNIT, int ROWS, bool SILU, bool PARAMS> __global__ __l
         s = __builtin_fma((double)w[e], (double)p[e], s);
         q = __builtin_fma((double)w[e], (double)px[e], q);
     }
-    group_total<kHeldThreads>(s, q, lds);
+    group_total<kHeldThreads>(lds, s, q);
     const double over = 1. / ((double)a.N * a.width);
     const float level = (float)(s * over), along = (float)(q * over);
     if (at.mine) {
