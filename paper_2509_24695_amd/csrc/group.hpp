@@ -7,8 +7,9 @@
 // 1 560 rows of 2 240 channels in 32 groups bf16 85 us, 31 for the sums (4.8 TB/s) and 50 for the rows (5.9 TB/s; a reading and a copying pass 80); backwards 14 040 rows
 // 62 us, 26 for the sums (4.8 TB/s), 5 for the fold and 32 (5.9 TB/s).  A thread keeps the same eight (fp32: four)
 // channels for all of its rows, so groups need not be whole pieces: sums are kept by channel, and group_fold adds up a group's channels and chunks.
-// Forwards the sums of x and x^2 are fp64, in which products of tensor values are exact: no cancellation shows for any mean that
-// fp32 rows can have.
+// Forwards the sums are of x - x0 and its square in fp64, x0 the group's first number.  As one of the group's `count` numbers x0 is at most sqrt(count)
+// deviations from the mean, so the variance loses at most count fp64 roundings to cancellation however far from zero the rows lie (without x0, rows
+// of 1e6 with a deviation of 0.1 had an rstd that was 0.6 % off).
 #pragma once
 
 #include "activation.hpp"
@@ -24,10 +25,10 @@ struct GroupArgs {
     void *y;                               // backward: dx
     TokStrides sx, sdy, sy;
     const float *weight, *bias;            // [d] or NULL
-    double *sums;                          // [BH][chunks][2][d]: of x and x^2 (backward fp32, of da and da xh)
+    double *sums;                          // [BH][chunks][2][d]: of x - x0 and its square (backward fp32, of da and da xh)
     double *pairs;                         // [BH][chunks][tiles][per_tile][2]: the same by group (backward of t and t xh); NULL: groups are narrow
     int per_tile, sum_tiles, tile_width;   // groups and channels of a tile of the launch that writes them
-    float *level, *scale;                  // [BH][G]: mean and rstd; backward: sum t / count and sum (t xh) / count
+    float *level, *scale;                  // [BH][G]: x0, then mean, and rstd; backward: sum t / count and sum (t xh) / count
     float *mean, *rstd;                    // [BH][G]: outputs, or backward inputs
     float *dw, *db;
     int H, N, d, G, width;                 // width: channels of a group
@@ -176,17 +177,32 @@ template <typename T, bool WIDE> __global__ __launch_bounds__(kGroupThreads) voi
     double s[kN], q[kN];
 #pragma unroll
     for (int e = 0; e < kN; ++e) s[e] = q[e] = 0.;
-    if (at.mine)
+    if (at.mine) {
+        float from[kN];
+        const T *row = at.at(a, a.x, a.sx) - at.c;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const float first = Elem<T>::load(row + a.width_div.quotient(at.c + e) * a.width);
+            from[e] = __builtin_isfinite(first) ? first : 0.f;        // (an infinity's mean is that infinity)
+        }
         group_walk<T, P, false>(a, at, [&](int64_t, V vx, V) {
             float x[kN];
             P::open(vx, x);
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
-                const double v = x[e];
+                const double v = (double)x[e] - from[e];
                 s[e] += v;
                 q[e] = __builtin_fma(v, v, q[e]);
             }
         });
+        // x0 for the next launch, which may write into the rows
+        if (at.chunk == 0 && at.line == 0)
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                const int g = (int)a.width_div.quotient(at.c + e);
+                if (at.c + e == g * a.width) a.level[(int64_t)at.bh * a.G + g] = from[e];
+            }
+    }
     group_store_sums<!WIDE, WIDE>(a, at, s, q, false);
 }
 
@@ -243,7 +259,7 @@ __device__ __forceinline__ void group_gather_pairs(const GroupArgs &a, int64_t b
     }
 }
 
-// mean and rstd from a group's sums of x and (x - from)^2
+// rstd from a group's sum of squares of deviations
 __device__ __forceinline__ float group_scale(double squares, double over, float eps)
 {
     const double var = squares * over;
@@ -264,8 +280,8 @@ __global__ __launch_bounds__(kGroupThreads) void group_fold(GroupArgs a)
         });
     group_total<kGroupThreads>(lds, s, q);
     if (threadIdx.x) return;
-    const double over = 1. / ((double)a.N * a.width), mean = s * over;
-    const float m = (float)mean, r = group_scale(__builtin_fma(-mean, s, q), over, a.eps);
+    const double over = 1. / ((double)a.N * a.width), past = s * over;
+    const float m = (float)(a.level[id] + past), r = group_scale(__builtin_fma(-past, s, q), over, a.eps);
     a.level[id] = m;
     a.scale[id] = r;
     if (a.mean) {
@@ -293,13 +309,13 @@ template <typename T, bool SILU, bool FOLD> __global__ __launch_bounds__(kGroupT
                 s += __shfl_xor(s, m, 64);
                 q += __shfl_xor(q, m, 64);
             }
-            const double over = 1. / ((double)a.N * a.width), m = s * over;
-            const float r = group_scale(__builtin_fma(-m, s, q), over, a.eps);
+            const double over = 1. / ((double)a.N * a.width), past = s * over;
+            const float m = (float)(a.level[(int64_t)at.bh * a.G + g] + past), r = group_scale(__builtin_fma(-past, s, q), over, a.eps);
             if (lane == 0) {
-                stats[0][g - first] = (float)m;
+                stats[0][g - first] = m;
                 stats[1][g - first] = r;
                 if (a.mean && at.chunk == 0 && g * a.width >= c0) {
-                    a.mean[(int64_t)at.bh * a.G + g] = (float)m;
+                    a.mean[(int64_t)at.bh * a.G + g] = m;
                     a.rstd[(int64_t)at.bh * a.G + g] = r;
                 }
             }

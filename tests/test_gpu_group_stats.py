@@ -1,5 +1,5 @@
-"""Statistics of the group norm where sums are hardest: constant groups, groups far from zero, and numbers whose squares fp32 does not hold; which have to agree with
-64 bits all the same.
+"""Statistics of the group norm where sums are hardest: constant groups, groups far from zero, and numbers whose squares fp32 does not hold; each for groups that a workgroup
+holds and for streamed ones, which have to agree with 64 bits alike.
 
 Bounds: sums are of fp64, of at most 2^21 numbers, off by less than 2^11 fp64 roundings (2^-42 of the terms).  So the mean is off by its rounding to fp32, and rstd by its own;
 what is left of the sums' errors is 1e-6 of the mean's distance from the numbers and 2 % of a rounding of rstd."""
@@ -12,8 +12,9 @@ from tests.selective_util import E, U, draw, f64, like, space
 
 pytestmark = pytest.mark.gpu
 
-# rows, d, groups: held by one workgroup in units of 16, 4 and 2 bytes (or 4)
-SHAPES = [(64, 16, 2), (4090, 16, 2), (61, 48, 8), (50, 40, 8)]
+# rows, d, groups: held by one workgroup in units of 16, 4 and 2 bytes (or 4), and streamed: narrow groups, wide ones whose sums the next launch adds up, wide ones with a
+# launch for it, groups across tiles
+SHAPES = [(64, 16, 2), (4090, 16, 2), (61, 48, 8), (50, 40, 8), (70000, 16, 2), (1500, 512, 4), (3000, 512, 4), (5000, 520, 1)]
 # name, dtype, (level, spread), eps
 GROUPS = [
     ("constant", "f32", (10000.123, 0.0), 1e-5), ("constant", "f32", (-65000.7, 0.0), 1e-5), ("constant", "f32", (1234567.9, 0.0), 1e-5), ("constant", "bf16", (1e4, 0.0), 1e-5),
