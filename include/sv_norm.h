@@ -70,6 +70,8 @@ size_t sv_groupnorm_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tok
  *  silu           0 or 1
  *  mean, rstd     fp32 [B][H][groups] device, or both NULL: kept for the backward pass
  *  eps            >= 0 and finite (0 with a group of equal values gives infinities or NaN)
+ *  workspace      of every call, small ones that leave it untouched among them
+ * Refused (SV_ERR_SHAPE) where a launch would have 2^24 workgroups or more: at B H groups + d / 8 or B H (d + 127) / 128 of that many.
  * Sums are fp64.  Conventions and errors as in sv_linattn.h; plain kernels, which may be captured into a HIP graph from the first call on; two calls that overlap in time need a workspace each; results are bit-reproducible. */
 sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const float *weight, const float *bias, int32_t groups, float eps,
                        int32_t silu, void *Y, const sv_tensor_desc *y, float *mean, float *rstd, void *workspace,

@@ -75,4 +75,10 @@ SV_HOST_DEVICE inline uint32_t held_task(uint32_t id, uint32_t grid) { return id
 
 constexpr int kHeldForwardWords = 32, kHeldBackwardWords = 16;      // (a thread of 1 024 has 128 registers)
 
+// The form of a whole call: more groups than a launch has workgroups (lanes are counted in 32 bits) are streamed like those that do not fit.
+inline HeldForm held_form(int64_t N, int64_t width_bytes, int most, int64_t groups)
+{
+    return held_grid(groups) * kHeldThreads < (int64_t)1 << 32 ? held_form(N, width_bytes, most) : HeldForm{};
+}
+
 }  // namespace sv

@@ -83,14 +83,13 @@ template <int MOST, typename F> void with_held(bool bf16, const HeldForm &form, 
     if (bf16) sized(uint16_t{}, two), sized(uint16_t{}, four), sized(uint16_t{}, sixteen);
     else sized(float{}, four), sized(float{}, sixteen);
 }
-// Gives a launch the form; its workgroups, 0: more than a launch has.
+// Gives a launch the form; its workgroups.
 unsigned held_args(GroupArgs &a, const HeldForm &form, int elem_bytes)
 {
     a.across = form.across;
     a.lines = form.lines;
     a.whole_lines = a.whole_lines && a.width * elem_bytes % 128 == 0;
-    const int64_t grid = held_grid(a.BH * a.G);
-    return grid_ok(grid, kHeldThreads) ? (unsigned)grid : 0;
+    return (unsigned)held_grid(a.BH * a.G);
 }
 
 size_t workspace_bytes_of(int32_t B, int32_t H, int32_t N, int32_t d, int32_t groups, size_t number)
@@ -134,9 +133,8 @@ extern "C" sv_status sv_groupnorm(const void *X, const sv_tensor_desc *x, const 
     a.weight = weight; a.bias = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
     a.whole_lines = lines_whole(out);
     const auto hs = static_cast<hipStream_t>(stream);
-    if (const HeldForm held = held_form(a.N, (int64_t)a.width * in.elem_bytes, kHeldForwardWords); held.unit) {
+    if (const HeldForm held = held_form(a.N, (int64_t)a.width * in.elem_bytes, kHeldForwardWords, a.BH * a.G); held.unit) {
         const unsigned grid = held_args(a, held, in.elem_bytes);
-        if (!grid) return SV_ERR_SHAPE;
         with_held<kHeldForwardWords>(in.bf16, held, [&](auto t, auto unit, auto rows) {
             if (silu) group_held<decltype(t), unit(), rows(), true><<<grid, kHeldThreads, 0, hs>>>(a);
             else group_held<decltype(t), unit(), rows(), false><<<grid, kHeldThreads, 0, hs>>>(a);
@@ -195,9 +193,8 @@ extern "C" sv_status sv_groupnorm_backward(const void *X, const sv_tensor_desc *
     const auto hs = static_cast<hipStream_t>(stream);
     const bool params = dweight || dbias;
     const int64_t param_folds = params ? (2 * a.d + 15) / 16 : 0;
-    if (const HeldForm held = held_form(a.N, (int64_t)a.width * in.elem_bytes, kHeldBackwardWords); held.unit) {
+    if (const HeldForm held = held_form(a.N, (int64_t)a.width * in.elem_bytes, kHeldBackwardWords, a.BH * a.G); held.unit) {
         const unsigned grid = held_args(a, held, in.elem_bytes);
-        if (!grid) return SV_ERR_SHAPE;
         with_held<kHeldBackwardWords>(in.bf16, held, [&](auto t, auto unit, auto rows) {
             auto go = [&](auto act, auto p) { group_held_back<decltype(t), unit(), rows(), act(), p()><<<grid, kHeldThreads, 0, hs>>>(a); };
             auto with = [&](auto act) {
