@@ -18,6 +18,8 @@ struct ScanPlan {
 
 // As many waves as run at once, forwards four on a SIMD, backwards two; forwards twice as many where segments are long enough for it (a state
 // that is handed on costs 16 bytes of traffic a number): 32 760 tokens of 2 240 channels without a gate 490 us, with four 545; 8 190 tokens 181 and 168.
+// Not where the sequences alone fill them by more than half: a first cut brings the sums with it (64, 100 and 117 sequences of 512 tokens of 2 240 channels
+// 406, 504 and 508 us, in three, two and two segments 481, 673 and 771; of 1 560 tokens 1 223, 1 526 and 1 533, cut 1 347, 1 918 and 2 209).
 constexpr int kScanMostSegments = 512, kScanLongSegment = 128;
 constexpr int64_t kScanForwardWaves = 4096, kScanBackwardWaves = 2048;
 
@@ -28,7 +30,7 @@ inline int64_t scan_longest_chain(int64_t n_tokens)
 }
 inline int64_t scan_most_segments(int64_t B, int64_t n_tokens, int64_t blocks, int64_t waves)
 {
-    int64_t s = waves / (B * blocks), more = waves == kScanForwardWaves ? 2 * waves / (B * blocks) : 0;
+    int64_t s = waves / (B * blocks), more = waves == kScanForwardWaves && s > 1 ? 2 * waves / (B * blocks) : 0;
     if (more > n_tokens / kScanLongSegment) more = n_tokens / kScanLongSegment;
     if (s < more) s = more;
     const int64_t longest = scan_longest_chain(n_tokens);

@@ -33,3 +33,12 @@ def test_long_cases(plans):
 def test_growth_cases(plans):
     for (c, _, _, per, segments), (f, b) in zip(test_gpu_scan_growth.CASES, plans([_call(c[0]) for c in test_gpu_scan_growth.CASES])):
         assert per == max(f[1], b[1]) and segments >= max(f[0], b[0])
+
+
+def test_sequences_that_fill_the_machine_are_not_cut(plans):
+    """More than half of the waves that run at once without a cut (4 096 forwards, 2 048 backwards): the sums of a cut cost more than its waves bring."""
+    sequences = list(range(1, 200))
+    for N in (512, 1560, 32760):
+        for B, (f, b) in zip(sequences, plans([(B, 1, 2240, N) for B in sequences])):
+            waves = 35 * B
+            assert (f[0] == 1) == (waves > 2048) and (b[0] == 1) == (waves > 1024), (B, N, f, b)
