@@ -35,6 +35,8 @@
  *  - A NaN or an infinity makes what depends on it by the formulas NaN or infinite; outputs of earlier tokens are what they would be
  *    without it, and so are gradients at later ones.
  *  - Outputs must not overlap inputs or each other, but for S_out = S_in and dS_in = dS_out.
+ *  - SV_ERR_SHAPE where H d is 2^27 or more, or where a launch would have 2^26 waves or more: one for 64 channels of a group of each sequence, twice as many
+ *    backwards (and one for B G N n / 32), n / 4 times as many for single tokens.
  */
 #ifndef SV_SCAN_H
 #define SV_SCAN_H
@@ -47,7 +49,8 @@ extern "C" {
 
 /* Bytes of device workspace of sv_selective_scan and of sv_selective_scan_backward for these sizes (either dtype; G groups, n numbers of state a channel);
  * contents need no preparation.  What a call needs does for every call with no more batches and tokens and the same H, d, G and n.
- * Pure host functions; 0 for unsupported arguments. */
+ * Backwards it is mostly n + 1 fp32 numbers for every four tokens of a channel: 17 bytes a token and channel at n = 16 (1.25 GB for 32 760 tokens
+ * of 2 240 channels).  Every call takes a workspace, a sequence of few tokens that leaves it untouched among them.  Pure host functions; 0 for unsupported arguments. */
 size_t sv_selective_scan_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t n);
 size_t sv_selective_scan_backward_workspace_bytes(int32_t B, int32_t H, int32_t n_tokens, int32_t d, int32_t G, int32_t n);
 

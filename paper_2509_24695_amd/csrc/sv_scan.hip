@@ -120,7 +120,7 @@ extern "C" sv_status sv_selective_scan(const void *U, const void *DT, const sv_t
     const int64_t states = (int64_t)a.B * a.segments * a.channels * n, waves = (int64_t)a.B * a.segments * a.blocks;
     if (a.segments > 1 && workspace_bytes < (size_t)(states + states / n) * sizeof(float)) return SV_ERR_WORKSPACE;
     const int64_t scan = (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
-    if (!grid_ok(waves, kScanWave) || !grid_ok(scan, 1024)) return SV_ERR_SHAPE;
+    if (!grid_ok(waves, kScanWave) || (a.segments > 1 && !grid_ok(scan, 1024))) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.y = Y;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.s_out = S_out;
@@ -199,7 +199,7 @@ extern "C" sv_status sv_selective_scan_backward(const void *U, const void *DT, c
     if (workspace_bytes < (size_t)space.total * sizeof(float)) return SV_ERR_WORKSPACE;
     const int64_t waves = (int64_t)a.B * a.segments * a.blocks, states = 2 * (int64_t)a.B * (((int64_t)a.channels * n + 63) / 64);
     const int64_t shared = ((int64_t)a.B * a.G * a.N * 2 * n + 255) / 256, params = dA || ddt_bias || dskip ? ((int64_t)a.channels * (n + 2) + 255) / 256 : 0;
-    if (!grid_ok(2 * waves, kScanWave) || !grid_ok(states, 1024) || !grid_ok(shared + params, 256)) return SV_ERR_SHAPE;
+    if (!grid_ok(2 * waves, kScanWave) || (a.segments > 1 && !grid_ok(states, 1024)) || !grid_ok(shared + params, 256)) return SV_ERR_SHAPE;
     a.u = U; a.dt = DT; a.z = Z; a.bm = Bm; a.cm = Cm; a.dy = dY;
     a.A = A; a.dt_bias = dt_bias; a.skip = skip; a.lengths = lengths;
     a.s_in = S_in; a.ds_out = dS_out;
