@@ -25,6 +25,8 @@
  *  - Sums are fp32; outputs and caches are rounded once (caches are copies).
  *  - A NaN or an infinity reaches what depends on it by the formulas and nothing else.
  *  - Outputs must not overlap inputs or each other, but for cache_out = cache_in where that is said.
+ *  - SV_ERR_SHAPE where H d is 2^28 or more, or where a launch would have 2^31 threads or more (one for 16 bytes of four to sixteen tokens, backwards for four channels of
+ *    eight to 64, 2^24 workgroups at most).
  */
 #ifndef SV_CONV_H
 #define SV_CONV_H

@@ -4,7 +4,7 @@
 //   da = dy or dy silu'(a),  t = w da,  dx = rstd (t - sum t / count - xh sum (t xh) / count),  dw = sum da xh,  db = sum da
 //
 // Bound by memory, twice over: a pass for the sums and one for the rows (a copy is as slow out of the cache behind the L2s as out of memory).  21 frames of
-// 1 560 rows of 2 240 channels in 32 groups bf16 85 us, 31 for the sums (4.8 TB/s) and 50 for the rows (5.9 TB/s; a reading and a copying pass 80); backwards 14 040 rows
+// 1 560 rows of 2 240 channels in 32 groups bf16 86 us, 32 for the sums (4.6 TB/s) and 54 for the rows (5.4 TB/s; a reading and a copying pass 80); backwards 14 040 rows
 // 62 us, 26 for the sums (4.8 TB/s), 5 for the fold and 32 (5.9 TB/s).  A thread keeps the same eight (fp32: four)
 // channels for all of its rows, so groups need not be whole pieces: sums are kept by channel, and group_fold adds up a group's channels and chunks.
 // Forwards the sums are of x - x0 and its square in fp64, x0 the group's first number.  As one of the group's `count` numbers x0 is at most sqrt(count)

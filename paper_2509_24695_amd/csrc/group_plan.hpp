@@ -68,7 +68,7 @@ inline HeldForm held_form(int64_t N, int64_t width_bytes, int most)
     return f;
 }
 // Workgroup ids go round the dies (one L2 each); a die takes a run of neighbouring groups, whose parts of a row share lines (901 x 3 rows of 32 groups of ten channels
-// fp32 9.6 us, dealt singly 11.0).  For ids below 8 ceil(groups / 8); a task past the last group is none.
+// fp32 9.6 us, dealt singly 11.0, with the sums of the time).  For ids below 8 ceil(groups / 8); a task past the last group is none.
 constexpr int kGroupDies = 8;
 inline int64_t held_grid(int64_t groups) { return (groups + kGroupDies - 1) / kGroupDies * kGroupDies; }
 SV_HOST_DEVICE inline uint32_t held_task(uint32_t id, uint32_t grid) { return id % kGroupDies * (grid / kGroupDies) + id / kGroupDies; }

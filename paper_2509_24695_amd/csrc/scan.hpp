@@ -6,8 +6,8 @@
 // by the vector unit: an exponential and four other instructions for each state, with softplus and the gate beside them.  A long sequence
 // is cut into segments that are walked side by side: scan_sums finds what each segment adds to a state of nothing and its sum of steps,
 // scan_states turns these into the states the segments begin from (what a segment keeps of its state is exp(A sum D)), and scan_walk
-// walks from there.  32 760 tokens of 2 240 channels, n = 16, with a gate, bf16: 488 us, the sums 223, the states 26, the walk 302 under the profiler's clock (590 MB;
-// an exponential costs 2.2 instructions, the walk 117 instructions a value and token: at the rate that the vector unit reaches, 36 T a second, 182 and 280 us).  Decays that are
+// walks from there.  32 760 tokens of 2 240 channels, n = 16, with a gate, bf16: 491 us (590 MB); under the profiler, whose clock is lower, the sums 219, the states 28, the walk 297
+// (an exponential costs 2.2 instructions, the walk 117 instructions a value and token: at the rate that the vector unit reaches, 36 T a second, 182 and 280 us).  Decays that are
 // kept instead of worked out twice would be 64 bytes a value.
 #pragma once
 
